@@ -287,6 +287,101 @@ SNN_API snn_status_t snn_conv_stack_destroy(snn_conv_stack_t* s);
 SNN_API snn_status_t snn_conv_forward_static(const snn_conv_desc_t* desc, const void* act_dev, int32_t N, int32_t H,
                                              int32_t W, void* out_dev, int32_t out_type, void* cuda_stream);
 
+/*
+ * Projections of language models: 1x1 layers (ksize 1, stride 1) applied to rows of 16-bit activations.
+ * A row is one token's activations [c_in]; a projection gives  alpha[co] * sum_ci W[co][ci] * x[ci],  summed in
+ * fp32, with one rounding to the output type.  (The paper's layers are convolutions on maps; a token is a map
+ * of one pixel, and its appendix's 8-channel vectors are the stored form of W.)  These entry points take row
+ * counts at the call, some of them from the device, where layers, groups and stacks fix their shapes before.
+ *
+ * Types: activations SNN_ACT_F16 or SNN_ACT_BF16 (not the type the layers were created for), outputs SNN_OUT_F32,
+ * SNN_OUT_F16 or SNN_OUT_BF16.  SNN_ACT_BF16, SNN_OUT_F16 and SNN_OUT_BF16 are for these entry points only.
+ * Rows lie ld elements apart (ld >= the row's length); rows of activations are 16-byte aligned (pointer, and ld a
+ * multiple of 8), rows of outputs aligned to their element.  Weights are +1 / -1, so an infinity or NaN in a row's
+ * activations reaches that row's outputs and no others.
+ * All calls are asynchronous on cuda_stream (NULL: the default stream of the handle's device, or of `device`) and
+ * allocate nothing; workspaces are the caller's, so calls on different streams, and captured graphs, share nothing
+ * but what the caller lets them share.  Calls may overlap.  Errors: INVALID_ARG, UNSUPPORTED, CUDA, TIMEOUT (an
+ * earlier launch of the handle gave up a bounded wait).
+ */
+enum { SNN_ACT_BF16 = 2 };
+enum { SNN_OUT_F16 = 3, SNN_OUT_BF16 = 4 };
+
+/*
+ * Matrix products grouped by expert: `count` projections of one shape, and rows of activations in the order of
+ * their experts:
+ *   out[i] = projection_e(act[row_i]),  offsets[e] <= i < offsets[e + 1],  row_i = rows[i], or i where rows is NULL.
+ *
+ * snn_conv_experts_create: `layers` are `count` (1..SNN_EXPERTS_MAX) 1x1 handles with stride 1, all of one c_in and
+ * c_out on one device, of any codebooks, tau and activation type.  The weights are copied into a layout of their own (one bit per
+ * weight, device memory owned by the handle): the layers may be destroyed afterwards.  Synchronous.
+ *
+ * snn_conv_experts_forward: act_dev holds act_rows rows, out_dev max_rows rows.  offsets_dev (DEVICE, count + 1 ints)
+ * and rows_dev (DEVICE, max_rows ints) are read on the device, so a router's results need not visit the host.
+ * offsets must not fall and lie in [0, max_rows]; what lies outside is taken for the nearest end.  An expert may have no rows.
+ * Rows of the output below offsets[0] and from offsets[count] on are left as they are.  A row index outside
+ * [0, act_rows) stands for a row of zeros.  (max_rows is a bound; only rows that experts have cost time.)
+ */
+#define SNN_EXPERTS_MAX 1024
+typedef struct snn_conv_experts snn_conv_experts_t; /* opaque; owned by the library */
+SNN_API snn_status_t snn_conv_experts_create(snn_conv_t* const* layers, int32_t count, snn_conv_experts_t** out);
+SNN_API snn_status_t snn_conv_experts_forward(snn_conv_experts_t* e, const void* act_dev, int32_t act_type,
+                                              int32_t act_rows, int64_t ld_act, const int32_t* rows_dev,
+                                              const int32_t* offsets_dev, int32_t max_rows, void* out_dev,
+                                              int32_t out_type, int64_t ld_out, void* cuda_stream);
+SNN_API snn_status_t snn_conv_experts_destroy(snn_conv_experts_t* e);
+
+/*
+ * The router in front of them.  logits [tokens][experts] (DEVICE, ld elements apart; `type` SNN_OUT_F32, SNN_OUT_F16
+ * or SNN_OUT_BF16).  For each token the top_k (1..SNN_ROUTE_TOP_MAX, at most experts) largest logits, equal ones in
+ * the order of the experts, the largest first; an expert whose logit is -infinity or NaN is not chosen.  Written (all DEVICE):
+ *   ids      [tokens][top_k]  the experts, -1 where fewer than top_k can be chosen
+ *   weights  [tokens][top_k]  exp(logit - largest) / sum, the sum over the chosen experts (normalise != 0) or over
+ *                             all that could be chosen; 0 where the id is -1.  (Largest +infinity: those that have it
+ *                             count 1 and the others 0.)
+ *   offsets  [experts + 1]    where each expert's rows begin, as snn_conv_experts_forward reads them
+ *   rows     [tokens * top_k] the token of each row, ordered by expert, then token; -1 from offsets[experts] on
+ *   slots    [tokens][top_k]  the row of each choice, -1 where the id is -1
+ * work_dev: snn_conv_experts_route_work(tokens, experts) bytes (may be 0), 4-byte aligned, written by the call.
+ */
+#define SNN_ROUTE_TOP_MAX 16
+SNN_API int64_t snn_conv_experts_route_work(int32_t tokens, int32_t experts);
+SNN_API snn_status_t snn_conv_experts_route(const void* logits_dev, int32_t type, int32_t tokens, int32_t experts,
+                                            int64_t ld, int32_t top_k, int32_t normalise, int32_t* ids_dev,
+                                            float* weights_dev, int32_t* offsets_dev, int32_t* rows_dev,
+                                            int32_t* slots_dev, void* work_dev, int32_t device, void* cuda_stream);
+
+/*
+ * What the experts gave, back in the order of the tokens:
+ *   out[t] = sum_j weights[t][j] * y[slots[t][j]],  j < top_k, in fp32 in the order of j, one rounding to out_type.
+ * y: [y_rows][columns] of y_type (an SNN_OUT_* type as above); a slot outside [0, y_rows) counts nothing, whatever its
+ * weight, so a token without any becomes a row of zeros.
+ */
+SNN_API snn_status_t snn_conv_experts_combine(const void* y_dev, int32_t y_type, int32_t y_rows, int64_t ld_y,
+                                              const int32_t* slots_dev, const float* weights_dev, int32_t tokens,
+                                              int32_t top_k, int32_t columns, void* out_dev, int32_t out_type,
+                                              int64_t ld_out, int32_t device, void* cuda_stream);
+
+/*
+ * Low-rank adapters of many requests beside one shared projection:
+ *   out[r] = projection(act[r]) + scale[a] * B[a] (A[a] act[r]),  a = adapter[r] (DEVICE, rows ints),
+ * or the projection alone where a lies outside [0, adapters).  A [adapters][rank][c_in] and B [adapters][c_out][rank]
+ * are dense DEVICE arrays of the activations' type, 16-byte aligned, read at the call (an adapter may be replaced between
+ * calls); scale [adapters] fp32.  rank: a multiple of 8, 8..SNN_ADAPTERS_RANK_MAX (adapters of a lower rank have
+ * zeros in A and B).  A x is kept in fp32 and added to alpha * S in fp32.
+ * work_dev: rows * rank floats, 16-byte aligned, written by the call.
+ * snn_conv_adapters_create: a 1x1 handle with stride 1; copied as for experts.
+ */
+#define SNN_ADAPTERS_RANK_MAX 128
+typedef struct snn_conv_adapters snn_conv_adapters_t; /* opaque; owned by the library */
+SNN_API snn_status_t snn_conv_adapters_create(snn_conv_t* layer, snn_conv_adapters_t** out);
+SNN_API snn_status_t snn_conv_adapters_forward(snn_conv_adapters_t* h, const void* act_dev, int32_t act_type,
+                                               int32_t rows, int64_t ld_act, const int32_t* adapter_dev,
+                                               const void* a_dev, const void* b_dev, const float* scale_dev,
+                                               int32_t adapters, int32_t rank, float* work_dev, void* out_dev,
+                                               int32_t out_type, int64_t ld_out, void* cuda_stream);
+SNN_API snn_status_t snn_conv_adapters_destroy(snn_conv_adapters_t* h);
+
 #ifdef __cplusplus
 }
 #endif

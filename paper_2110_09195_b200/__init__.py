@@ -5,3 +5,6 @@ from .binding import (  # noqa: F401
     ACT_BIN, ACT_F16, OUT_F32, OUT_I32, OUT_BITS, PATH_AUTO, PATH_REUSE, PATH_DECODED, PATH_DECODED_TC, PATH_NAMES,
     SnnConv, SnnConvGroup, SnnConvStack, SnnError, forward_static, kernel_launches, library_path, load_library, microbench, version,
 )
+from .projections import (  # noqa: F401
+    ACT_BF16, OUT_BF16, OUT_F16, Route, SnnConvAdapters, SnnConvExperts, alloc_route, combine, route,
+)

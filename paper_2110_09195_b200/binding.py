@@ -33,6 +33,9 @@ EXPORTED_SYMBOLS = (
     "snn_microbench", "snn_conv_forward_static",
     "snn_conv_group_create", "snn_conv_group_forward", "snn_conv_group_destroy",
     "snn_conv_stack_create", "snn_conv_stack_forward", "snn_conv_stack_destroy",
+    "snn_conv_experts_create", "snn_conv_experts_forward", "snn_conv_experts_destroy",
+    "snn_conv_experts_route", "snn_conv_experts_route_work", "snn_conv_experts_combine",
+    "snn_conv_adapters_create", "snn_conv_adapters_forward", "snn_conv_adapters_destroy",
 )
 
 
@@ -103,6 +106,25 @@ def load_library():
     lib.snn_conv_stack_forward.argtypes = [vp, vp, vp, i32, vp]
     lib.snn_conv_stack_destroy.restype = i32
     lib.snn_conv_stack_destroy.argtypes = [vp]
+    i64 = ctypes.c_int64
+    lib.snn_conv_experts_create.restype = i32
+    lib.snn_conv_experts_create.argtypes = [ctypes.POINTER(vp), i32, ctypes.POINTER(vp)]
+    lib.snn_conv_experts_forward.restype = i32
+    lib.snn_conv_experts_forward.argtypes = [vp, vp, i32, i32, i64, vp, vp, i32, vp, i32, i64, vp]
+    lib.snn_conv_experts_destroy.restype = i32
+    lib.snn_conv_experts_destroy.argtypes = [vp]
+    lib.snn_conv_experts_route_work.restype = i64
+    lib.snn_conv_experts_route_work.argtypes = [i32, i32]
+    lib.snn_conv_experts_route.restype = i32
+    lib.snn_conv_experts_route.argtypes = [vp, i32, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp]
+    lib.snn_conv_experts_combine.restype = i32
+    lib.snn_conv_experts_combine.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, i32, vp, i32, i64, i32, vp]
+    lib.snn_conv_adapters_create.restype = i32
+    lib.snn_conv_adapters_create.argtypes = [vp, ctypes.POINTER(vp)]
+    lib.snn_conv_adapters_forward.restype = i32
+    lib.snn_conv_adapters_forward.argtypes = [vp, vp, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp, i32, i64, vp]
+    lib.snn_conv_adapters_destroy.restype = i32
+    lib.snn_conv_adapters_destroy.argtypes = [vp]
     lib.snn_microbench.restype = i32
     lib.snn_microbench.argtypes = [i32, i32, ctypes.POINTER(ctypes.c_double)]
     _lib = lib

@@ -13,6 +13,7 @@
 #include <tuple>
 #include <utility>
 
+#include "snn_handle.h"
 #include "snn_internal.h"
 
 using namespace snn;
@@ -35,40 +36,6 @@ snn_status_t cuda_fail(cudaError_t e, const char* what) {
   snn_status_t st = (e == cudaErrorMemoryAllocation) ? SNN_ERR_OOM : SNN_ERR_CUDA;
   return fail(st, "%s: %s", what, cudaGetErrorString(e));
 }
-
-struct DeviceGuard {
-  int prev = -1;
-  bool ok = false;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) return;
-    ok = (prev == dev) || cudaSetDevice(dev) == cudaSuccess;
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-  }
-};
-
-}  // namespace
-
-struct snn_conv {
-  int C, K, tau, stride, pad, act_type, device;
-  int ksize = 3;
-  LayerDev L;
-  std::mutex mu;
-  std::map<std::tuple<int, int, int>, int> tuned;        // (N,H,W) -> path measured fastest by snn_conv_tune
-  // (N,H,W, packed-sign output?) -> tensor-core plan and weight operand (a group of one)
-  std::map<std::tuple<int, int, int, int>, GroupDev*> solo;
-  // staging for snn_conv_forward_host
-  void* stage_in = nullptr;
-  void* stage_out = nullptr;
-  size_t stage_in_bytes = 0, stage_out_bytes = 0;
-  cudaStream_t host_stream = nullptr;
-  int* tc_status_host = nullptr;  // pinned, written by the tensor-core kernel on a bounded-wait timeout
-  int* tc_status_dev = nullptr;   // the same word as the device sees it
-};
-
-namespace {
 
 bool make_geom(const snn_conv* h, int N, int H, int W, Geom* g) {
   if (N < 0 || H < 1 || W < 1) return false;

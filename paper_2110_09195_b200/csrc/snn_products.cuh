@@ -1,0 +1,68 @@
+// Device helpers of the projections' kernels: 16-bit types, the warp's matrix instruction, +1 / -1 from bits.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+#include "snn_internal.h"
+
+namespace snn {
+namespace {
+
+// What differs between the two types of activations: +1.0 twice in a register, and conversions.
+struct F16 {
+  static constexpr uint32_t kOne = 0x3c003c00u;
+  static __device__ __forceinline__ float2 unpack(uint32_t v) {
+    __half2 h;
+    memcpy(&h, &v, 4);
+    return __half22float2(h);
+  }
+};
+struct BF16 {
+  static constexpr uint32_t kOne = 0x3f803f80u;
+  static __device__ __forceinline__ float2 unpack(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+};
+
+// D[16 x 8] += A[16 x 16] B[16 x 8], fp32 sums; g = lane / 4, t = lane % 4:
+// a = rows g, g + 8, g, g + 8 at k = 2t, 2t, 2t + 8, 2t + 8; b = column g at k = 2t, 2t + 8; d = rows g, g, g + 8, g + 8 at columns 2t, 2t + 1.
+// (The order of k is free as long as both operands have the same.)
+template <class T>
+__device__ __forceinline__ void mma_16x8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma_16x8<F16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma_16x8<BF16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The two weights whose bits lie at 15 - shift and 31 - shift, as 16-bit +1 / -1.
+template <class T>
+__device__ __forceinline__ uint32_t plus_minus(uint32_t w, int shift) {
+  return ((w << shift) & 0x80008000u) ^ T::kOne;
+}
+
+// 16 bytes that another kernel may have written while this one was being set up: no read-only path.
+__device__ __forceinline__ uint4 ld16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+// One value in an output type, rounded to nearest even.
+__device__ __forceinline__ void store_out(void* out, int type, long long i, float v) {
+  if (type == SNN_OUT_F32) static_cast<float*>(out)[i] = v;
+  else if (type == SNN_OUT_F16) static_cast<__half*>(out)[i] = __float2half_rn(v);
+  else static_cast<__nv_bfloat16*>(out)[i] = __float2bfloat16_rn(v);
+}
+
+__device__ __forceinline__ int clamp_offset(int v, int most) { return min(max(v, 0), most); }
+
+}  // namespace
+}  // namespace snn

@@ -1,0 +1,257 @@
+// Routing of tokens to experts: the choice, the order of the rows by expert, and the weighted sum that undoes it.
+#include <math_constants.h>
+
+#include "snn_products.h"
+
+#include "snn_products.cuh"
+
+namespace snn {
+namespace {
+
+constexpr int RT_BLOCK = 64;   // tokens of a CTA: two words of a mask for each expert
+constexpr int RT_WARPS = 16;
+
+struct RouteParams {
+  const void* logits;
+  long long ld;
+  int type, T, E, k, normalise;
+  int32_t* ids;
+  float* weights;
+  int32_t *offsets, *rows, *slots, *work;
+};
+
+__device__ __forceinline__ float logit(const RouteParams& p, int t, int e) {
+  const long long i = t * p.ld + e;
+  if (p.type == SNN_OUT_F32) return static_cast<const float*>(p.logits)[i];
+  if (p.type == SNN_OUT_F16) return __half2float(static_cast<const __half*>(p.logits)[i]);
+  return __bfloat162float(static_cast<const __nv_bfloat16*>(p.logits)[i]);
+}
+
+// A float as an unsigned number of the same order, above 0; -infinity and NaN, which are not chosen, as 0.
+__device__ __forceinline__ uint32_t ordered(float v) {
+  if (!(v > -CUDART_INF_F)) return 0u;
+  const uint32_t u = __float_as_uint(v + 0.f);   // (-0 is +0: equal logits have to be equal)
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+
+// exp(v - most), 1 where both are the same infinity
+__device__ __forceinline__ float above(uint32_t u, uint32_t most) { return u == most ? 1.f : expf(unordered(u) - unordered(most)); }
+
+// One token by one warp, E <= 32 V: lane l holds experts l, l + 32, ...  The k-th largest is taken k times: the warp's largest, then the
+// lowest expert that has it.  Lane j keeps choice j.
+template <int V>
+__device__ __forceinline__ void choose(const RouteParams& p, int t, uint32_t* mask, int local) {
+  const int lane = threadIdx.x & 31;
+  uint32_t u[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) u[i] = lane + 32 * i < p.E ? ordered(logit(p, t, lane + 32 * i)) : 0u;
+  uint32_t best = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) best = max(best, u[i]);
+  const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+  float all = 0.f;
+  if (!p.normalise) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) all += u[i] ? above(u[i], top) : 0.f;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+  }
+  int id = -1;
+  float w = 0.f;
+  for (int j = 0; j < p.k; ++j) {
+    best = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) best = max(best, u[i]);
+    const uint32_t most = __reduce_max_sync(0xffffffffu, best);
+    if (!most) break;
+    uint32_t e = 0xffffffffu;
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i)
+      if (u[i] == most) e = lane + 32 * i;
+    e = __reduce_min_sync(0xffffffffu, e);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (e == lane + 32 * i) u[i] = 0;
+    if (lane == j) {
+      id = (int)e;
+      w = above(most, top);
+    }
+  }
+  if (p.normalise) {
+    all = w;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+  }
+  if (lane < p.k) {
+    p.ids[(size_t)t * p.k + lane] = id;
+    p.weights[(size_t)t * p.k + lane] = id < 0 ? 0.f : w / all;
+    if (id >= 0) atomicOr(mask + 2 * id + (local >> 5), 1u << (local & 31));   // (bits: any order gives the same word)
+  }
+}
+
+// Exclusive sums of count[0..E) in place, by the whole CTA; returns the total.
+__device__ int scan_counts(int* count, int E, int* part) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = RT_WARPS * 32;
+  int base = 0;
+  for (int e0 = 0; e0 < E; e0 += n) {
+    const int e = e0 + (int)threadIdx.x, v = e < E ? count[e] : 0;
+    int upto = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += o;
+    }
+    if (lane == 31) part[warp] = upto;
+    __syncthreads();
+    int before = base, all = base;
+    for (int w = 0; w < RT_WARPS; ++w) {
+      if (w < warp) before += part[w];
+      all += part[w];
+    }
+    if (e < E) count[e] = before + upto - v;
+    base = all;
+    __syncthreads();
+  }
+  return base;
+}
+
+// Rows and slots of the CTA's tokens: start[e] is the first row of the CTA's choices of expert e, the mask says which of its tokens
+// come before.
+__device__ void place(const RouteParams& p, const uint32_t* mask, const int* start, int t0, int tokens) {
+  for (int i = threadIdx.x; i < tokens * p.k; i += RT_WARPS * 32) {
+    const int local = i / p.k, id = p.ids[(size_t)t0 * p.k + i];
+    int slot = -1;
+    if (id >= 0) {
+      const uint32_t lo = mask[2 * id], hi = mask[2 * id + 1];
+      slot = start[id] + (local < 32 ? __popc(lo & ((1u << local) - 1u)) : __popc(lo) + __popc(hi & ((1u << (local - 32)) - 1u)));
+      p.rows[slot] = t0 + local;
+    }
+    p.slots[(size_t)t0 * p.k + i] = slot;
+  }
+}
+
+// First launch: each CTA's tokens choose, and the CTA counts its choices of each expert.  With one CTA that is all there is to count, and it
+// goes on to place them.
+template <int V>
+__global__ void __launch_bounds__(RT_WARPS * 32) route_choose_kernel(const RouteParams p) {
+  __shared__ uint32_t mask[2 * 32 * V];
+  __shared__ int count[32 * V], part[RT_WARPS];
+  const int t0 = (int)blockIdx.x * RT_BLOCK, tokens = min(RT_BLOCK, p.T - t0), warp = threadIdx.x >> 5;
+  for (int i = threadIdx.x; i < 2 * p.E; i += RT_WARPS * 32) mask[i] = 0;
+  __syncthreads();
+  for (int i = warp; i < tokens; i += RT_WARPS) choose<V>(p, t0 + i, mask, i);
+  __syncthreads();
+  const bool alone = gridDim.x == 1;
+  for (int e = threadIdx.x; e < p.E; e += RT_WARPS * 32) {
+    const int n = __popc(mask[2 * e]) + __popc(mask[2 * e + 1]);
+    if (alone) count[e] = n;
+    else p.work[(size_t)blockIdx.x * p.E + e] = n;
+  }
+  if (!alone) return;
+  __syncthreads();
+  const int total = scan_counts(count, p.E, part);
+  for (int e = threadIdx.x; e < p.E; e += RT_WARPS * 32) p.offsets[e] = count[e];
+  if (threadIdx.x == 0) p.offsets[p.E] = total;
+  place(p, mask, count, t0, tokens);
+  for (int i = total + (int)threadIdx.x; i < p.T * p.k; i += RT_WARPS * 32) p.rows[i] = -1;
+}
+
+// Second launch: each CTA adds up all CTAs' counts, for the experts' first rows, and those of the CTAs before it, for its own.
+__global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteParams p) {
+  extern __shared__ int sm[];
+  int* const all = sm;                                                 // [E]
+  int* const before = sm + p.E;                                        // [E]
+  uint32_t* const mask = reinterpret_cast<uint32_t*>(sm + 2 * p.E);    // [E][2]
+  __shared__ int part[RT_WARPS];
+  const int t0 = (int)blockIdx.x * RT_BLOCK, tokens = min(RT_BLOCK, p.T - t0), n = RT_WARPS * 32;
+  for (int i = threadIdx.x; i < 4 * p.E; i += n) sm[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < tokens * p.k; i += n) {
+    const int id = p.ids[(size_t)t0 * p.k + i], local = i / p.k;
+    if (id >= 0) atomicOr(mask + 2 * id + (local >> 5), 1u << (local & 31));
+  }
+  // (sums of whole numbers: any order gives the same)
+  for (int i = threadIdx.x; i < (int)gridDim.x * p.E; i += n) {
+    const int b = i / p.E, e = i - b * p.E, v = p.work[i];
+    if (v) {
+      atomicAdd(all + e, v);
+      if (b < (int)blockIdx.x) atomicAdd(before + e, v);
+    }
+  }
+  __syncthreads();
+  const int total = scan_counts(all, p.E, part);
+  for (int e = threadIdx.x; e < p.E; e += n) {
+    if (blockIdx.x == 0) p.offsets[e] = all[e];
+    all[e] += before[e];
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[p.E] = total;
+  __syncthreads();
+  place(p, mask, all, t0, tokens);
+  for (int i = total + (int)blockIdx.x * n + (int)threadIdx.x; i < p.T * p.k; i += (int)gridDim.x * n) p.rows[i] = -1;
+}
+
+// ---------------------------------------------------------------- combine
+
+struct CombineParams {
+  const void* y;
+  const int32_t* slots;
+  const float* weights;
+  void* out;
+  long long ld_y, ld_out;
+  int y_type, y_rows, T, k, C, out_type;
+};
+
+__device__ __forceinline__ float value(const void* y, int type, long long i) {
+  if (type == SNN_OUT_F32) return static_cast<const float*>(y)[i];
+  if (type == SNN_OUT_F16) return __half2float(static_cast<const __half*>(y)[i]);
+  return __bfloat162float(static_cast<const __nv_bfloat16*>(y)[i]);
+}
+
+// A thread sums a token's column; neighbouring threads, neighbouring columns.
+__global__ void __launch_bounds__(256) combine_kernel(const CombineParams p) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long t = i / p.C;
+  const int c = (int)(i - t * p.C);
+  if (t >= p.T) return;
+  float s = 0.f;
+  for (int j = 0; j < p.k; ++j) {
+    const int slot = p.slots[t * p.k + j];
+    if (slot >= 0 && slot < p.y_rows) s = fmaf(p.weights[t * p.k + j], value(p.y, p.y_type, slot * p.ld_y + c), s);
+  }
+  store_out(p.out, p.out_type, t * p.ld_out + c, s);
+}
+
+}  // namespace
+
+long long route_work_bytes(int T, int E) { return T <= RT_BLOCK ? 0 : (long long)((T + RT_BLOCK - 1) / RT_BLOCK) * E * 4; }
+
+cudaError_t route_forward(const RouteCall& c, int* launched) {
+  const RouteParams p{c.logits, c.ld, c.type, c.T, c.E, c.k, c.normalise, c.ids, c.weights, c.offsets, c.rows, c.slots, c.work};
+  // (no tokens: one CTA writes the offsets)
+  const unsigned blocks = (unsigned)max(1, (c.T + RT_BLOCK - 1) / RT_BLOCK);
+  const int v = (c.E + 31) / 32;
+#define SNN_CHOOSE(V) route_choose_kernel<V><<<blocks, RT_WARPS * 32, 0, c.stream>>>(p)
+  if (v <= 1) SNN_CHOOSE(1);
+  else if (v <= 2) SNN_CHOOSE(2);
+  else if (v <= 4) SNN_CHOOSE(4);
+  else if (v <= 8) SNN_CHOOSE(8);
+  else if (v <= 16) SNN_CHOOSE(16);
+  else SNN_CHOOSE(32);
+#undef SNN_CHOOSE
+  *launched += 1;
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || blocks == 1) return e;
+  route_place_kernel<<<blocks, RT_WARPS * 32, (size_t)c.E * 16, c.stream>>>(p);
+  *launched += 1;
+  return cudaGetLastError();
+}
+
+cudaError_t combine_forward(const CombineCall& c, int* launched) {
+  const CombineParams p{c.y, c.slots, c.weights, c.out, c.ld_y, c.ld_out, c.y_type, c.y_rows, c.T, c.k, c.C, c.out_type};
+  combine_kernel<<<(unsigned)(((long long)c.T * c.C + 255) / 256), 256, 0, c.stream>>>(p);
+  *launched += 1;
+  return cudaGetLastError();
+}
+
+}  // namespace snn
