@@ -12,7 +12,7 @@ namespace {
 __global__ void products_layout_kernel(const uint32_t* __restrict__ planes, uint32_t* __restrict__ bits, int C, int K, int n_mt, int n_kb) {
   const long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= (long long)n_mt * n_kb * 128) return;
-  const int j = (int)(i & 3), lane = (int)(i >> 2) & 31, g = lane >> 2, t = lane & 3;
+  const int j = 2 * (int)(i & 1) + ((int)(i >> 3) & 1), t = (int)(i >> 1) & 3, g = (int)(i >> 4) & 7;
   const long long tile = i >> 7;
   const int kb = (int)(tile % n_kb), mt = (int)(tile / n_kb);
   const int c0 = kb * 256 + j * 64 + t * 16;
@@ -87,29 +87,6 @@ __device__ __forceinline__ bool find_chunk(const int32_t* offsets, int E, int R,
   return true;
 }
 
-// B (A x) of one output: rank products in fp32.
-template <class T>
-__device__ __forceinline__ float lowrank_term(const Lowrank& low, int K, int row, int co) {
-  const int a = low.adapter[row];
-  if (a < 0 || a >= low.n) return 0.f;
-  const uint16_t* b = static_cast<const uint16_t*>(low.b) + ((size_t)a * K + co) * low.rank;
-  const float* h = low.h + (size_t)row * low.rank;
-  float s = 0.f;
-  for (int j = 0; j < low.rank; j += 8) {
-    const uint4 v = ld16(b + j);
-    const float4 h0 = *reinterpret_cast<const float4*>(h + j), h1 = *reinterpret_cast<const float4*>(h + j + 4);
-    float2 f = T::unpack(v.x);
-    s = fmaf(f.x, h0.x, fmaf(f.y, h0.y, s));
-    f = T::unpack(v.y);
-    s = fmaf(f.x, h0.z, fmaf(f.y, h0.w, s));
-    f = T::unpack(v.z);
-    s = fmaf(f.x, h1.x, fmaf(f.y, h1.y, s));
-    f = T::unpack(v.w);
-    s = fmaf(f.x, h1.z, fmaf(f.y, h1.w, s));
-  }
-  return s;
-}
-
 // A warp computes 32 output channels times 8 NT rows over a share of the input channels: the weights, the M operand, are expanded from
 // bits in registers, the rows, the N operand, come straight from memory as the instruction wants them (a lane's 16 neighbouring
 // channels are four steps' operands).  The warps of a CTA take different input channels (k_warps of them) and different output
@@ -135,11 +112,12 @@ __global__ void __launch_bounds__(256) products_small_kernel(const SmallParams p
   const int mt = 2 * ((int)blockIdx.y * m_warps + mw);
   float acc[2][NT][4] = {};
   if (mt < p.n_mt) {
-    const uint4* w0 = reinterpret_cast<const uint4*>(p.bits) + ((size_t)(e * p.n_mt + mt) * p.n_kb) * 32 + lane;
-    const uint4* w1 = w0 + (size_t)p.n_kb * 32;
+    const uint2* w0 = reinterpret_cast<const uint2*>(p.bits) + ((size_t)(e * p.n_mt + mt) * p.n_kb) * 64 + 8 * g + t;
+    const uint2* w1 = w0 + (size_t)p.n_kb * 64;
     for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
-      const uint4 u0 = ld16(w0 + (size_t)kb * 32), u1 = ld16(w1 + (size_t)kb * 32);
-      const uint32_t ua[4] = {u0.x, u0.y, u0.z, u0.w}, ub[4] = {u1.x, u1.y, u1.z, u1.w};
+      const uint2 ue = ld8(w0 + (size_t)kb * 64), uo = ld8(w0 + (size_t)kb * 64 + 4);
+      const uint2 ve = ld8(w1 + (size_t)kb * 64), vo = ld8(w1 + (size_t)kb * 64 + 4);
+      const uint32_t ua[4] = {ue.x, uo.x, ue.y, uo.y}, ub[4] = {ve.x, vo.x, ve.y, vo.y};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = kb * 256 + j * 64 + t * 16;
@@ -216,7 +194,7 @@ cudaError_t products_create(const LayerDev* const* layers, int E, int C, int K, 
   p->E = E;
   p->C = C;
   p->K = K;
-  p->n_mt = (K + 127) / 128 * 8;
+  p->n_mt = (K + 255) / 256 * 16;
   p->n_kb = (C + 255) / 256;
   const size_t words = (size_t)p->n_mt * p->n_kb * 128, rows = (size_t)p->n_mt * 16;
   cudaError_t e = cudaMalloc((void**)&p->bits, words * 4 * E);
@@ -244,6 +222,8 @@ void products_destroy(Products* p) {
 }
 
 cudaError_t products_forward(const Products& p, const ProductCall& c, int* launched) {
+  const int per_expert = c.offsets ? c.max_rows / max(1, min(p.E, c.max_rows)) : c.max_rows;
+  if (per_expert >= 48 && c.act_rows > 0) return products_tall(p, c, launched);
   return c.act_type == SNN_ACT_F16 ? small_forward<F16>(p, c, launched) : small_forward<BF16>(p, c, launched);
 }
 

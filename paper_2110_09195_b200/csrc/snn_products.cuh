@@ -5,7 +5,7 @@
 
 #include <cstdint>
 
-#include "snn_internal.h"
+#include "snn_products.h"
 
 namespace snn {
 namespace {
@@ -55,11 +55,40 @@ __device__ __forceinline__ uint4 ld16(const void* p) {
   return v;
 }
 
+__device__ __forceinline__ uint2 ld8(const void* p) {
+  uint2 v;
+  asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+
 // One value in an output type, rounded to nearest even.
 __device__ __forceinline__ void store_out(void* out, int type, long long i, float v) {
   if (type == SNN_OUT_F32) static_cast<float*>(out)[i] = v;
   else if (type == SNN_OUT_F16) static_cast<__half*>(out)[i] = __float2half_rn(v);
   else static_cast<__nv_bfloat16*>(out)[i] = __float2bfloat16_rn(v);
+}
+
+// B (A x) of one output: rank products in fp32.
+template <class T>
+__device__ __forceinline__ float lowrank_term(const Lowrank& low, int K, int row, int co) {
+  const int a = low.adapter[row];
+  if (a < 0 || a >= low.n) return 0.f;
+  const uint16_t* b = static_cast<const uint16_t*>(low.b) + ((size_t)a * K + co) * low.rank;
+  const float* h = low.h + (size_t)row * low.rank;
+  float s = 0.f;
+  for (int j = 0; j < low.rank; j += 8) {
+    const uint4 v = ld16(b + j);
+    const float4 h0 = *reinterpret_cast<const float4*>(h + j), h1 = *reinterpret_cast<const float4*>(h + j + 4);
+    float2 f = T::unpack(v.x);
+    s = fmaf(f.x, h0.x, fmaf(f.y, h0.y, s));
+    f = T::unpack(v.y);
+    s = fmaf(f.x, h0.z, fmaf(f.y, h0.w, s));
+    f = T::unpack(v.z);
+    s = fmaf(f.x, h1.x, fmaf(f.y, h1.y, s));
+    f = T::unpack(v.w);
+    s = fmaf(f.x, h1.z, fmaf(f.y, h1.w, s));
+  }
+  return s;
 }
 
 __device__ __forceinline__ int clamp_offset(int v, int most) { return min(max(v, 0), most); }

@@ -9,14 +9,16 @@
 namespace snn {
 
 // Weights of E projections [K x C], one bit each (set: -1), for both product kernels:
-//   bits [E][n_mt][n_kb][32 lanes][4 words]:  a tile of 16 output channels times 256 input channels is 512 bytes.
-//   Lane 4g + t, word j: rows g and g + 8 of the tile, input channels 256 kb + 64 j + 16 t .. + 15, as 16 pairs of
+//   bits [E][n_mt][n_kb][8 g][2 o][4 t][2 i]:  a tile of 16 output channels times 256 input channels is 512 bytes.
+//   Word (g, o, t, i): rows g and g + 8 of the tile, input channels 256 kb + 64 (2 i + o) + 16 t .. + 15, as 16 pairs of
 //   neighbouring channels, pair p of row g in bits p (the even one) and 16 + p, of row g + 8 in bits 8 + p and 24 + p.
+// (A lane 4g + t of the small kernel's warps reads two times 8 bytes, a thread of the tall kernel's two warpgroups, which take odd and
+// even blocks of 64, twice 16.)
 // A shift and a masked exclusive-or turn a pair into two 16-bit +1 / -1 in one register.  Rows and channels that do not
 // exist have bit 0; the former's sums are not stored, the latter meet zeros.
 struct Products {
   int device = 0, E = 0, C = 0, K = 0;
-  int n_mt = 0;   // tiles of 16 output channels, a multiple of 8
+  int n_mt = 0;   // tiles of 16 output channels, a multiple of 16
   int n_kb = 0;   // blocks of 256 input channels
   uint32_t* bits = nullptr;
   float* alpha = nullptr;       // [E][16 n_mt], zeros behind K
@@ -47,6 +49,7 @@ struct ProductCall {
   cudaStream_t stream;
 };
 cudaError_t products_forward(const Products& p, const ProductCall& c, int* launched);
+cudaError_t products_tall(const Products& p, const ProductCall& c, int* launched);   // (snn_products_tall.cu: many rows)
 
 // h[r][0..rank) = scale[a] * (A[a] x[r]) for the rows with an adapter; the others' are not written.
 struct ShrinkCall {

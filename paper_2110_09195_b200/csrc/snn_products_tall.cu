@@ -1,0 +1,597 @@
+// Projections of language models, many rows: the 5th-generation tensor cores, the weights expanded from bits into tensor memory.
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "snn_products.h"
+
+#include "snn_products.cuh"
+#include "snn_tc_common.cuh"
+
+namespace snn {
+namespace {
+
+// out[row, co] = alpha * sum_k W[co, k] x[row, k] as D[256 channels x up to 192 rows] = W (M operand) * x^T (N operand), by a pair of
+// CTAs (a cluster of two, one instruction for both): each has 128 of the channels and half of the rows.
+//
+// The weights come as bits (snn_products.h): in each CTA two warpgroups in turn expand 128 channels x 64 input channels at a time into
+// 16-bit +1 / -1, two instructions for two weights, and store them to tensor memory, from where the instruction takes its M operand.
+// Shared memory then holds and feeds the rows alone, and no 16-bit weight is ever read from memory.  A single CTA with all the rows
+// waited for them 40 % of the time: 64 bytes a cycle and SM at the instructions' full rate, from L2 and through shared memory; a pair needs
+// half.  TMA brings the rows; rows named by an index come by 16-byte asynchronous copies of three warps (TMA's gather of four rows an
+// instruction took 2900 cycles for 192 rows of 128 bytes, seven times the instructions that they feed).
+// 512 columns: four stages of weights (32 columns each) and two accumulators of 192, so that one is written out while the next is
+// being summed.
+constexpr int TL_N = 192;             // rows of a tile, at most
+constexpr int TL_A_STAGES = 4;
+constexpr int TL_A_COLS = 32;         // 64 input channels, two to a column
+constexpr int TL_D0 = TL_A_STAGES * TL_A_COLS;
+constexpr int TL_HALF = TL_N / 2;      // rows of a CTA
+constexpr int TL_B_BYTES = TL_HALF * 128;
+constexpr int TL_BOX = 32;            // rows of one TMA box
+constexpr int TL_THREADS = 512;       // warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs
+constexpr int TL_PENDING = 8;         // stages of copied rows on their way
+// Stages of rows, and 32-bit values of A x for each row kept beside them (RANK: 0 without adapters, else a bound of their rank).
+template <int RANK>
+struct TallShape {
+  static constexpr int kStages = RANK == 128 ? 8 : RANK == 64 ? 12 : RANK == 32 ? 14 : RANK == 16 ? 15 : 16;
+  static constexpr int kH = RANK * TL_N * 4;
+};
+
+// The same value in all lanes, known to be so
+__device__ __forceinline__ int uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+struct TallParams {
+  const uint32_t* bits;
+  const float* alpha;
+  const uint16_t* act;
+  const int32_t *rows, *offsets;
+  void* out;
+  long long ld_act, ld_out;
+  int act_rows, max_rows, E, C, K, n_mt, n_kb, out_type, n_cp;
+  int* status;
+  Lowrank low;
+};
+
+struct TallBars {
+  uint64_t b_full[16], b_empty[16], a_full[TL_A_STAGES], a_empty[TL_A_STAGES], d_full[2], d_empty[2], drain;
+  uint32_t tmem;
+  int who[TL_N];   // adapters of the tile's rows, below 0: none
+};
+
+// Issued by the lanes for which `on` is not 0: D[256 x N] (+)= A[256 x 64] * B[N x 64]^T in four steps of 16, A in tensor memory, then the
+// commits to both CTAs' barriers.  One statement, under a predicate: four statements with a branch on the lane around them took 700 cycles a
+// stage, with a predicate each 400, this one 70.
+__device__ __forceinline__ void stage_ts_f16(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate, uint32_t bar0, uint32_t bar1, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 d1, d2, d3;\n\t.reg .b32 a1, a2, a3;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+      "add.u64 d1, %2, 2;\n\tadd.u64 d2, %2, 4;\n\tadd.u64 d3, %2, 6;\n\t"
+      "add.u32 a1, %1, 8;\n\tadd.u32 a2, %1, 16;\n\tadd.u32 a3, %1, 24;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [a1], d1, %3, 1;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [a2], d2, %3, 1;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [a3], d3, %3, 1;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], %8;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%6], %8;\n\t}" ::"r"(d),
+      "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(bar0), "r"(bar1), "r"(on), "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void commit_on(uint32_t bar, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}" ::"r"(bar),
+      "r"(on), "h"((uint16_t)3)
+      : "memory");
+}
+// 32 columns of the warp's 32 lanes; they are there after tmem_st_wait
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]),
+      "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]),
+      "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 8 columns; load and wait are one statement
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+      : "r"(taddr)
+      : "memory");
+}
+// (the barrier: the pair's first CTA's)
+__device__ __forceinline__ void tma_rows(uint32_t dst, const void* map, int c, int row, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(c),
+               "r"(row), "r"(bar)
+               : "memory");
+}
+// 16 bytes, or zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+// two products and sums at once
+__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b)); }
+__device__ __forceinline__ uint64_t pack2(float2 v) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+  return r;
+}
+__device__ __forceinline__ float sum2(uint64_t v) {
+  float a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+  return a + b;
+}
+
+// The address of the pair's first CTA's copy of a variable in shared memory, and an arrival there.  What the arrival stands for is in tensor
+// memory or in the SM's own shared memory, after wait::st, wait::ld or a proxy fence, and is read by the MMA unit: no wider release is needed
+// (one of cluster scope, with waits that acquire at that scope, made every stage take 900 cycles, whatever its size).
+__device__ __forceinline__ uint32_t at_first(uint32_t addr) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+__device__ __forceinline__ void arrive_at_first(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(at_first(bar)) : "memory");
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
+// Barrier ID among THREADS of the CTA's threads, whole warps; whether all of them say so.
+template <int ID, int THREADS>
+__device__ __forceinline__ bool bar_all(bool v) {
+  uint32_t r;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.and.pred p, %2, %3, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)v), "n"(ID), "n"(THREADS)
+      : "memory");
+  return r != 0;
+}
+
+// The experts' ranges in shared memory: end[e] counts the row tiles up to and with expert e.
+struct Ranges {
+  int *lo, *n, *end;
+};
+struct Tile {
+  int e, r0, n, ct;   // expert, first row, rows, the CTA's channel tile
+};
+// Tile `index` of the launch, channels of the same rows one after the other; `t.e` is where the search begins (indices rise).
+__device__ __forceinline__ bool tall_tile(const Ranges& R, int E, int n_cp, int index, int rank, Tile& t) {
+  const int q = index / n_cp;
+  int e = t.e;
+  while (e < E && q >= R.end[e]) ++e;
+  t.e = uni(e);
+  if (t.e >= E) return false;
+  const int n = R.n[t.e], tiles = (n + TL_N - 1) / TL_N, per = ((n + tiles - 1) / tiles + 31) & ~31;   // about the same rows in each
+  const int k = q - (t.e ? R.end[t.e - 1] : 0);
+  t.ct = 2 * (index - q * n_cp) + rank;
+  t.r0 = uni(R.lo[t.e] + k * per);
+  t.n = uni(min(per, n - k * per));
+  return true;
+}
+
+// A channel's outputs of up to 32 rows.
+__device__ __forceinline__ void to_out(float* p, float v) { *p = v; }
+__device__ __forceinline__ void to_out(__half* p, float v) { *p = __float2half_rn(v); }
+__device__ __forceinline__ void to_out(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+template <class O>
+__device__ __forceinline__ void store_column(O* out, long long ld, int n, float alpha, const uint32_t (&v)[32]) {
+#pragma unroll
+  for (int c = 0; c < 32; ++c, out += ld)
+    if (c < n) to_out(out, alpha * __uint_as_float(v[c]));
+}
+
+// A channel's row of B in registers: pairs of fp32 values, or (the longest) as it is stored.
+template <class T, int RANK>
+struct BRow {
+  uint64_t v[RANK ? RANK / 2 : 1];
+  __device__ __forceinline__ void set(int j, uint4 u) {
+    v[4 * j] = pack2(T::unpack(u.x));
+    v[4 * j + 1] = pack2(T::unpack(u.y));
+    v[4 * j + 2] = pack2(T::unpack(u.z));
+    v[4 * j + 3] = pack2(T::unpack(u.w));
+  }
+  __device__ __forceinline__ void get(int j, uint64_t (&w)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = v[4 * j + i];
+  }
+};
+template <class T>
+struct BRow<T, 128> {
+  uint4 v[16];
+  __device__ __forceinline__ void set(int j, uint4 u) { v[j] = u; }
+  __device__ __forceinline__ void get(int j, uint64_t (&w)[4]) const {
+    w[0] = pack2(T::unpack(v[j].x));
+    w[1] = pack2(T::unpack(v[j].y));
+    w[2] = pack2(T::unpack(v[j].z));
+    w[3] = pack2(T::unpack(v[j].w));
+  }
+};
+
+// RANK: 0 without adapters, else a bound of their rank.
+template <class T, bool GATHER, int RANK>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TL_THREADS, 1) products_tall_kernel(const TallParams p, const __grid_constant__ CUtensorMap map) {
+  constexpr int STAGES = TallShape<RANK>::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  TallBars* const bars = reinterpret_cast<TallBars*>(smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH);
+  Ranges R;
+  R.lo = reinterpret_cast<int*>(bars + 1);
+  R.n = R.lo + p.E;
+  R.end = R.n + p.E;
+  const int warp = uni(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const uint32_t b_smem = smem_u32(smem);
+  const int rank = (int)(blockIdx.x & 1), first_tile = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
+  if (warp == 0) {
+    // tiles of each expert, summed up: every lane a run of experts
+    const int per = (p.E + 31) >> 5, e0 = lane * per, e1 = min(p.E, e0 + per);
+    int count = 0;
+    for (int e = e0; e < e1; ++e) {
+      const int lo = p.offsets ? clamp_offset(p.offsets[e], p.max_rows) : 0;
+      const int n = p.offsets ? max(clamp_offset(p.offsets[e + 1], p.max_rows) - lo, 0) : p.max_rows;
+      R.lo[e] = lo;
+      R.n[e] = n;
+      count += (n + TL_N - 1) / TL_N;
+    }
+    int upto = count;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += v;
+    }
+    int end = upto - count;
+    for (int e = e0; e < e1; ++e) R.end[e] = end += (R.n[e] + TL_N - 1) / TL_N;
+  } else if (warp == 1 && lane == 0) {
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(smem_u32(&bars->b_full[i]), GATHER ? 6 : 1);
+      mbar_init(smem_u32(&bars->b_empty[i]), 1);
+    }
+    for (int i = 0; i < TL_A_STAGES; ++i) {
+      mbar_init(smem_u32(&bars->a_full[i]), 8);
+      mbar_init(smem_u32(&bars->a_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bars->d_full[i]), 1);
+      mbar_init(smem_u32(&bars->d_empty[i]), 8);
+    }
+    mbar_init(smem_u32(&bars->drain), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  } else if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars->tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  pair_sync();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem;
+  const int nk = (p.C + 63) >> 6;
+  bool ok = true;
+  Tile t{};
+
+  if (GATHER && (warp == 0 || warp == 2 || warp == 3)) {
+    // ------------------------------------------------------------ rows by an index: 8 lanes copy 128 bytes of a row
+    const int first = 4 * (warp ? warp - 1 : 0) + (lane >> 3), chunk = lane & 7;   // rows first, first + 12, ... of the CTA's
+    const uint32_t dst = b_smem + (uint32_t)first * 128u;
+    int s = 0, issued = 0;
+    uint32_t phase = 0;
+    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
+      const int half = ((t.n + 31) & ~31) / 2, r0 = t.r0 + rank * half, n = t.n - rank * half;
+      int who[TL_HALF / 12];
+#pragma unroll
+      for (int i = 0; i < TL_HALF / 12; ++i) {
+        const int c = first + 12 * i;
+        who[i] = c < min(n, half) ? p.rows[r0 + c] : -1;
+        if (who[i] >= p.act_rows) who[i] = -1;   // (outside: zeros)
+      }
+      for (int kb = 0; kb < nk; ++kb) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->b_empty[s]), phase ^ 1u));
+        if (!ok) break;
+        const int k = kb * 64 + chunk * 8;
+        const uint16_t* const x = p.act + k;
+        const bool in = k < p.C;
+#pragma unroll
+        for (int i = 0; i < TL_HALF / 12; ++i) {
+          const int c = first + 12 * i;
+          const bool there = in && who[i] >= 0;
+          if (c < half) copy16(dst + s * TL_B_BYTES + i * 1536 + ((chunk ^ (c & 7)) << 4), there ? x + (size_t)who[i] * (size_t)p.ld_act : p.act, there);
+        }
+        copy_commit();
+        if (++s == STAGES) {
+          s = 0;
+          phase ^= 1u;
+        }
+        if (++issued > TL_PENDING) {   // the oldest stage on its way has landed
+          copy_wait<TL_PENDING>();
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) arrive_at_first(smem_u32(&bars->b_full[(s + STAGES - 1 - TL_PENDING) % STAGES]));
+        }
+      }
+    }
+    copy_wait<0>();
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0)
+      for (int i = min(issued, TL_PENDING); i > 0; --i) arrive_at_first(smem_u32(&bars->b_full[(s + STAGES - i) % STAGES]));
+    if (!ok && lane == 0) raise_status(p.status, 20);
+  } else if (!GATHER && warp == 0) {
+    // ------------------------------------------------------------ rows: one stage is 64 input channels of the tile's rows
+    int s = 0, filled = 0;
+    uint32_t phase = 0;
+    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
+      const int half = ((t.n + 31) & ~31) / 2, r0 = t.r0 + rank * half;
+      const uint32_t bytes = (uint32_t)((half + TL_BOX - 1) / TL_BOX * TL_BOX) * 256u;   // of both CTAs
+      for (int kb = 0; kb < nk; ++kb) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->b_empty[s]), phase ^ 1u));
+        if (!ok) break;
+        const uint32_t full = smem_u32(&bars->b_full[s]), dst = b_smem + s * TL_B_BYTES;
+        if (rank == 0 && lane == 0) mbar_expect_tx(full, bytes);
+        __syncwarp();
+        if (lane * TL_BOX < half) tma_rows(dst + lane * TL_BOX * 128, &map, kb * 64, r0 + lane * TL_BOX, at_first(full));
+        filled = min(filled + 1, STAGES);
+        if (++s == STAGES) {
+          s = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    // both CTAs' copies in flight land before the pair ends, whatever became of the other warps
+    for (int i = 0; rank == 0 && i < filled; ++i) {
+      if (--s < 0) {
+        s = STAGES - 1;
+        phase ^= 1u;
+      }
+      ok = mbar_wait(smem_u32(&bars->b_full[s]), phase) && ok;
+    }
+    if (!ok && lane == 0) raise_status(p.status, 21);
+  } else if (warp == 1 && rank == 0) {
+    // ------------------------------------------------------------ MMA, for both CTAs
+    int s = 0, a = 0, d = 0;
+    uint32_t b_phase = 0, a_phase = 0, d_phase = 0;
+    const uint32_t type = std::is_same<T, BF16>::value ? 1u : 0u, leader = elect_one(), tmem_u = (uint32_t)uni((int)tmem);
+    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
+      const uint32_t n32 = (uint32_t)(t.n + 31) & ~31u;   // (a pair's instructions take multiples of 32)
+      const uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((n32 >> 3) << 17) | ((256u >> 4) << 24);
+      const uint32_t acc = tmem_u + TL_D0 + d * TL_N;
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_empty[d]), d_phase ^ 1u));
+      for (int kb = 0; ok && kb < nk; ++kb) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->b_full[s]), b_phase) && mbar_wait(smem_u32(&bars->a_full[a]), a_phase));
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t desc = ((uint64_t)2 << 61) | ((uint64_t)1 << 46) | ((uint64_t)64 << 32) | ((uint64_t)1 << 16) | ((b_smem + s * TL_B_BYTES) >> 4);
+        stage_ts_f16(acc, tmem_u + a * TL_A_COLS, desc, idesc, kb ? 1u : 0u, smem_u32(&bars->b_empty[s]), smem_u32(&bars->a_empty[a]), leader);
+        __syncwarp();
+        if (++s == STAGES) {
+          s = 0;
+          b_phase ^= 1u;
+        }
+        if (++a == TL_A_STAGES) {
+          a = 0;
+          a_phase ^= 1u;
+        }
+      }
+      if (!ok) break;
+      commit_on(smem_u32(&bars->d_full[d]), leader);
+      __syncwarp();
+      if ((d ^= 1) == 0) d_phase ^= 1u;
+    }
+    commit_on(smem_u32(&bars->drain), leader);
+    __syncwarp();
+    ok = mbar_wait(smem_u32(&bars->drain), 0) && ok;
+    if (!ok && lane == 0) raise_status(p.status, 22);
+  } else if (warp >= 4 && warp < 12) {
+    // ------------------------------------------------------------ weights: thread m of a warpgroup is channel m of the tile
+    const int m = ((int)threadIdx.x - 128) & 127, group = (warp - 4) >> 2;   // blocks group, group + 2, ... of a tile
+    const int shift = (m >> 3) & 1 ? 8 : 0;
+    const uint32_t dst = tmem + ((uint32_t)(m & ~31) << 16);
+    uint32_t base = 0;      // blocks of the tiles before
+    uint32_t stored = ~0u;  // a block that is on its way to tensor memory; it is waited for when the next one has been expanded
+    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs, base += (uint32_t)nk) {
+      const uint4* src = reinterpret_cast<const uint4*>(p.bits) + ((size_t)(t.e * p.n_mt + t.ct * 8 + (m >> 4)) * p.n_kb) * 32 + 4 * (m & 7) + 2 * group;
+      uint4 next[2] = {ld16(src), ld16(src + 1)};
+      for (int kb = 0; ok && kb < p.n_kb; ++kb) {
+        const uint32_t w[2][4] = {{next[0].x >> shift, next[0].z >> shift, next[1].x >> shift, next[1].z >> shift},
+                                  {next[0].y >> shift, next[0].w >> shift, next[1].y >> shift, next[1].w >> shift}};
+        if (kb + 1 < p.n_kb) {
+          next[0] = ld16(src + (size_t)(kb + 1) * 32);
+          next[1] = ld16(src + (size_t)(kb + 1) * 32 + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int block = 4 * kb + 2 * i + group;
+          if (block >= nk) break;
+          uint32_t v[32];
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 * q + j] = plus_minus<T>(w[i][q], 15 - j);
+          if (stored != ~0u) {
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at_first(smem_u32(&bars->a_full[stored]));
+          }
+          const uint32_t at = base + (uint32_t)block;
+          stored = at % TL_A_STAGES;
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->a_empty[stored]), (at / TL_A_STAGES & 1u) ^ 1u));
+          if (!ok) break;
+          tc_fence_after();
+          tmem_st32(dst + stored * TL_A_COLS, v);
+        }
+      }
+    }
+    if (stored != ~0u) {
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (ok && lane == 0) arrive_at_first(smem_u32(&bars->a_full[stored]));
+    }
+    if (!ok && lane == 0) raise_status(p.status, 23);
+  } else if (warp >= 12) {
+    // ------------------------------------------------------------ outputs: thread m is channel m of the tile, a column is a row
+    const int m = (int)threadIdx.x - 384;
+    float4* const h_smem = reinterpret_cast<float4*>(smem + STAGES * TL_B_BYTES);
+    int* const who = bars->who;
+    int d = 0;
+    uint32_t phase = 0;
+    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
+      const int co = t.ct * 128 + m;
+      const float alpha = p.alpha[(size_t)t.e * p.n_mt * 16 + co];
+      BRow<T, RANK> bv;
+      int held = -1;
+      if (RANK) {   // the rows' A x and adapters, while the sums are under way
+        const int quads = t.n * p.low.rank / 4;
+        const float* h = p.low.h + (size_t)t.r0 * p.low.rank;
+        for (int i = m; i < quads; i += 128) copy16(smem_u32(h_smem + i), h + 4 * i, true);
+        copy_commit();
+        for (int i = m; i < t.n; i += 128) {
+          const int a = p.low.adapter[t.r0 + i];
+          who[i] = a < p.low.n ? a : -1;
+        }
+        copy_wait<0>();
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), phase));
+      if (RANK) ok = bar_all<1, 128>(ok);   // (everybody's part of A x has landed; the four warps go on, or give up, together)
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t src = tmem + ((uint32_t)(m & ~31) << 16) + TL_D0 + d * TL_N;
+      const long long first = (long long)t.r0 * p.ld_out + co;
+      if (RANK == 0) {
+        for (int c0 = 0; c0 < t.n; c0 += 32) {
+          uint32_t v[32];
+          tmem_ld32(src + c0, v);
+          const int n = co < p.K ? min(32, t.n - c0) : 0;
+          const long long at = first + c0 * p.ld_out;
+          if (p.out_type == SNN_OUT_F32) store_column(static_cast<float*>(p.out) + at, p.ld_out, n, alpha, v);
+          else if (p.out_type == SNN_OUT_F16) store_column(static_cast<__half*>(p.out) + at, p.ld_out, n, alpha, v);
+          else store_column(static_cast<__nv_bfloat16*>(p.out) + at, p.ld_out, n, alpha, v);
+          __syncwarp();
+        }
+      } else {
+        // rows of one adapter lie together: a channel's row of B stays in registers until the next one's
+        const int n_rank = p.low.rank;
+        for (int c0 = 0; c0 < t.n; c0 += 8) {
+          uint32_t v[8];
+          tmem_ld8(src + c0, v);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            float f = alpha * __uint_as_float(v[c]);
+            const int a = c0 + c < t.n ? who[c0 + c] : -1;   // (the same for the whole warp)
+            if (a >= 0) {
+              if (a != held) {
+                held = a;
+                const uint16_t* b = static_cast<const uint16_t*>(p.low.b) + ((size_t)held * p.K + min(co, p.K - 1)) * n_rank;
+                // (channels of one tile, one adapter: the rows of B of a warp are neighbours)
+#pragma unroll
+                for (int j = 0; j < RANK / 8; ++j) {
+                  const uint4 u = 8 * j < n_rank ? ld16(b + 8 * j) : make_uint4(0, 0, 0, 0);
+                  bv.set(j, u);
+                }
+              }
+              const float4* h = h_smem + (size_t)(c0 + c) * (n_rank / 4);
+              uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+              for (int j = 0; j < RANK / 8; ++j) {
+                if (8 * j >= n_rank) break;
+                const ulonglong2 h0 = *reinterpret_cast<const ulonglong2*>(h + 2 * j), h1 = *reinterpret_cast<const ulonglong2*>(h + 2 * j + 1);
+                uint64_t w[4];
+                bv.get(j, w);
+                fma2(s0, w[0], h0.x);
+                fma2(s1, w[1], h0.y);
+                fma2(s0, w[2], h1.x);
+                fma2(s1, w[3], h1.y);
+              }
+              f += sum2(s0) + sum2(s1);
+            }
+            if (co < p.K && c0 + c < t.n) store_out(p.out, p.out_type, first + (c0 + c) * p.ld_out, f);
+          }
+          __syncwarp();
+        }
+        bar_sync_some<1, 128>();   // (everybody has read A x)
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_at_first(smem_u32(&bars->d_empty[d]));
+      if ((d ^= 1) == 0) phase ^= 1u;
+    }
+    if (!ok && lane == 0) raise_status(p.status, 24);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) mbar_wait(smem_u32(&bars->drain), 0);   // (the last arrival here from the pair's MMAs)
+  __syncwarp();
+  pair_sync();
+  tc_fence_after();
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+using MapEncoder = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// The driver's tensor-map encoder, looked up once (the library does not link the driver).
+MapEncoder map_encoder() {
+  static const MapEncoder f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      p = nullptr;
+    }
+    return reinterpret_cast<MapEncoder>(p);
+  }();
+  return f;
+}
+
+template <class T, bool GATHER, int RANK>
+cudaError_t tall_launch(const Products& p, const ProductCall& c, const CUtensorMap& map, int* launched) {
+  static unsigned long long done = 0;
+  cudaError_t e = allow_max_smem(products_tall_kernel<T, GATHER, RANK>, &done);
+  if (e != cudaSuccess) return e;
+  const TallParams q{p.bits, p.alpha, static_cast<const uint16_t*>(c.act), c.rows, c.offsets, c.out, c.ld_act, c.ld_out, c.act_rows, c.max_rows, p.E, p.C, p.K, p.n_mt, p.n_kb, c.out_type,
+                     (p.K + 255) / 256, p.status_dev, c.low};
+  const long long tiles = ((long long)c.max_rows / TL_N + (c.offsets ? min(p.E, c.max_rows) : 1)) * q.n_cp;
+  const size_t smem = 1024 + TallShape<RANK>::kStages * TL_B_BYTES + TallShape<RANK>::kH + sizeof(TallBars) + (size_t)p.E * 12;
+  products_tall_kernel<T, GATHER, RANK><<<2u * (unsigned)min(tiles, (long long)max(1, sm_count() / 2)), TL_THREADS, smem, c.stream>>>(q, map);
+  *launched += 1;
+  return cudaGetLastError();
+}
+
+template <class T>
+cudaError_t tall_kind(const Products& p, const ProductCall& c, const CUtensorMap& map, int* launched) {
+  if (!c.low.adapter) return c.rows ? tall_launch<T, true, 0>(p, c, map, launched) : tall_launch<T, false, 0>(p, c, map, launched);
+  if (c.low.rank <= 16) return tall_launch<T, false, 16>(p, c, map, launched);
+  if (c.low.rank <= 32) return tall_launch<T, false, 32>(p, c, map, launched);
+  if (c.low.rank <= 64) return tall_launch<T, false, 64>(p, c, map, launched);
+  return tall_launch<T, false, 128>(p, c, map, launched);
+}
+
+}  // namespace
+
+cudaError_t products_tall(const Products& p, const ProductCall& c, int* launched) {
+  const MapEncoder encode = map_encoder();
+  if (!encode) return cudaErrorNotSupported;
+  CUtensorMap map;
+  const bool bf16 = c.act_type != SNN_ACT_F16;
+  const cuuint64_t dims[2] = {(cuuint64_t)p.C, (cuuint64_t)c.act_rows}, strides[1] = {(cuuint64_t)c.ld_act * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)TL_BOX}, steps[2] = {1, 1};
+  if (encode(&map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(c.act), dims, strides, box, steps,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  return bf16 ? tall_kind<BF16>(p, c, map, launched) : tall_kind<F16>(p, c, map, launched);
+}
+
+}  // namespace snn
