@@ -12,59 +12,108 @@ struct ShrinkParams {
   const float* scale;
   float* h;
   long long ld_act;
-  int rows, C, n, rank;
+  int rows, C, n, rank, per_cta;
 };
 
-// A CTA takes 8 neighbouring rows and 16 of the rank; its warps take different input channels, and their sums meet in shared
+// A CTA takes up to 8 NT neighbouring rows and 16 MT of the rank; its warps take different input channels, and their sums meet in shared
 // memory.  One pass for each adapter that the rows have (rows of one request lie together: mostly one); the rows of other adapters are
-// computed along and not written, since the instruction has 8 columns in any case.
-template <class T>
+// computed along and not written.  Bound by reading A: once for each CTA, so with few rows a CTA has few of them, and all of A's
+// readers run at once; with many rows 16, and A comes from L2.
+template <class T, int NT, int MT, int U>
 __global__ void __launch_bounds__(256) shrink_kernel(const ShrinkParams p) {
-  __shared__ float red[8][8][17];
+  constexpr int N = 8 * NT, M = 16 * MT;
+  __shared__ float red[8][N][M + 1];
+  __shared__ int who[N];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int r0 = (int)blockIdx.x * 8, j0 = (int)blockIdx.y * 16;
-  const int mine = r0 + g < p.rows ? p.adapter[r0 + g] : -1;   // of row g
-  const uint16_t* x = p.act + (size_t)min(r0 + g, p.rows - 1) * (size_t)p.ld_act;
-  for (int c = 0; c < 8; ++c) {
-    const int a = __shfl_sync(0xffffffffu, mine, 4 * c);
-    const unsigned same = __ballot_sync(0xffffffffu, mine == a);
-    if (a < 0 || a >= p.n || (same & ((1u << (4 * c)) - 1u))) continue;   // none, or seen before
-    const uint16_t* w0 = p.a + ((size_t)a * p.rank + j0 + g) * p.C;
-    const uint16_t* w1 = w0 + (size_t)8 * p.C;
-    const bool two = j0 + 8 < p.rank;
-    float acc[4] = {};
-    for (int k = warp * 64; k < p.C; k += 512) {
+  const int r0 = (int)blockIdx.x * p.per_cta, n = min(p.per_cta, p.rows - r0), j0 = (int)blockIdx.y * M;
+  if (threadIdx.x < N) {
+    const int a = (int)threadIdx.x < n ? p.adapter[r0 + threadIdx.x] : -1;
+    who[threadIdx.x] = a >= 0 && a < p.n ? a : -1;
+  }
+  __syncthreads();
+  const uint16_t* x[NT];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int i = k + 16 * t + 8 * h;
-        const bool in = i < p.C;
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        const uint4 u = in ? ld16(w0 + i) : zero, v = in && two ? ld16(w1 + i) : zero, b = in ? ld16(x + i) : zero;
-        mma_16x8<T>(acc, u.x, v.x, u.y, v.y, b.x, b.y);
-        mma_16x8<T>(acc, u.z, v.z, u.w, v.w, b.z, b.w);
-      }
+  for (int i = 0; i < NT; ++i) x[i] = 8 * i + g < n ? p.act + (size_t)(r0 + 8 * i + g) * (size_t)p.ld_act + 16 * t : nullptr;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  for (int c = 0; c < n; ++c) {
+    const int a = who[c];
+    bool seen = a < 0;
+    for (int i = 0; i < c; ++i) seen = seen || who[i] == a;
+    if (seen) continue;
+    const uint16_t* w[2 * MT];
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) w[i] = j0 + 8 * i < p.rank ? p.a + ((size_t)a * p.rank + j0 + 8 * i + g) * p.C + 16 * t : nullptr;
+    float acc[MT][NT][4] = {};
+    // U blocks of 64 input channels on their way, then their products
+    for (int k0 = warp * 64; k0 < p.C; k0 += 512 * U) {
+      uint4 b[U][NT][2], u[U][2 * MT][2];
+#pragma unroll
+      for (int v = 0; v < U; ++v)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k = k0 + 512 * v + 8 * h;
+          const bool in = k + 16 * t < p.C;
+#pragma unroll
+          for (int i = 0; i < 2 * MT; ++i) u[v][i][h] = in && w[i] ? ld16(w[i] + k) : zero;
+#pragma unroll
+          for (int i = 0; i < NT; ++i) b[v][i][h] = in && x[i] ? ld16(x[i] + k) : zero;
+        }
+#pragma unroll
+      for (int v = 0; v < U; ++v)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              const uint4 &lo = u[v][2 * m][h], &hi = u[v][2 * m + 1][h], &r = b[v][i][h];
+              mma_16x8<T>(acc[m][i], lo.x, hi.x, lo.y, hi.y, r.x, r.y);
+              mma_16x8<T>(acc[m][i], lo.z, hi.z, lo.w, hi.w, r.z, r.w);
+            }
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) red[warp][2 * t + (q & 1)][g + 8 * (q >> 1)] = acc[q];
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) red[warp][8 * i + 2 * t + (q & 1)][16 * m + g + 8 * (q >> 1)] = acc[m][i][q];
     __syncthreads();
-    if (threadIdx.x < 128) {
-      const int row = threadIdx.x >> 4, j = threadIdx.x & 15;
+    for (int i = threadIdx.x; i < n * M; i += 256) {
+      const int row = i / M, j = i % M;
+      if (who[row] != a || j0 + j >= p.rank) continue;
       float s = 0.f;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) s += red[w][row][j];
-      if ((same >> (4 * row)) & 1u && j0 + j < p.rank) p.h[(size_t)(r0 + row) * p.rank + j0 + j] = p.scale[a] * s;
+      for (int v = 0; v < 8; ++v) s += red[v][row][j];
+      p.h[(size_t)(r0 + row) * p.rank + j0 + j] = p.scale[a] * s;
     }
     __syncthreads();
+  }
+}
+
+template <class T, int NT, int MT, int U>
+void shrink_launch(const ShrinkParams& p, cudaStream_t s) {
+  shrink_kernel<T, NT, MT, U><<<dim3((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT))), 256, 0, s>>>(p);
+}
+
+template <class T>
+void shrink_type(ShrinkParams p, cudaStream_t s) {
+  const int sms = sm_count();
+  if (p.rows >= 16 * sms) {
+    p.per_cta = 16;
+    if (p.rank > 16) shrink_launch<T, 2, 2, 2>(p, s);
+    else shrink_launch<T, 2, 1, 2>(p, s);
+  } else {
+    p.per_cta = max(1, min(8, p.rows / sms));
+    shrink_launch<T, 1, 1, 4>(p, s);
   }
 }
 
 }  // namespace
 
 cudaError_t shrink_forward(const ShrinkCall& c, int* launched) {
-  const ShrinkParams p{static_cast<const uint16_t*>(c.act), static_cast<const uint16_t*>(c.a), c.adapter, c.scale, c.h, c.ld_act, c.rows, c.C, c.n, c.rank};
-  const dim3 grid((unsigned)((c.rows + 7) / 8), (unsigned)((c.rank + 15) / 16));
-  if (c.act_type == SNN_ACT_F16) shrink_kernel<F16><<<grid, 256, 0, c.stream>>>(p);
-  else shrink_kernel<BF16><<<grid, 256, 0, c.stream>>>(p);
+  const ShrinkParams p{static_cast<const uint16_t*>(c.act), static_cast<const uint16_t*>(c.a), c.adapter, c.scale, c.h, c.ld_act, c.rows, c.C, c.n, c.rank, 8};
+  if (c.act_type == SNN_ACT_F16) shrink_type<F16>(p, c.stream);
+  else shrink_type<BF16>(p, c.stream);
   *launched += 1;
   return cudaGetLastError();
 }

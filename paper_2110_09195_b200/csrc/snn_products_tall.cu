@@ -29,13 +29,17 @@ constexpr int TL_D0 = TL_A_STAGES * TL_A_COLS;
 constexpr int TL_HALF = TL_N / 2;      // rows of a CTA
 constexpr int TL_B_BYTES = TL_HALF * 128;
 constexpr int TL_BOX = 32;            // rows of one TMA box
-constexpr int TL_THREADS = 512;       // warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs
+// warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs (with adapters: 12-19)
 constexpr int TL_PENDING = 8;         // stages of copied rows on their way
-// Stages of rows, and 32-bit values of A x for each row kept beside them (RANK: 0 without adapters, else a bound of their rank).
+// Stages of rows, and bytes of the tile's rows' A x and of an adapter's B kept beside them (RANK: 0 without adapters, else a bound of
+// their rank).
 template <int RANK>
 struct TallShape {
-  static constexpr int kStages = RANK == 128 ? 8 : RANK == 64 ? 12 : RANK == 32 ? 14 : RANK == 16 ? 15 : 16;
-  static constexpr int kH = RANK * TL_N * 4;
+  static constexpr int kStages = RANK == 128 ? 4 : RANK == 64 ? 10 : RANK == 32 ? 13 : RANK == 16 ? 15 : 16;
+  static constexpr int kOutWarps = RANK ? 8 : 4;
+  static constexpr int kThreads = 384 + 32 * kOutWarps;
+  static constexpr int kH = RANK ? TL_N * (RANK + 4) * 4 : 0;       // fp32, rows in different banks
+  static constexpr int kB = RANK ? 256 * (RANK + 8) * 2 : 0;        // 16-bit, the same; each warp its own
 };
 
 // The same value in all lanes, known to be so
@@ -55,8 +59,9 @@ struct TallParams {
 
 struct TallBars {
   uint64_t b_full[16], b_empty[16], a_full[TL_A_STAGES], a_empty[TL_A_STAGES], d_full[2], d_empty[2], drain;
-  uint32_t tmem;
-  int who[TL_N];   // adapters of the tile's rows, below 0: none
+  uint32_t tmem, pad;
+  int who[TL_N];         // adapters of the tile's rows, below 0: none
+  int group[TL_N / 8];   // of eight rows
 };
 
 // Issued by the lanes for which `on` is not 0: D[256 x N] (+)= A[256 x 64] * B[N x 64]^T in four steps of 16, A in tensor memory, then the
@@ -95,13 +100,15 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// 8 columns; load and wait are one statement
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+// 8 columns of the warp's 32 lanes, a thread (g = lane / 4, t = lane % 4): columns 2t and 2t + 1 of lanes g and g + 8 (first four values),
+// g + 16 and g + 24.  Loads and wait are one statement.
+__device__ __forceinline__ void tmem_ld_16x8(uint32_t taddr, float (&v)[2][4]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
+      "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%8];\n\t"
+      "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%4,%5,%6,%7}, [%9];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-      : "r"(taddr)
+      : "=f"(v[0][0]), "=f"(v[0][1]), "=f"(v[0][2]), "=f"(v[0][3]), "=f"(v[1][0]), "=f"(v[1][1]), "=f"(v[1][2]), "=f"(v[1][3])
+      : "r"(taddr), "r"(taddr + (16u << 16))
       : "memory");
 }
 // (the barrier: the pair's first CTA's)
@@ -119,19 +126,6 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// two products and sums at once
-__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b)); }
-__device__ __forceinline__ uint64_t pack2(float2 v) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
-  return r;
-}
-__device__ __forceinline__ float sum2(uint64_t v) {
-  float a, b;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
-  return a + b;
-}
-
 // The address of the pair's first CTA's copy of a variable in shared memory, and an arrival there.  What the arrival stands for is in tensor
 // memory or in the SM's own shared memory, after wait::st, wait::ld or a proxy fence, and is read by the MMA unit: no wider release is needed
 // (one of cluster scope, with waits that acquire at that scope, made every stage take 900 cycles, whatever its size).
@@ -193,40 +187,105 @@ __device__ __forceinline__ void store_column(O* out, long long ld, int n, float 
     if (c < n) to_out(out, alpha * __uint_as_float(v[c]));
 }
 
-// A channel's row of B in registers: pairs of fp32 values, or (the longest) as it is stored.
-template <class T, int RANK>
-struct BRow {
-  uint64_t v[RANK ? RANK / 2 : 1];
-  __device__ __forceinline__ void set(int j, uint4 u) {
-    v[4 * j] = pack2(T::unpack(u.x));
-    v[4 * j + 1] = pack2(T::unpack(u.y));
-    v[4 * j + 2] = pack2(T::unpack(u.z));
-    v[4 * j + 3] = pack2(T::unpack(u.w));
+// 32 channels from co0, up to 8 rows from r0, in the layout of tmem_ld_16x8.  16-bit outputs change hands first: a thread then has four
+// neighbouring channels of a row (twice), eight threads a row's 32 bytes.
+__device__ __forceinline__ uint32_t pack_out(int type, float lo, float hi) {
+  uint32_t r;
+  if (type == SNN_OUT_F16) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    memcpy(&r, &h, 4);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    memcpy(&r, &h, 4);
   }
-  __device__ __forceinline__ void get(int j, uint64_t (&w)[4]) const {
+  return r;
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void store_16x8(const TallParams& p, int r0, int n, int co0, const float (&v)[2][4]) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  if (p.out_type == SNN_OUT_F32) {
+    float* const out = static_cast<float*>(p.out) + (long long)(r0 + 2 * q) * p.ld_out + co0 + g;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = v[4 * j + i];
+    for (int i = 0; i < 8; ++i)
+      if (2 * q + (i & 1) < n && co0 + g + 8 * (i >> 1) < p.K) out[(i & 1) * p.ld_out + 8 * (i >> 1)] = v[i >> 2][i & 3];
+    return;
   }
-};
+  uint32_t w[4];   // row g, channels 8 i + 2 q and the next
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = transpose_8x8(pack_out(p.out_type, v[i >> 1][2 * (i & 1)], v[i >> 1][2 * (i & 1) + 1]));
+#pragma unroll
+  for (int i = 0; i < 4; i += 2) {
+    // an even q gives its pair of the second eight for its neighbour's of the first
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, q & 1 ? w[i] : w[i + 1], 1);
+    const uint32_t lo = q & 1 ? other : w[i], hi = q & 1 ? w[i + 1] : other;
+    const int co = co0 + 8 * (i + (q & 1)) + 2 * (q & 2);
+    if (g < n && co < p.K) {
+      uint16_t* const out = static_cast<uint16_t*>(p.out) + (long long)(r0 + g) * p.ld_out + co;
+      if (co + 4 <= p.K && ((uintptr_t)out & 7) == 0) {
+        *reinterpret_cast<uint2*>(out) = make_uint2(lo, hi);
+      } else {
+        const uint16_t part[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (co + k < p.K) out[k] = part[k];
+      }
+    }
+  }
+}
+
+// B (A x) in fp32 on the FMA units, two of the rank at a time, in the layout of tmem_ld_16x8: a thread has four channels and two rows of
+// eight, so that a value from shared memory serves two or four products.  Two warps for each 32 channels, which take turns at eight rows: one
+// alone is bound by latency, 142 us for 4096 rows of 4096 x 4096 and rank 32.  (On the warp's matrix instruction, with A x in three 16-bit or
+// two tf32 parts, each instruction waited for one of the pair's: 72 to 96 cycles.  With a channel a thread, and a load of A x for every two
+// products: 163 us.)
+__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b)); }
+__device__ __forceinline__ uint64_t pack2(float2 v) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+  return r;
+}
+__device__ __forceinline__ float sum2(uint64_t v) {
+  float a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+  return a + b;
+}
+// 8 of the rank: b, of channels g, g + 8, g + 16, g + 24; h, of rows 2t and 2t + 1, h_row floats apart
 template <class T>
-struct BRow<T, 128> {
-  uint4 v[16];
-  __device__ __forceinline__ void set(int j, uint4 u) { v[j] = u; }
-  __device__ __forceinline__ void get(int j, uint64_t (&w)[4]) const {
-    w[0] = pack2(T::unpack(v[j].x));
-    w[1] = pack2(T::unpack(v[j].y));
-    w[2] = pack2(T::unpack(v[j].z));
-    w[3] = pack2(T::unpack(v[j].w));
+__device__ __forceinline__ void lowrank_step(uint64_t (&d)[2][4], const uint4 (&b)[4], const float* h, int h_row) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    ulonglong2 x[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const ulonglong2*>(h + i * h_row + 4 * half);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const uint64_t w0 = pack2(T::unpack(half ? b[c].z : b[c].x)), w1 = pack2(T::unpack(half ? b[c].w : b[c].y));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fma2(d[i][c], w0, x[i].x);
+        fma2(d[i][c], w1, x[i].y);
+      }
+    }
   }
-};
+}
+// ... added to the outputs of the rows whose bit is set
+__device__ __forceinline__ void add_lowrank(float (&v)[2][4], const uint64_t (&d)[2][4], uint32_t which) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if ((which >> (i & 1)) & 1u) v[i >> 2][i & 3] += sum2(d[i & 1][i >> 1]);
+}
 
 // RANK: 0 without adapters, else a bound of their rank.
 template <class T, bool GATHER, int RANK>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TL_THREADS, 1) products_tall_kernel(const TallParams p, const __grid_constant__ CUtensorMap map) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kThreads, 1) products_tall_kernel(const TallParams p, const __grid_constant__ CUtensorMap map) {
   constexpr int STAGES = TallShape<RANK>::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  TallBars* const bars = reinterpret_cast<TallBars*>(smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH);
+  TallBars* const bars = reinterpret_cast<TallBars*>(smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH + TallShape<RANK>::kB);
   Ranges R;
   R.lo = reinterpret_cast<int*>(bars + 1);
   R.n = R.lo + p.E;
@@ -264,7 +323,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TL_THREADS, 1) produ
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bars->d_full[i]), 1);
-      mbar_init(smem_u32(&bars->d_empty[i]), 8);
+      mbar_init(smem_u32(&bars->d_empty[i]), 2 * TallShape<RANK>::kOutWarps);
     }
     mbar_init(smem_u32(&bars->drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -443,29 +502,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TL_THREADS, 1) produ
     if (!ok && lane == 0) raise_status(p.status, 23);
   } else if (warp >= 12) {
     // ------------------------------------------------------------ outputs: thread m is channel m of the tile, a column is a row
-    const int m = (int)threadIdx.x - 384;
-    float4* const h_smem = reinterpret_cast<float4*>(smem + STAGES * TL_B_BYTES);
-    int* const who = bars->who;
+    const int m = ((int)threadIdx.x - 384) & 127, turn = (warp - 12) >> 2;
+    constexpr int OUTS = 32 * TallShape<RANK>::kOutWarps;
+    const int h_row = p.low.rank + 4, b_row = p.low.rank + 8;   // (elements)
+    float* const h_smem = reinterpret_cast<float*>(smem + STAGES * TL_B_BYTES);
+    uint16_t* const b_smem_warp = reinterpret_cast<uint16_t*>(smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH) + (warp - 12) * 32 * b_row;
+    int *const who = bars->who, *const group = bars->group;
+    constexpr int MIXED = -2;
     int d = 0;
     uint32_t phase = 0;
     for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
       const int co = t.ct * 128 + m;
       const float alpha = p.alpha[(size_t)t.e * p.n_mt * 16 + co];
-      BRow<T, RANK> bv;
       int held = -1;
-      if (RANK) {   // the rows' A x and adapters, while the sums are under way
-        const int quads = t.n * p.low.rank / 4;
-        const float* h = p.low.h + (size_t)t.r0 * p.low.rank;
-        for (int i = m; i < quads; i += 128) copy16(smem_u32(h_smem + i), h + 4 * i, true);
+      if (RANK) {   // the rows' adapters and A x, while the sums are under way
+        const int quads = p.low.rank / 4;
+        for (int i = (int)threadIdx.x - 384; i < t.n * quads; i += OUTS)
+          copy16(smem_u32(h_smem + (i / quads) * h_row + 4 * (i % quads)), p.low.h + (size_t)t.r0 * p.low.rank + 4 * i, true);
         copy_commit();
-        for (int i = m; i < t.n; i += 128) {
-          const int a = p.low.adapter[t.r0 + i];
-          who[i] = a < p.low.n ? a : -1;
+        for (int i = (int)threadIdx.x - 384; i < TL_N; i += OUTS) {
+          const int a = i < t.n ? p.low.adapter[t.r0 + i] : -1, one = a >= 0 && a < p.low.n ? a : -1;
+          who[i] = one;
+          // the adapter that the eight rows around this one have (those behind the last count with it)
+          const int lead = __shfl_sync(0xffffffffu, one, lane & 24);
+          const unsigned same = __ballot_sync(0xffffffffu, one == lead || i >= t.n);
+          if ((i & 7) == 0) group[i >> 3] = ((same >> (lane & 24)) & 255u) == 255u ? lead : MIXED;
         }
         copy_wait<0>();
       }
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), phase));
-      if (RANK) ok = bar_all<1, 128>(ok);   // (everybody's part of A x has landed; the four warps go on, or give up, together)
+      if (RANK) ok = bar_all<1, OUTS>(ok);   // (everybody's part of A x has landed; the warps go on, or give up, together)
       if (!ok) break;
       tc_fence_after();
       const uint32_t src = tmem + ((uint32_t)(m & ~31) << 16) + TL_D0 + d * TL_N;
@@ -482,46 +548,61 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TL_THREADS, 1) produ
           __syncwarp();
         }
       } else {
-        // rows of one adapter lie together: a channel's row of B stays in registers until the next one's
-        const int n_rank = p.low.rank;
-        for (int c0 = 0; c0 < t.n; c0 += 8) {
-          uint32_t v[8];
-          tmem_ld8(src + c0, v);
+        // Eight rows at a time.  Rows of one request lie together, so they mostly have one adapter: its B stays in shared memory until the
+        // next one's.  Else there is a pass for each of their adapters.
+        const int n_rank = p.low.rank, g = lane >> 2, q = lane & 3, co0 = t.ct * 128 + (m & ~31);
+        float scale[4];
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            float f = alpha * __uint_as_float(v[c]);
-            const int a = c0 + c < t.n ? who[c0 + c] : -1;   // (the same for the whole warp)
-            if (a >= 0) {
-              if (a != held) {
-                held = a;
-                const uint16_t* b = static_cast<const uint16_t*>(p.low.b) + ((size_t)held * p.K + min(co, p.K - 1)) * n_rank;
-                // (channels of one tile, one adapter: the rows of B of a warp are neighbours)
+        for (int i = 0; i < 4; ++i) scale[i] = __shfl_sync(0xffffffffu, alpha, 8 * i + g);
+        const uint16_t* const b_all = static_cast<const uint16_t*>(p.low.b);
+        const size_t b_size = (size_t)p.K * n_rank;
+        for (int c0 = 8 * turn; c0 < t.n; c0 += 16) {
+          float v[2][4];
+          tmem_ld_16x8(src + c0, v);
 #pragma unroll
-                for (int j = 0; j < RANK / 8; ++j) {
-                  const uint4 u = 8 * j < n_rank ? ld16(b + 8 * j) : make_uint4(0, 0, 0, 0);
-                  bv.set(j, u);
-                }
-              }
-              const float4* h = h_smem + (size_t)(c0 + c) * (n_rank / 4);
-              uint64_t s0 = 0, s1 = 0;
-#pragma unroll
-              for (int j = 0; j < RANK / 8; ++j) {
-                if (8 * j >= n_rank) break;
-                const ulonglong2 h0 = *reinterpret_cast<const ulonglong2*>(h + 2 * j), h1 = *reinterpret_cast<const ulonglong2*>(h + 2 * j + 1);
-                uint64_t w[4];
-                bv.get(j, w);
-                fma2(s0, w[0], h0.x);
-                fma2(s1, w[1], h0.y);
-                fma2(s0, w[2], h1.x);
-                fma2(s1, w[3], h1.y);
-              }
-              f += sum2(s0) + sum2(s1);
+          for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] *= scale[i >> 1];
+          const float* const h = h_smem + (c0 + 2 * q) * h_row;
+          const int a = group[c0 >> 3];   // (the same for the whole warp)
+          if (a >= 0) {
+            if (a != held) {
+              held = a;
+              __syncwarp();
+              const int chunks = n_rank / 8, all = min(32, p.K - co0) * chunks;
+              for (int i = lane; i < all; i += 32)
+                *reinterpret_cast<uint4*>(b_smem_warp + (i / chunks) * b_row + 8 * (i % chunks)) = ld16(b_all + a * b_size + (size_t)co0 * n_rank + 8 * i);
+              __syncwarp();
             }
-            if (co < p.K && c0 + c < t.n) store_out(p.out, p.out_type, first + (c0 + c) * p.ld_out, f);
+            uint64_t low[2][4] = {};
+#pragma unroll 2
+            for (int j = 0; j < n_rank; j += 8) {
+              uint4 b[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) b[i] = *reinterpret_cast<const uint4*>(b_smem_warp + (8 * i + g) * b_row + j);
+              lowrank_step<T>(low, b, h + j, h_row);
+            }
+            add_lowrank(v, low, 3u);
+          } else if (a == MIXED) {
+            const int mine = lane < 8 ? who[c0 + lane] : -1;
+            unsigned left = __ballot_sync(0xffffffffu, mine >= 0);
+            while (left) {
+              const int one = __shfl_sync(0xffffffffu, mine, __ffs(left) - 1);
+              const unsigned same = __ballot_sync(0xffffffffu, mine == one);
+              left &= ~same;
+              uint64_t low[2][4] = {};
+#pragma unroll 2
+              for (int j = 0; j < n_rank; j += 8) {
+                uint4 b[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[i] = ld16(b_all + one * b_size + (size_t)min(co0 + 8 * i + g, p.K - 1) * n_rank + j);
+                lowrank_step<T>(low, b, h + j, h_row);
+              }
+              // (rows are apart: what other rows' A x gives with this B goes nowhere)
+              add_lowrank(v, low, (same >> (2 * q)) & 3u);
+            }
           }
-          __syncwarp();
+          store_16x8(p, t.r0 + c0, t.n - c0, co0, v);
         }
-        bar_sync_some<1, 128>();   // (everybody has read A x)
+        bar_sync_some<1, OUTS>();   // (everybody has read A x)
       }
       tc_fence_before();
       __syncwarp();
@@ -564,8 +645,8 @@ cudaError_t tall_launch(const Products& p, const ProductCall& c, const CUtensorM
   const TallParams q{p.bits, p.alpha, static_cast<const uint16_t*>(c.act), c.rows, c.offsets, c.out, c.ld_act, c.ld_out, c.act_rows, c.max_rows, p.E, p.C, p.K, p.n_mt, p.n_kb, c.out_type,
                      (p.K + 255) / 256, p.status_dev, c.low};
   const long long tiles = ((long long)c.max_rows / TL_N + (c.offsets ? min(p.E, c.max_rows) : 1)) * q.n_cp;
-  const size_t smem = 1024 + TallShape<RANK>::kStages * TL_B_BYTES + TallShape<RANK>::kH + sizeof(TallBars) + (size_t)p.E * 12;
-  products_tall_kernel<T, GATHER, RANK><<<2u * (unsigned)min(tiles, (long long)max(1, sm_count() / 2)), TL_THREADS, smem, c.stream>>>(q, map);
+  const size_t smem = 1024 + TallShape<RANK>::kStages * TL_B_BYTES + TallShape<RANK>::kH + TallShape<RANK>::kB + sizeof(TallBars) + (size_t)p.E * 12;
+  products_tall_kernel<T, GATHER, RANK><<<2u * (unsigned)min(tiles, (long long)max(1, sm_count() / 2)), TallShape<RANK>::kThreads, smem, c.stream>>>(q, map);
   *launched += 1;
   return cudaGetLastError();
 }
