@@ -178,6 +178,7 @@ snn_status_t snn_conv_experts_combine(const void* y_dev, int32_t y_type, int32_t
     return api_fail(SNN_ERR_INVALID_ARG, "tokens=%d y_rows=%d columns=%d top_k=%d", tokens, y_rows, columns, top_k);
   if (ld_y < columns || ld_out < columns)
     return api_fail(SNN_ERR_INVALID_ARG, "rows of %lld and %lld for %d columns", (long long)ld_y, (long long)ld_out, columns);
+  if ((long long)tokens * columns >= (1ll << 38)) return api_fail(SNN_ERR_UNSUPPORTED, "%d tokens of %d columns: split the call", tokens, columns);
   if (tokens == 0) return SNN_OK;
   if (!slots_dev || !weights_dev || !out_dev || (y_rows > 0 && !y_dev)) return api_fail(SNN_ERR_INVALID_ARG, "null device pointer");
   if (((uintptr_t)y_dev & (out_size(y_type) - 1)) || ((uintptr_t)out_dev & (out_size(out_type) - 1)) || (((uintptr_t)slots_dev | (uintptr_t)weights_dev) & 3))

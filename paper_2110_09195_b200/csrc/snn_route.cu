@@ -199,8 +199,97 @@ struct CombineParams {
   const float* weights;
   void* out;
   long long ld_y, ld_out;
-  int y_type, y_rows, T, k, C, out_type;
+  int y_type, y_rows, T, k, C, out_type, groups;
 };
+
+// 8 neighbouring values as fp32, and their 16 or 32 bytes: read once, so they are the first to leave the caches.
+template <class Y>
+struct Eight;
+template <>
+struct Eight<float> {
+  uint4 lo, hi;
+  __device__ __forceinline__ void load(const float* p) {
+    lo = ld16_stream(p);
+    hi = ld16_stream(p + 4);
+  }
+  __device__ __forceinline__ void zero() { lo = hi = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ float2 pair(int i) const {
+    const uint4& v = i < 2 ? lo : hi;
+    return i & 1 ? make_float2(__uint_as_float(v.z), __uint_as_float(v.w)) : make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+  }
+};
+template <class T>
+struct Eight16 {
+  uint4 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = ld16_stream(p); }
+  __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ float2 pair(int i) const { return T::unpack(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
+};
+template <>
+struct Eight<F16> : Eight16<F16> {};
+template <>
+struct Eight<BF16> : Eight16<BF16> {};
+template <class Y>
+struct Element {
+  using type = uint16_t;
+};
+template <>
+struct Element<float> {
+  using type = float;
+};
+
+__device__ __forceinline__ uint32_t pack_pair(int type, float2 v) {
+  uint32_t r;
+  if (type == SNN_OUT_F16) {
+    const __half2 h = __floats2half2_rn(v.x, v.y);
+    memcpy(&r, &h, 4);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+    memcpy(&r, &h, 4);
+  }
+  return r;
+}
+
+// A thread sums 8 neighbouring columns of a token, 4 rows on their way at a time; neighbouring threads, neighbouring columns.  Bound by memory:
+// each row is read once.
+template <class Y>
+__global__ void __launch_bounds__(256) combine_kernel(const CombineParams p) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long t = i / p.groups;
+  const int c = (int)(i - t * p.groups) * 8;
+  if (t >= p.T) return;
+  const typename Element<Y>::type* const y = static_cast<const typename Element<Y>::type*>(p.y) + c;
+  float2 s[4] = {};
+  for (int j0 = 0; j0 < p.k; j0 += 4) {
+    Eight<Y> v[4];
+    float w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int slot = j0 + j < p.k ? p.slots[t * p.k + j0 + j] : -1;
+      const bool there = slot >= 0 && slot < p.y_rows;
+      w[j] = there ? p.weights[t * p.k + j0 + j] : 0.f;
+      if (there) v[j].load(y + slot * p.ld_y);
+      else v[j].zero();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float2 f = v[j].pair(q);
+        s[q].x = fmaf(w[j], f.x, s[q].x);
+        s[q].y = fmaf(w[j], f.y, s[q].y);
+      }
+  }
+  const long long at = t * p.ld_out + c;
+  if (p.out_type == SNN_OUT_F32) {
+    float4* const out = reinterpret_cast<float4*>(static_cast<float*>(p.out) + at);
+    __stcs(out, make_float4(s[0].x, s[0].y, s[1].x, s[1].y));
+    __stcs(out + 1, make_float4(s[2].x, s[2].y, s[3].x, s[3].y));
+  } else {
+    __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + at),
+           make_uint4(pack_pair(p.out_type, s[0]), pack_pair(p.out_type, s[1]), pack_pair(p.out_type, s[2]), pack_pair(p.out_type, s[3])));
+  }
+}
 
 __device__ __forceinline__ float value(const void* y, int type, long long i) {
   if (type == SNN_OUT_F32) return static_cast<const float*>(y)[i];
@@ -208,16 +297,24 @@ __device__ __forceinline__ float value(const void* y, int type, long long i) {
   return __bfloat162float(static_cast<const __nv_bfloat16*>(y)[i]);
 }
 
-// A thread sums a token's column; neighbouring threads, neighbouring columns.
-__global__ void __launch_bounds__(256) combine_kernel(const CombineParams p) {
+// The same where columns, row lengths or pointers are not multiples of 8 values: one column a thread.
+__global__ void __launch_bounds__(256) combine_odd_kernel(const CombineParams p) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   const long long t = i / p.C;
   const int c = (int)(i - t * p.C);
   if (t >= p.T) return;
   float s = 0.f;
-  for (int j = 0; j < p.k; ++j) {
-    const int slot = p.slots[t * p.k + j];
-    if (slot >= 0 && slot < p.y_rows) s = fmaf(p.weights[t * p.k + j], value(p.y, p.y_type, slot * p.ld_y + c), s);
+  for (int j0 = 0; j0 < p.k; j0 += 4) {
+    float v[4], w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int slot = j0 + j < p.k ? p.slots[t * p.k + j0 + j] : -1;
+      const bool there = slot >= 0 && slot < p.y_rows;
+      w[j] = there ? p.weights[t * p.k + j0 + j] : 0.f;
+      v[j] = there ? value(p.y, p.y_type, slot * p.ld_y + c) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = fmaf(w[j], v[j], s);
   }
   store_out(p.out, p.out_type, t * p.ld_out + c, s);
 }
@@ -248,8 +345,14 @@ cudaError_t route_forward(const RouteCall& c, int* launched) {
 }
 
 cudaError_t combine_forward(const CombineCall& c, int* launched) {
-  const CombineParams p{c.y, c.slots, c.weights, c.out, c.ld_y, c.ld_out, c.y_type, c.y_rows, c.T, c.k, c.C, c.out_type};
-  combine_kernel<<<(unsigned)(((long long)c.T * c.C + 255) / 256), 256, 0, c.stream>>>(p);
+  CombineParams p{c.y, c.slots, c.weights, c.out, c.ld_y, c.ld_out, c.y_type, c.y_rows, c.T, c.k, c.C, c.out_type, c.C / 8};
+  const bool eights = c.C % 8 == 0 && c.ld_y % 8 == 0 && c.ld_out % 8 == 0 && (((uintptr_t)c.y | (uintptr_t)c.out) & 15) == 0;
+  const long long blocks = ((long long)c.T * (eights ? p.groups : c.C) + 255) / 256;
+  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  if (!eights) combine_odd_kernel<<<(unsigned)blocks, 256, 0, c.stream>>>(p);
+  else if (c.y_type == SNN_OUT_F32) combine_kernel<float><<<(unsigned)blocks, 256, 0, c.stream>>>(p);
+  else if (c.y_type == SNN_OUT_F16) combine_kernel<F16><<<(unsigned)blocks, 256, 0, c.stream>>>(p);
+  else combine_kernel<BF16><<<(unsigned)blocks, 256, 0, c.stream>>>(p);
   *launched += 1;
   return cudaGetLastError();
 }
