@@ -139,6 +139,7 @@ class _PythonChecks:
         return -1
 
     group_forward = stack_forward = static_forward = layer_forward
+    experts_forward = adapters_forward = route = combine = layer_forward
 
 
 def _load_fast():
@@ -153,6 +154,9 @@ def _load_fast():
                 raise ImportError(f"_snn_fast was built for torch {module.TORCH_VERSION}, not {torch.__version__}")
             module.bind(*(ctypes.cast(f, ctypes.c_void_p).value
                           for f in (lib.snn_conv_forward, lib.snn_conv_group_forward, lib.snn_conv_stack_forward)))
+            module.bind_projections(*(ctypes.cast(f, ctypes.c_void_p).value
+                                      for f in (lib.snn_conv_experts_forward, lib.snn_conv_adapters_forward, lib.snn_conv_experts_route,
+                                                lib.snn_conv_experts_combine, lib.snn_conv_experts_route_work)))
             module.bind_static(ctypes.cast(lib.snn_conv_forward_static, ctypes.c_void_p).value, np.ndarray)
         except (ImportError, AttributeError) as e:   # (AttributeError: a module built from older source)
             warnings.warn(f"the forward calls are checked in Python, which takes longer: {e} "

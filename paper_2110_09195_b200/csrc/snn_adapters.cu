@@ -2,6 +2,7 @@
 #include "snn_products.h"
 
 #include "snn_products.cuh"
+#include "snn_tc_common.cuh"
 
 namespace snn {
 namespace {
@@ -26,6 +27,8 @@ __global__ void __launch_bounds__(256) shrink_kernel(const ShrinkParams p) {
   __shared__ int who[N];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int r0 = (int)blockIdx.x * p.per_cta, n = min(p.per_cta, p.rows - r0), j0 = (int)blockIdx.y * M;
+  grid_dep_wait();
+  grid_dep_launch();   // (the projection's kernel begins with its own sums; it waits for these before it adds them)
   if (threadIdx.x < N) {
     const int a = (int)threadIdx.x < n ? p.adapter[r0 + threadIdx.x] : -1;
     who[threadIdx.x] = a >= 0 && a < p.n ? a : -1;
@@ -91,31 +94,28 @@ __global__ void __launch_bounds__(256) shrink_kernel(const ShrinkParams p) {
 }
 
 template <class T, int NT, int MT, int U>
-void shrink_launch(const ShrinkParams& p, cudaStream_t s) {
-  shrink_kernel<T, NT, MT, U><<<dim3((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT))), 256, 0, s>>>(p);
+cudaError_t shrink_launch(const ShrinkParams& p, cudaStream_t s) {
+  const dim3 grid((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT)));
+  return launch_dependent(shrink_kernel<T, NT, MT, U>, grid, 256, 0, s, p);
 }
 
 template <class T>
-void shrink_type(ShrinkParams p, cudaStream_t s) {
+cudaError_t shrink_type(ShrinkParams p, cudaStream_t s) {
   const int sms = sm_count();
   if (p.rows >= 16 * sms) {
     p.per_cta = 16;
-    if (p.rank > 16) shrink_launch<T, 2, 2, 2>(p, s);
-    else shrink_launch<T, 2, 1, 2>(p, s);
-  } else {
-    p.per_cta = max(1, min(8, p.rows / sms));
-    shrink_launch<T, 1, 1, 4>(p, s);
+    return p.rank > 16 ? shrink_launch<T, 2, 2, 2>(p, s) : shrink_launch<T, 2, 1, 2>(p, s);
   }
+  p.per_cta = max(1, min(8, p.rows / sms));
+  return shrink_launch<T, 1, 1, 4>(p, s);
 }
 
 }  // namespace
 
 cudaError_t shrink_forward(const ShrinkCall& c, int* launched) {
   const ShrinkParams p{static_cast<const uint16_t*>(c.act), static_cast<const uint16_t*>(c.a), c.adapter, c.scale, c.h, c.ld_act, c.rows, c.C, c.n, c.rank, 8};
-  if (c.act_type == SNN_ACT_F16) shrink_type<F16>(p, c.stream);
-  else shrink_type<BF16>(p, c.stream);
   *launched += 1;
-  return cudaGetLastError();
+  return c.act_type == SNN_ACT_F16 ? shrink_type<F16>(p, c.stream) : shrink_type<BF16>(p, c.stream);
 }
 
 }  // namespace snn

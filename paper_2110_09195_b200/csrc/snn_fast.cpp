@@ -9,6 +9,7 @@
 // takes the GPU 9.2.
 #include <Python.h>
 
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -216,6 +217,169 @@ PyObject* static_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- projections.  Matrices have dense rows, any distance apart that the library takes; all else is contiguous.
+using ExpertsForward = snn_status_t (*)(snn_conv_experts_t*, const void*, int32_t, int32_t, int64_t, const int32_t*, const int32_t*, int32_t, void*, int32_t,
+                                        int64_t, void*);
+using Route = snn_status_t (*)(const void*, int32_t, int32_t, int32_t, int64_t, int32_t, int32_t, int32_t*, float*, int32_t*, int32_t*, int32_t*, void*, int32_t,
+                               void*);
+using Combine = snn_status_t (*)(const void*, int32_t, int32_t, int64_t, const int32_t*, const float*, int32_t, int32_t, int32_t, void*, int32_t, int64_t, int32_t,
+                                 void*);
+using AdaptersForward = snn_status_t (*)(snn_conv_adapters_t*, const void*, int32_t, int32_t, int64_t, const int32_t*, const void*, const void*, const float*,
+                                         int32_t, int32_t, float*, void*, int32_t, int64_t, void*);
+using RouteWork = int64_t (*)(int32_t, int32_t);
+ExpertsForward g_experts = nullptr;
+Route g_route = nullptr;
+Combine g_combine = nullptr;
+AdaptersForward g_adapters = nullptr;
+RouteWork g_route_work = nullptr;
+
+// What projections.py packs for a handle ("=Q4i").
+struct Projection {
+  uint64_t handle;
+  int32_t device, count, c_in, c_out;
+};
+const at::Tensor* on_device(PyObject* o, int device) {   // (device below 0: any)
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || (device >= 0 && t.get_device() != device) || t.is_neg() || t.is_conj()) return nullptr;
+  return &t;
+}
+struct Matrix {
+  const at::Tensor* t = nullptr;
+  int64_t rows = 0, columns = 0, ld = 0;
+  int32_t type = -1;   // SNN_OUT_*
+  bool take(PyObject* o, int device) {
+    t = on_device(o, device);
+    if (!t || t->dim() != 2) return false;
+    rows = t->size(0);
+    columns = t->size(1);
+    ld = rows > 1 ? t->stride(0) : (columns + 7) / 8 * 8;
+    if ((columns > 1 && t->stride(1) != 1) || ld < columns || rows > INT32_MAX || columns > INT32_MAX) return false;
+    const at::ScalarType s = t->scalar_type();
+    type = s == at::kFloat ? SNN_OUT_F32 : s == at::kHalf ? SNN_OUT_F16 : s == at::kBFloat16 ? SNN_OUT_BF16 : -1;
+    return type >= 0;
+  }
+  int32_t act_type() const { return type == SNN_OUT_F16 ? SNN_ACT_F16 : type == SNN_OUT_BF16 ? SNN_ACT_BF16 : -1; }
+};
+const at::Tensor* dense(PyObject* o, int device, at::ScalarType type, std::initializer_list<int64_t> shape) {
+  const at::Tensor* t = on_device(o, device);
+  if (!t || t->scalar_type() != type || !t->is_contiguous() || !(t->sizes() == at::IntArrayRef(shape.begin(), shape.size()))) return nullptr;
+  return t;
+}
+
+// experts_forward(description, x, offsets, rows or None, out)
+PyObject* experts_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    const Projection* d = n == 5 ? described<Projection>(a[0], sizeof(Projection)) : nullptr;
+    Matrix x, y;
+    if (!d || !d->handle || !g_experts || !x.take(a[1], d->device) || !y.take(a[4], d->device) || x.act_type() < 0 || x.columns != d->c_in || y.columns != d->c_out)
+      return kUnusual;
+    const at::Tensor* offsets = dense(a[2], d->device, at::kInt, {d->count + 1});
+    const at::Tensor* rows = a[3] == Py_None ? nullptr : dense(a[3], d->device, at::kInt, {y.rows});
+    if (!offsets || (!rows && a[3] != Py_None)) return kUnusual;
+    const void* const act = x.t->data_ptr();
+    void* const out = y.t->data_ptr();
+    const int32_t *off = offsets->data_ptr<int32_t>(), *index = rows ? rows->data_ptr<int32_t>() : nullptr;
+    void* const stream = current_stream(d->device);
+    return unlocked([&] {
+      return g_experts(reinterpret_cast<snn_conv_experts_t*>(d->handle), act, x.act_type(), (int32_t)x.rows, x.ld, index, off, (int32_t)y.rows, out, y.type, y.ld,
+                       stream);
+    });
+  });
+}
+
+// adapters_forward(description, x, adapter, a, b, scale, out)
+PyObject* adapters_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    const Projection* d = n == 7 ? described<Projection>(a[0], sizeof(Projection)) : nullptr;
+    Matrix x, y;
+    if (!d || !d->handle || !g_adapters || !x.take(a[1], d->device) || !y.take(a[6], d->device) || x.act_type() < 0 || x.columns != d->c_in ||
+        y.columns != d->c_out || y.rows != x.rows)
+      return kUnusual;
+    const at::Tensor* first = on_device(a[3], d->device);
+    if (!first || first->dim() != 3) return kUnusual;
+    const int64_t count = first->size(0), rank = first->size(1);
+    const at::ScalarType type = x.t->scalar_type();
+    first = dense(a[3], d->device, type, {count, rank, d->c_in});
+    const at::Tensor *second = dense(a[4], d->device, type, {count, d->c_out, rank}), *scale = dense(a[5], d->device, at::kFloat, {count});
+    const at::Tensor* adapter = dense(a[2], d->device, at::kInt, {x.rows});
+    if (!first || !second || !scale || !adapter || count > INT32_MAX || rank > SNN_ADAPTERS_RANK_MAX || c10::cuda::current_device() != d->device) return kUnusual;
+    void* const stream = current_stream(d->device);
+    const c10::DataPtr work = c10::cuda::CUDACachingAllocator::get()->allocate((size_t)(x.rows * rank) * 4);   // (of the current stream)
+    const void *act = x.t->data_ptr(), *pa = first->data_ptr(), *pb = second->data_ptr();
+    const float* const ps = scale->data_ptr<float>();
+    const int32_t* const pi = adapter->data_ptr<int32_t>();
+    void* const out = y.t->data_ptr();
+    return unlocked([&] {
+      return g_adapters(reinterpret_cast<snn_conv_adapters_t*>(d->handle), act, x.act_type(), (int32_t)x.rows, x.ld, pi, pa, pb, ps, (int32_t)count, (int32_t)rank,
+                        static_cast<float*>(work.get()), out, y.type, y.ld, stream);
+    });
+  });
+}
+
+// route(logits, top_k, normalise, ids, weights, offsets, rows, slots, work)
+PyObject* route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Matrix x;
+    int32_t k = 0;
+    if (n != 9 || !g_route || !x.take(a[0], -1) || !int_between(a[1], 1, SNN_ROUTE_TOP_MAX, &k) || !PyBool_Check(a[2])) return kUnusual;
+    const int device = x.t->get_device();
+    const at::Tensor *ids = dense(a[3], device, at::kInt, {x.rows, k}), *weights = dense(a[4], device, at::kFloat, {x.rows, k});
+    const at::Tensor *offsets = dense(a[5], device, at::kInt, {x.columns + 1}), *rows = dense(a[6], device, at::kInt, {x.rows * k});
+    const at::Tensor *slots = dense(a[7], device, at::kInt, {x.rows, k}), *work = on_device(a[8], device);
+    if (!ids || !weights || !offsets || !rows || !slots || !work || work->scalar_type() != at::kInt || work->dim() != 1 || !work->is_contiguous() ||
+        work->numel() * 4 < g_route_work((int32_t)x.rows, (int32_t)x.columns))
+      return kUnusual;
+    void* const stream = current_stream(device);
+    const void* const logits = x.t->data_ptr();
+    return unlocked([&] {
+      return g_route(logits, x.type, (int32_t)x.rows, (int32_t)x.columns, x.ld, k, a[2] == Py_True, ids->data_ptr<int32_t>(), weights->data_ptr<float>(),
+                     offsets->data_ptr<int32_t>(), rows->data_ptr<int32_t>(), slots->data_ptr<int32_t>(), work->data_ptr(), device, stream);
+    });
+  });
+}
+
+// combine(y, slots, weights, out)
+PyObject* combine(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Matrix y, out;
+    if (n != 4 || !g_combine || !y.take(a[0], -1)) return kUnusual;
+    const int device = y.t->get_device();
+    const at::Tensor* slots = on_device(a[1], device);
+    if (!slots || slots->dim() != 2 || !out.take(a[3], device)) return kUnusual;
+    const int64_t t = slots->size(0), k = slots->size(1);
+    slots = dense(a[1], device, at::kInt, {t, k});
+    const at::Tensor* weights = dense(a[2], device, at::kFloat, {t, k});
+    if (!slots || !weights || out.rows != t || out.columns != y.columns || k > SNN_ROUTE_TOP_MAX) return kUnusual;
+    void* const stream = current_stream(device);
+    const void* const from = y.t->data_ptr();
+    void* const to = out.t->data_ptr();
+    return unlocked([&] {
+      return g_combine(from, y.type, (int32_t)y.rows, y.ld, slots->data_ptr<int32_t>(), weights->data_ptr<float>(), (int32_t)t, (int32_t)k, (int32_t)y.columns, to,
+                       out.type, out.ld, device, stream);
+    });
+  });
+}
+
+// bind_projections(experts, adapters, route, combine, route_work): addresses of the library's entry points
+PyObject* bind_projections(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "bind_projections takes five addresses");
+    return nullptr;
+  }
+  void* p[5];
+  for (int i = 0; i < 5; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i] && PyErr_Occurred()) return nullptr;
+  }
+  g_experts = reinterpret_cast<ExpertsForward>(p[0]);
+  g_adapters = reinterpret_cast<AdaptersForward>(p[1]);
+  g_route = reinterpret_cast<Route>(p[2]);
+  g_combine = reinterpret_cast<Combine>(p[3]);
+  g_route_work = reinterpret_cast<RouteWork>(p[4]);
+  Py_RETURN_NONE;
+}
+
 // bind_static(address of the library's entry point, numpy.ndarray)
 PyObject* bind_static(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 2 || !PyType_Check(a[1])) {
@@ -252,6 +416,11 @@ PyMethodDef methods[] = {
     {"group_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(group_forward)), METH_FASTCALL, nullptr},
     {"stack_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(stack_forward)), METH_FASTCALL, nullptr},
     {"static_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(static_forward)), METH_FASTCALL, nullptr},
+    {"experts_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(experts_forward)), METH_FASTCALL, nullptr},
+    {"adapters_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(adapters_forward)), METH_FASTCALL, nullptr},
+    {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(route)), METH_FASTCALL, nullptr},
+    {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(combine)), METH_FASTCALL, nullptr},
+    {"bind_projections", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_projections)), METH_FASTCALL, nullptr},
     {"bind_static", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_static)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -2,6 +2,7 @@
 #include "snn_products.h"
 
 #include "snn_products.cuh"
+#include "snn_tc_common.cuh"
 
 namespace snn {
 namespace {
@@ -40,39 +41,50 @@ struct SmallParams {
   long long ld_act, ld_out;
   int act_rows, max_rows, E, C, K, n_mt, n_kb, out_type, k_warps;
   Lowrank low;
+  Powers pow;
 };
 
-// The chunk-th piece of at most `most` rows, counted over the experts in their order: expert, first row, rows.  Found by each warp for
-// itself: every lane counts the pieces of a run of experts, a scan over the lanes says whose run holds it.
-__device__ __forceinline__ bool find_chunk(const int32_t* offsets, int E, int R, int most, int chunk, int* e_out, int* r_out, int* n_out) {
-  const int lane = threadIdx.x & 31;
-  if (!offsets) {
-    *e_out = 0;
-    *r_out = chunk * most;
-    *n_out = min(most, R - chunk * most);
-    return *n_out > 0;
-  }
-  const int per = (E + 31) >> 5, e0 = lane * per, e1 = min(E, e0 + per);
-  int count = 0;
-  for (int e = e0; e < e1; ++e) {
-    const int lo = clamp_offset(offsets[e], R), hi = clamp_offset(offsets[e + 1], R);
-    count += (max(hi - lo, 0) + most - 1) / most;
-  }
-  int upto = count;
+// Pieces of at most `most` rows of an expert, counted over the experts in their order, by each warp for itself: every lane counts the
+// pieces of a run of experts, and a scan over the lanes says whose run a piece is in.
+struct Pieces {
+  int upto, count, total;   // this lane's, and of all
+};
+__device__ __forceinline__ int pieces_of(const int32_t* offsets, int e, int R, int most, int* lo_out, int* hi_out) {
+  const int lo = clamp_offset(offsets[e], R), hi = clamp_offset(offsets[e + 1], R);
+  *lo_out = lo;
+  *hi_out = hi;
+  return (max(hi - lo, 0) + most - 1) / most;
+}
+__device__ __forceinline__ Pieces count_pieces(const int32_t* offsets, int E, int R, int most) {
+  if (!offsets) return Pieces{0, 0, (R + most - 1) / most};
+  const int lane = threadIdx.x & 31, per = (E + 31) >> 5, e0 = lane * per, e1 = min(E, e0 + per);
+  Pieces r{0, 0, 0};
+  int lo, hi;
+  for (int e = e0; e < e1; ++e) r.count += pieces_of(offsets, e, R, most, &lo, &hi);
+  r.upto = r.count;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, upto, d);
-    if (lane >= d) upto += v;
+    const int v = __shfl_up_sync(0xffffffffu, r.upto, d);
+    if (lane >= d) r.upto += v;
   }
-  const unsigned who = __ballot_sync(0xffffffffu, chunk < upto);
-  if (!who) return false;
-  const int src = __ffs(who) - 1;
+  r.total = __shfl_sync(0xffffffffu, r.upto, 31);
+  return r;
+}
+// Expert, first row and rows of a piece below the total.
+__device__ __forceinline__ void find_piece(const Pieces& all, const int32_t* offsets, int E, int R, int most, int piece, int* e_out, int* r_out, int* n_out) {
+  if (!offsets) {
+    *e_out = 0;
+    *r_out = piece * most;
+    *n_out = min(most, R - piece * most);
+    return;
+  }
+  const int lane = threadIdx.x & 31, per = (E + 31) >> 5, e0 = lane * per, e1 = min(E, e0 + per);
+  const int src = __ffs(__ballot_sync(0xffffffffu, piece < all.upto)) - 1;
   int e = 0, r = 0, n = 0;
   if (lane == src) {
-    int left = chunk - (upto - count);
+    int left = piece - (all.upto - all.count), lo, hi;
     for (e = e0; e < e1; ++e) {
-      const int lo = clamp_offset(offsets[e], R), hi = clamp_offset(offsets[e + 1], R);
-      const int pieces = (max(hi - lo, 0) + most - 1) / most;
+      const int pieces = pieces_of(offsets, e, R, most, &lo, &hi);
       if (left < pieces) {
         r = lo + left * most;
         n = min(most, hi - r);
@@ -84,108 +96,151 @@ __device__ __forceinline__ bool find_chunk(const int32_t* offsets, int E, int R,
   *e_out = __shfl_sync(0xffffffffu, e, src);
   *r_out = __shfl_sync(0xffffffffu, r, src);
   *n_out = __shfl_sync(0xffffffffu, n, src);
-  return true;
 }
 
-// A warp computes 32 output channels times 8 NT rows over a share of the input channels: the weights, the M operand, are expanded from
+// A warp computes 32 MP output channels times 8 rows over a share of the input channels: the weights, the M operand, are expanded from
 // bits in registers, the rows, the N operand, come straight from memory as the instruction wants them (a lane's 16 neighbouring
-// channels are four steps' operands).  The warps of a CTA take different input channels (k_warps of them) and different output
-// channels; the former's sums meet in shared memory.
-template <class T, int NT>
-__global__ void __launch_bounds__(256) products_small_kernel(const SmallParams p) {
-  constexpr int N = 8 * NT;
-  __shared__ float red[8][N][33];
+// channels are four steps' operands) and stay in registers for all of the warp's output channels (loaded for every 32 of them, they took
+// as many cycles of the L1 cache as the rest).  The warps of a CTA take different input channels (k_warps of them) and different output
+// channels; the former's sums meet in shared memory.  The work, pieces of rows times strips of output channels, is counted on the device and
+// shared out evenly: a CTA has a run of strips, mostly of one piece.  Bound by latency where there are few weights, else by the
+// expansion: 16 masks and 15 multiplications, at half rate each, for four of the instructions (64 tokens over 64 experts of 2048 x 2048, 4
+// each: half of the issue slots used).  16 rows a warp were no faster for any number of rows (16 experts of 4096 x 4096, 128 rows: 47 us
+// against 41, 256 rows: 76 against 65).
+constexpr int SM_N = 8;
+template <class T, int MP>
+__global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParams p) {
+  constexpr int M = 32 * MP;
+  __shared__ float red_both[2][8][SM_N][M + 1];
+  int turn = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int kw = warp % p.k_warps, mw = warp / p.k_warps, m_warps = 8 / p.k_warps;
-  int e, r0, n;
-  if (!find_chunk(p.offsets, p.E, p.max_rows, N, (int)blockIdx.x, &e, &r0, &n)) return;
-  const uint16_t* x[NT];
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int c = 8 * i + g;
-    x[i] = nullptr;
-    if (c < n) {
-      const int row = p.rows ? p.rows[r0 + c] : r0 + c;
-      if (row >= 0 && row < p.act_rows) x[i] = static_cast<const uint16_t*>(p.act) + (size_t)row * (size_t)p.ld_act;
+  const int kw = warp % p.k_warps, mw = warp / p.k_warps, m_warps = 8 / p.k_warps, n_groups = (p.K + M * m_warps - 1) / (M * m_warps);
+  // The kernel before may be the one that writes A x: it has waited for what came before it, and so for the rows and all else that is read
+  // or overwritten here.  Else this waits for whatever came before.
+  if (!p.low.adapter) grid_dep_wait();
+  const Pieces pieces = count_pieces(p.offsets, p.E, p.max_rows, SM_N);
+  const long long items = (long long)pieces.total * n_groups;
+  long long item = items * blockIdx.x / gridDim.x;
+  const long long last = items * (blockIdx.x + 1) / gridDim.x;
+  bool waited = !p.low.adapter;
+  grid_dep_launch();
+  while (item < last) {
+    const int piece = (int)(item / n_groups), group0 = (int)(item - (long long)piece * n_groups);
+    const int group1 = (int)min((long long)n_groups, group0 + (last - item));
+    item += group1 - group0;
+    int e, r0, n;
+    find_piece(pieces, p.offsets, p.E, p.max_rows, SM_N, piece, &e, &r0, &n);
+    const uint16_t* x = nullptr;
+    if (g < n) {
+      const int row = p.rows ? p.rows[r0 + g] : r0 + g;
+      if (row >= 0 && row < p.act_rows) x = static_cast<const uint16_t*>(p.act) + (size_t)row * (size_t)p.ld_act + 16 * t;
     }
-  }
-  const int mt = 2 * ((int)blockIdx.y * m_warps + mw);
-  float acc[2][NT][4] = {};
-  if (mt < p.n_mt) {
-    const uint2* w0 = reinterpret_cast<const uint2*>(p.bits) + ((size_t)(e * p.n_mt + mt) * p.n_kb) * 64 + 8 * g + t;
-    const uint2* w1 = w0 + (size_t)p.n_kb * 64;
-    for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
-      const uint2 ue = ld8(w0 + (size_t)kb * 64), uo = ld8(w0 + (size_t)kb * 64 + 4);
-      const uint2 ve = ld8(w1 + (size_t)kb * 64), vo = ld8(w1 + (size_t)kb * 64 + 4);
-      const uint32_t ua[4] = {ue.x, uo.x, ue.y, uo.y}, ub[4] = {ve.x, vo.x, ve.y, vo.y};
+    for (int group = group0; group < group1; ++group) {
+      // (tiles behind the last: the sums of the last pair there is, which nobody writes)
+      const int mt0 = 2 * MP * (group * m_warps + mw);
+      const uint2* const bits = reinterpret_cast<const uint2*>(p.bits) + (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
+      uint2 w[2][2];   // [tile][odd blocks of 64]
+      auto load_bits = [&](int pair, int kb) {
+        const int mt = min(mt0 + 2 * pair, p.n_mt - 2);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int c = kb * 256 + j * 64 + t * 16;
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint4 b[NT];
+          for (int o = 0; o < 2; ++o) w[m][o] = ld8(bits + ((size_t)(mt + m) * p.n_kb + kb) * 64 + 4 * o);
+      };
+      float acc[2 * MP][4] = {};
+      load_bits(0, kw);
+      for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
+        uint4 b[4][2];
 #pragma unroll
-          for (int i = 0; i < NT; ++i) b[i] = x[i] && c + 8 * h < p.C ? ld16(x[i] + c + 8 * h) : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int s = 2 * h + q;
-            const uint32_t a0 = plus_minus<T>(ua[j], 15 - 2 * s), a2 = plus_minus<T>(ua[j], 14 - 2 * s);
-            const uint32_t a1 = plus_minus<T>(ua[j], 7 - 2 * s), a3 = plus_minus<T>(ua[j], 6 - 2 * s);
-            const uint32_t c0 = plus_minus<T>(ub[j], 15 - 2 * s), c2 = plus_minus<T>(ub[j], 14 - 2 * s);
-            const uint32_t c1 = plus_minus<T>(ub[j], 7 - 2 * s), c3 = plus_minus<T>(ub[j], 6 - 2 * s);
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-              const uint32_t b0 = q ? b[i].z : b[i].x, b1 = q ? b[i].w : b[i].y;
-              mma_16x8<T>(acc[0][i], a0, a1, a2, a3, b0, b1);
-              mma_16x8<T>(acc[1][i], c0, c1, c2, c3, b0, b1);
-            }
+          for (int h = 0; h < 2; ++h) {
+            const int c = kb * 256 + j * 64 + 8 * h;
+            b[j][h] = x && c + 16 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
           }
+#pragma unroll
+        for (int pair = 0; pair < MP; ++pair) {
+          const uint32_t u[2][4] = {{w[0][0].x, w[0][1].x, w[0][0].y, w[0][1].y}, {w[1][0].x, w[1][1].x, w[1][0].y, w[1][1].y}};
+          if (pair + 1 < MP) load_bits(pair + 1, kb);
+          else if (kb + p.k_warps < p.n_kb) load_bits(0, kb + p.k_warps);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+              const uint4& v = b[j][s >> 1];
+#pragma unroll
+              for (int m = 0; m < 2; ++m) {
+                const uint32_t a0 = plus_minus<T>(u[m][j], 15 - 2 * s, p.pow), a1 = plus_minus<T>(u[m][j], 7 - 2 * s, p.pow);
+                const uint32_t a2 = plus_minus<T>(u[m][j], 14 - 2 * s, p.pow), a3 = plus_minus<T>(u[m][j], 6 - 2 * s, p.pow);
+                mma_16x8<T>(acc[2 * pair + m], a0, a1, a2, a3, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
+              }
+            }
         }
+      }
+      float (*const red)[SM_N][M + 1] = red_both[turn];
+      turn ^= 1;
+#pragma unroll
+      for (int m = 0; m < 2 * MP; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) red[warp][2 * t + (q & 1)][16 * m + g + 8 * (q >> 1)] = acc[m][q];
+      __syncthreads();   // (the other half of the buffer is for the next strip)
+      if (!waited) grid_dep_wait();
+      waited = true;
+      const int width = M * m_warps, first = group * width;
+      for (int i = threadIdx.x; i < n * width; i += 256) {
+        const int c = i / width, m = i % width, co = first + m;
+        if (co >= p.K) continue;
+        float s = 0.f;
+        for (int k = 0; k < p.k_warps; ++k) s += red[(m / M) * p.k_warps + k][c][m % M];
+        float v = p.alpha[(size_t)e * p.n_mt * 16 + co] * s;
+        if (p.low.adapter) v += lowrank_term<T>(p.low, p.K, r0 + c, co);
+        store_out(p.out, p.out_type, (long long)(r0 + c) * p.ld_out + co, v);
       }
     }
   }
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) red[warp][8 * i + 2 * t + (q & 1)][16 * m + g + 8 * (q >> 1)] = acc[m][i][q];
-  __syncthreads();
-  const int width = 32 * m_warps, first = (int)blockIdx.y * width;
-  for (int i = threadIdx.x; i < n * width; i += 256) {
-    const int c = i / width, m = i % width, co = first + m;
-    if (co >= p.K) continue;
-    float s = 0.f;
-    for (int k = 0; k < p.k_warps; ++k) s += red[(m >> 5) * p.k_warps + k][c][m & 31];
-    float v = p.alpha[(size_t)e * p.n_mt * 16 + co] * s;
-    if (p.low.adapter) v += lowrank_term<T>(p.low, p.K, r0 + c, co);
-    store_out(p.out, p.out_type, (long long)(r0 + c) * p.ld_out + co, v);
-  }
+  if (!waited) grid_dep_wait();   // (no CTA ends before what came before has)
 }
 
-template <class T, int NT>
+// Pieces of 8 rows that the experts have at most (the host does not know how the rows are spread).
+long long most_pieces(const Products& p, const ProductCall& c) {
+  return c.offsets ? ((long long)c.max_rows + (long long)min(p.E, c.max_rows) * (SM_N - 1)) / SM_N : (c.max_rows + SM_N - 1) / SM_N;
+}
+
+template <class T, int MP>
 cudaError_t small_launch(const Products& p, const ProductCall& c, int* launched) {
   SmallParams q{p.bits, p.alpha, c.act, c.rows, c.offsets, c.out, c.ld_act, c.ld_out, c.act_rows, c.max_rows, p.E, p.C, p.K, p.n_mt, p.n_kb,
-                c.out_type, 1, c.low};
-  const int most = 8 * NT;
-  const long long chunks = c.offsets ? ((long long)c.max_rows + (long long)min(p.E, c.max_rows) * (most - 1)) / most : (c.max_rows + most - 1) / most;
-  // all warps on one strip of output channels until that gives every SM a CTA or the input channels are used up
-  const int strips = (p.K + 31) / 32;
-  int k_warps = 8;
-  while (k_warps > 1 && (k_warps > p.n_kb || chunks * ((strips + 16 / k_warps - 1) / (16 / k_warps)) >= 4ll * sm_count())) k_warps /= 2;
-  q.k_warps = k_warps;
-  const int m_warps = 8 / k_warps;
-  products_small_kernel<T, NT><<<dim3((unsigned)chunks, (unsigned)((strips + m_warps - 1) / m_warps)), 256, 0, c.stream>>>(q);
+                c.out_type, 8, c.low, powers()};
+  // all warps on one strip of output channels, unless there are not so many blocks of 256 input channels: small pieces of work
+  while (q.k_warps > p.n_kb) q.k_warps /= 2;
+  const int width = 32 * MP * (8 / q.k_warps);
   *launched += 1;
-  return cudaGetLastError();
+  return launch_dependent(products_small_kernel<T, MP>, (unsigned)min(2ll * sm_count(), most_pieces(p, c) * ((p.K + width - 1) / width)), 256, 0, c.stream, q);
 }
 
 template <class T>
 cudaError_t small_forward(const Products& p, const ProductCall& c, int* launched) {
-  const int per_expert = c.offsets ? c.max_rows / max(1, min(p.E, c.max_rows)) : c.max_rows;
-  if (per_expert <= 6) return small_launch<T, 1>(p, c, launched);
-  if (per_expert <= 12) return small_launch<T, 2>(p, c, launched);
-  return small_launch<T, 4>(p, c, launched);
+  // 64 output channels a warp where that leaves work for the SMs (one token over an expert of 4096 x 4096: 5.6 us with 32, 6.6 with 64; 32
+  // tokens 11.4 and 9.8; 64 tokens over 64 experts of 2048 x 2048 39 and 33)
+  if (2 * most_pieces(p, c) * (p.K / 64) >= 3ll * sm_count()) return small_launch<T, 2>(p, c, launched);
+  return small_launch<T, 1>(p, c, launched);
+}
+
+// Which kernel, by the time that each would take on 148 SMs (us).  Few rows: each piece of 8 expands all of its expert's weights, 11 G
+// weights a ms.  Many rows: tiles of 256 output channels in turns of a tile for each pair of SMs, 0.16 to 0.24 us for 64 input channels,
+// whatever the number of rows up to 192.  (Measured both ways: one expert of 4096 x 4096, 32 rows 9.8 and 15.6 us, 64 rows 15 and 16; 16
+// of them, 128 rows 41 and 51, 256 rows 65 and 51; 64 of 2048 x 2048, 512 rows 48 and 53, 1024 rows 78 and 54.  With adapters of rank 16, one of
+// 4096 x 4096 and requests of 50 rows, 64 rows 22 and 23, 256 rows 56 and 31; with an adapter for each row 22 and 40, 56 and 71.)
+bool many_rows(const Products& p, const ProductCall& c) {
+  if (c.act_rows < 1) return false;
+  const double pairs = sm_count() / 2.0, used = c.offsets ? min(p.E, c.max_rows) : 1, blocks = (p.C + 63) / 64, rows = fmin(192.0, c.max_rows / used);
+  double few = 3.0 + (c.max_rows / 8.0 + (c.offsets ? 0.5 * used : 0.5)) * p.K * (double)p.C / 11e6;
+  const double tiles = (c.max_rows < 192 * used ? used : c.max_rows / 192.0) * ((p.K + 255) / 256);
+  double many = 5.5 + blocks * (tiles <= pairs ? 0.16 + 0.0002 * rows : tiles / pairs * (0.2 + 0.0002 * rows));
+  if (c.low.adapter) {
+    few += 0.02 * c.max_rows;
+    many += 6.0 + 0.04 * rows;
+  }
+  return many < few;
 }
 
 }  // namespace
@@ -222,8 +277,7 @@ void products_destroy(Products* p) {
 }
 
 cudaError_t products_forward(const Products& p, const ProductCall& c, int* launched) {
-  const int per_expert = c.offsets ? c.max_rows / max(1, min(p.E, c.max_rows)) : c.max_rows;
-  if (per_expert >= 48 && c.act_rows > 0) return products_tall(p, c, launched);
+  if (many_rows(p, c)) return products_tall(p, c, launched);
   return c.act_type == SNN_ACT_F16 ? small_forward<F16>(p, c, launched) : small_forward<BF16>(p, c, launched);
 }
 

@@ -55,6 +55,7 @@ struct TallParams {
   int act_rows, max_rows, E, C, K, n_mt, n_kb, out_type, n_cp;
   int* status;
   Lowrank low;
+  Powers pow;
 };
 
 struct TallBars {
@@ -293,7 +294,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
   const int warp = uni(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t b_smem = smem_u32(smem);
   const int rank = (int)(blockIdx.x & 1), first_tile = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
+  // As in the kernel for few rows: after the one that writes A x, only the warps that read it wait.
   if (warp == 0) {
+    if (!RANK) grid_dep_wait();
     // tiles of each expert, summed up: every lane a run of experts
     const int per = (p.E + 31) >> 5, e0 = lane * per, e1 = min(p.E, e0 + per);
     int count = 0;
@@ -329,13 +332,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   } else if (warp == 2) {
+    // (not before the kernel before has ended: it may still have to get tensor memory of its own)
+    if (!RANK) grid_dep_wait();
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars->tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  if (!RANK || warp >= 12) grid_dep_wait();
   tc_fence_before();
   __syncthreads();
   pair_sync();
   tc_fence_after();
+  grid_dep_launch();   // (only now: a dependent that has tensor memory before this pair does would wait for it for good)
   const uint32_t tmem = bars->tmem;
   const int nk = (p.C + 63) >> 6;
   bool ok = true;
@@ -477,7 +484,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[8 * q + j] = plus_minus<T>(w[i][q], 15 - j);
+            for (int j = 0; j < 8; ++j) v[8 * q + j] = plus_minus<T>(w[i][q], 15 - j, p.pow);
           if (stored != ~0u) {
             tmem_st_wait();
             tc_fence_before();
@@ -643,12 +650,12 @@ cudaError_t tall_launch(const Products& p, const ProductCall& c, const CUtensorM
   cudaError_t e = allow_max_smem(products_tall_kernel<T, GATHER, RANK>, &done);
   if (e != cudaSuccess) return e;
   const TallParams q{p.bits, p.alpha, static_cast<const uint16_t*>(c.act), c.rows, c.offsets, c.out, c.ld_act, c.ld_out, c.act_rows, c.max_rows, p.E, p.C, p.K, p.n_mt, p.n_kb, c.out_type,
-                     (p.K + 255) / 256, p.status_dev, c.low};
+                     (p.K + 255) / 256, p.status_dev, c.low, powers()};
   const long long tiles = ((long long)c.max_rows / TL_N + (c.offsets ? min(p.E, c.max_rows) : 1)) * q.n_cp;
   const size_t smem = 1024 + TallShape<RANK>::kStages * TL_B_BYTES + TallShape<RANK>::kH + TallShape<RANK>::kB + sizeof(TallBars) + (size_t)p.E * 12;
-  products_tall_kernel<T, GATHER, RANK><<<2u * (unsigned)min(tiles, (long long)max(1, sm_count() / 2)), TallShape<RANK>::kThreads, smem, c.stream>>>(q, map);
   *launched += 1;
-  return cudaGetLastError();
+  return launch_dependent(products_tall_kernel<T, GATHER, RANK>, 2u * (unsigned)min(tiles, (long long)max(1, sm_count() / 2)), TallShape<RANK>::kThreads, smem,
+                          c.stream, q, map);
 }
 
 template <class T>

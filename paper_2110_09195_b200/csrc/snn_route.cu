@@ -4,6 +4,7 @@
 #include "snn_products.h"
 
 #include "snn_products.cuh"
+#include "snn_tc_common.cuh"
 
 namespace snn {
 namespace {
@@ -139,6 +140,8 @@ __global__ void __launch_bounds__(RT_WARPS * 32) route_choose_kernel(const Route
   __shared__ int count[32 * V], part[RT_WARPS];
   const int t0 = (int)blockIdx.x * RT_BLOCK, tokens = min(RT_BLOCK, p.T - t0), warp = threadIdx.x >> 5;
   for (int i = threadIdx.x; i < 2 * p.E; i += RT_WARPS * 32) mask[i] = 0;
+  grid_dep_wait();
+  grid_dep_launch();
   __syncthreads();
   for (int i = warp; i < tokens; i += RT_WARPS) choose<V>(p, t0 + i, mask, i);
   __syncthreads();
@@ -166,6 +169,8 @@ __global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteP
   __shared__ int part[RT_WARPS];
   const int t0 = (int)blockIdx.x * RT_BLOCK, tokens = min(RT_BLOCK, p.T - t0), n = RT_WARPS * 32;
   for (int i = threadIdx.x; i < 4 * p.E; i += n) sm[i] = 0;
+  grid_dep_wait();
+  grid_dep_launch();
   __syncthreads();
   for (int i = threadIdx.x; i < tokens * p.k; i += n) {
     const int id = p.ids[(size_t)t0 * p.k + i], local = i / p.k;
@@ -256,6 +261,8 @@ template <class Y>
 __global__ void __launch_bounds__(256) combine_kernel(const CombineParams p) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   const long long t = i / p.groups;
+  grid_dep_wait();
+  grid_dep_launch();
   const int c = (int)(i - t * p.groups) * 8;
   if (t >= p.T) return;
   const typename Element<Y>::type* const y = static_cast<const typename Element<Y>::type*>(p.y) + c;
@@ -301,6 +308,8 @@ __device__ __forceinline__ float value(const void* y, int type, long long i) {
 __global__ void __launch_bounds__(256) combine_odd_kernel(const CombineParams p) {
   const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
   const long long t = i / p.C;
+  grid_dep_wait();
+  grid_dep_launch();
   const int c = (int)(i - t * p.C);
   if (t >= p.T) return;
   float s = 0.f;
@@ -328,7 +337,8 @@ cudaError_t route_forward(const RouteCall& c, int* launched) {
   // (no tokens: one CTA writes the offsets)
   const unsigned blocks = (unsigned)max(1, (c.T + RT_BLOCK - 1) / RT_BLOCK);
   const int v = (c.E + 31) / 32;
-#define SNN_CHOOSE(V) route_choose_kernel<V><<<blocks, RT_WARPS * 32, 0, c.stream>>>(p)
+  cudaError_t e;
+#define SNN_CHOOSE(V) e = launch_dependent(route_choose_kernel<V>, blocks, RT_WARPS * 32, 0, c.stream, p)
   if (v <= 1) SNN_CHOOSE(1);
   else if (v <= 2) SNN_CHOOSE(2);
   else if (v <= 4) SNN_CHOOSE(4);
@@ -337,11 +347,9 @@ cudaError_t route_forward(const RouteCall& c, int* launched) {
   else SNN_CHOOSE(32);
 #undef SNN_CHOOSE
   *launched += 1;
-  cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || blocks == 1) return e;
-  route_place_kernel<<<blocks, RT_WARPS * 32, (size_t)c.E * 16, c.stream>>>(p);
   *launched += 1;
-  return cudaGetLastError();
+  return launch_dependent(route_place_kernel, blocks, RT_WARPS * 32, (size_t)c.E * 16, c.stream, p);
 }
 
 cudaError_t combine_forward(const CombineCall& c, int* launched) {
@@ -349,12 +357,11 @@ cudaError_t combine_forward(const CombineCall& c, int* launched) {
   const bool eights = c.C % 8 == 0 && c.ld_y % 8 == 0 && c.ld_out % 8 == 0 && (((uintptr_t)c.y | (uintptr_t)c.out) & 15) == 0;
   const long long blocks = ((long long)c.T * (eights ? p.groups : c.C) + 255) / 256;
   if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
-  if (!eights) combine_odd_kernel<<<(unsigned)blocks, 256, 0, c.stream>>>(p);
-  else if (c.y_type == SNN_OUT_F32) combine_kernel<float><<<(unsigned)blocks, 256, 0, c.stream>>>(p);
-  else if (c.y_type == SNN_OUT_F16) combine_kernel<F16><<<(unsigned)blocks, 256, 0, c.stream>>>(p);
-  else combine_kernel<BF16><<<(unsigned)blocks, 256, 0, c.stream>>>(p);
   *launched += 1;
-  return cudaGetLastError();
+  if (!eights) return launch_dependent(combine_odd_kernel, (unsigned)blocks, 256, 0, c.stream, p);
+  if (c.y_type == SNN_OUT_F32) return launch_dependent(combine_kernel<float>, (unsigned)blocks, 256, 0, c.stream, p);
+  if (c.y_type == SNN_OUT_F16) return launch_dependent(combine_kernel<F16>, (unsigned)blocks, 256, 0, c.stream, p);
+  return launch_dependent(combine_kernel<BF16>, (unsigned)blocks, 256, 0, c.stream, p);
 }
 
 }  // namespace snn

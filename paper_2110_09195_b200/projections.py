@@ -12,8 +12,10 @@ recorded for autograd.
 from __future__ import annotations
 
 import ctypes
+import struct
 
-from .binding import ACT_F16, OUT_F32, SnnConv, SnnError, _check, _raw_stream, load_library
+from . import binding
+from .binding import ACT_F16, OUT_F32, SnnConv, SnnError, _check, _load_fast, _raw_stream, load_library
 
 ACT_BF16 = 2
 OUT_F16, OUT_BF16 = 3, 4
@@ -99,6 +101,8 @@ class SnnConvExperts:
     snn_conv_experts_t).  `layers` are SnnConv objects with ksize=1 and stride 1; their weights are copied, so they
     may be destroyed afterwards."""
 
+    _h = _desc = None
+
     def __init__(self, layers):
         lib = load_library()
         layers = list(layers)
@@ -111,12 +115,19 @@ class SnnConvExperts:
         self._h = h
         self.count, self.device = len(layers), layers[0].device
         self.c_in, self.c_out = layers[0].c_in, layers[0].c_out
+        self._desc = struct.pack("=Q4i", h.value, self.device, self.count, self.c_in, self.c_out)
 
     def forward(self, x, offsets, rows=None, out=None, out_type=None, stream=None):
         """snn_conv_experts_forward: out[i] = projection_e(x[rows[i]]) for offsets[e] <= i < offsets[e + 1] (rows None:
         x[i]).  `offsets` (count + 1) and `rows` are int32 tensors that the kernels read: nothing waits for them here.
         `out` has a row for each of `rows` (without rows: any number, by default one for each row of x); its rows
         outside the experts' ranges are left as they are.  Outputs are of the type of `out`, else out_type, else x's."""
+        if out is not None and out_type is None and stream is None:
+            st = (binding._fast or _load_fast()).experts_forward(self._desc, x, offsets, rows, out)
+            if st == 0:
+                return out
+            if st > 0:
+                _check(st)
         if self._h is None:
             raise SnnError(1, "the experts were destroyed")
         act_type = _act_type(x)
@@ -132,6 +143,7 @@ class SnnConvExperts:
 
     def destroy(self):
         if getattr(self, "_h", None) is not None:
+            self._desc = None
             load_library().snn_conv_experts_destroy(self._h)
             self._h = None
 
@@ -173,6 +185,12 @@ def route(logits, top_k, normalise=True, out=None, stream=None):
     """snn_conv_experts_route: the top_k experts of each row of `logits` [tokens, experts] (float32, float16 or bfloat16),
     their weights (softmax over the chosen, or over all experts with normalise=False), and the order of the rows by
     expert that SnnConvExperts.forward and combine take.  Returns `out`, or a new Route."""
+    if out is not None and stream is None:
+        st = (binding._fast or _load_fast()).route(logits, top_k, normalise, out.ids, out.weights, out.offsets, out.rows, out.slots, out.work)
+        if st == 0:
+            return out
+        if st > 0:
+            _check(st)
     device = logits.get_device()
     if device < 0:
         raise SnnError(1, "logits must live on a CUDA device")
@@ -200,6 +218,12 @@ def route(logits, top_k, normalise=True, out=None, stream=None):
 def combine(y, slots, weights, out=None, out_type=None, stream=None):
     """snn_conv_experts_combine: out[t] = sum_j weights[t, j] * y[slots[t, j]]; a slot outside y counts nothing.  Outputs
     are of the type of `out`, else out_type, else y's."""
+    if out is not None and out_type is None and stream is None:
+        st = (binding._fast or _load_fast()).combine(y, slots, weights, out)
+        if st == 0:
+            return out
+        if st > 0:
+            _check(st)
     device = y.get_device()
     if device < 0:
         raise SnnError(1, "y must live on a CUDA device")
@@ -222,6 +246,8 @@ class SnnConvAdapters:
     """One projection shared by many requests, each with a low-rank adapter of its own or none (wraps
     snn_conv_adapters_t).  `layer` is an SnnConv object with ksize=1 and stride 1; its weights are copied."""
 
+    _h = _desc = None
+
     def __init__(self, layer):
         lib = load_library()
         if not isinstance(layer, SnnConv) or layer._h is None:
@@ -231,12 +257,19 @@ class SnnConvAdapters:
         _check(lib.snn_conv_adapters_create(layer._h, ctypes.byref(h)))
         self._h = h
         self.device, self.c_in, self.c_out = layer.device, layer.c_in, layer.c_out
+        self._desc = struct.pack("=Q4i", h.value, self.device, 1, self.c_in, self.c_out)
 
     def forward(self, x, adapter, a, b, scale, out=None, out_type=None, stream=None):
         """snn_conv_adapters_forward: out[r] = projection(x[r]) + scale[i] * b[i] @ (a[i] @ x[r]) with i = adapter[r], or
         the projection alone where i is outside [0, adapters).  a [adapters, rank, c_in] and b [adapters, c_out, rank]
         are contiguous and of x's type, scale [adapters] float32, adapter [rows] int32.  Outputs are of the type of
         `out`, else out_type, else x's."""
+        if out is not None and out_type is None and stream is None:
+            st = (binding._fast or _load_fast()).adapters_forward(self._desc, x, adapter, a, b, scale, out)
+            if st == 0:
+                return out
+            if st > 0:
+                _check(st)
         import torch
         if self._h is None:
             raise SnnError(1, "the adapters were destroyed")
@@ -261,6 +294,7 @@ class SnnConvAdapters:
 
     def destroy(self):
         if getattr(self, "_h", None) is not None:
+            self._desc = None
             load_library().snn_conv_adapters_destroy(self._h)
             self._h = None
 
