@@ -10,7 +10,9 @@ namespace snn {
 namespace {
 
 constexpr int RT_BLOCK = 64;   // tokens of a CTA: two words of a mask for each expert
+constexpr int RT_CHOOSE_WARPS = 32;   // two tokens a warp
 constexpr int RT_WARPS = 16;
+constexpr int RT_DIRECT = 32;         // CTAs up to which each adds up the others' counts by itself (8191 tokens, 128 CTAs: 20.8 us; 16385 with sums of their own 18.3)
 
 struct RouteParams {
   const void* logits;
@@ -21,13 +23,6 @@ struct RouteParams {
   int32_t *offsets, *rows, *slots, *work;
 };
 
-__device__ __forceinline__ float logit(const RouteParams& p, int t, int e) {
-  const long long i = t * p.ld + e;
-  if (p.type == SNN_OUT_F32) return static_cast<const float*>(p.logits)[i];
-  if (p.type == SNN_OUT_F16) return __half2float(static_cast<const __half*>(p.logits)[i]);
-  return __bfloat162float(static_cast<const __nv_bfloat16*>(p.logits)[i]);
-}
-
 // A float as an unsigned number of the same order, above 0; -infinity and NaN, which are not chosen, as 0.
 __device__ __forceinline__ uint32_t ordered(float v) {
   if (!(v > -CUDART_INF_F)) return 0u;
@@ -37,53 +32,103 @@ __device__ __forceinline__ uint32_t ordered(float v) {
 __device__ __forceinline__ float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 
 // exp(v - most), 1 where both are the same infinity
-__device__ __forceinline__ float above(uint32_t u, uint32_t most) { return u == most ? 1.f : expf(unordered(u) - unordered(most)); }
+__device__ __forceinline__ float above(float v, float most) { return v == most ? 1.f : expf(v - most); }
 
-// One token by one warp, E <= 32 V: lane l holds experts l, l + 32, ...  The k-th largest is taken k times: the warp's largest, then the
-// lowest expert that has it.  Lane j keeps choice j.
+// A warp's logits of a token, E <= 32 V: lane l holds experts l, l + 32, ...
 template <int V>
-__device__ __forceinline__ void choose(const RouteParams& p, int t, uint32_t* mask, int local) {
+__device__ __forceinline__ void load_logits(const RouteParams& p, int t, float (&v)[V]) {
   const int lane = threadIdx.x & 31;
-  uint32_t u[V];
+  const long long at = t * p.ld + lane;
+  if (p.type == SNN_OUT_F32) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) u[i] = lane + 32 * i < p.E ? ordered(logit(p, t, lane + 32 * i)) : 0u;
-  uint32_t best = 0;
+    for (int i = 0; i < V; ++i) v[i] = lane + 32 * i < p.E ? static_cast<const float*>(p.logits)[at + 32 * i] : -CUDART_INF_F;
+  } else {
+    uint16_t u[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) best = max(best, u[i]);
-  const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-  float all = 0.f;
-  if (!p.normalise) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) all += u[i] ? above(u[i], top) : 0.f;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
-  }
-  int id = -1;
-  float w = 0.f;
-  for (int j = 0; j < p.k; ++j) {
-    best = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) best = max(best, u[i]);
-    const uint32_t most = __reduce_max_sync(0xffffffffu, best);
-    if (!most) break;
-    uint32_t e = 0xffffffffu;
-#pragma unroll
-    for (int i = V - 1; i >= 0; --i)
-      if (u[i] == most) e = lane + 32 * i;
-    e = __reduce_min_sync(0xffffffffu, e);
+    for (int i = 0; i < V; ++i) u[i] = lane + 32 * i < p.E ? static_cast<const uint16_t*>(p.logits)[at + 32 * i] : 0;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (e == lane + 32 * i) u[i] = 0;
+      v[i] = lane + 32 * i >= p.E ? -CUDART_INF_F : p.type == SNN_OUT_F16 ? __half2float(__ushort_as_half(u[i])) : __uint_as_float((uint32_t)u[i] << 16);
+  }
+}
+
+// One token by one warp.  k times the warp's largest is taken, the lowest expert that has it, and its lane goes on to its next: up to 8
+// experts a lane are sorted before, so that the next is at hand; of more it is looked for.  Lane j keeps choice j.  Bound by the number
+// of instructions, and with few tokens by their latency: the exponentials come at the end, for all choices at once.
+template <int V>
+__device__ __forceinline__ void choose(const RouteParams& p, int t, const float (&v)[V], uint32_t* mask, int local) {
+  const int lane = threadIdx.x & 31;
+  constexpr bool SORTED = V <= 8;
+  uint32_t u[V];
+  int x[V];   // where u was in v
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    u[i] = ordered(v[i]);
+    x[i] = i;
+  }
+  if (SORTED) {
+    // (neighbours change places only if the later one is larger: equal ones keep their order)
+#pragma unroll
+    for (int n = V - 1; n > 0; --n)
+#pragma unroll
+      for (int i = 0; i < n; ++i)
+        if (u[i + 1] > u[i]) {
+          const uint32_t w = u[i];
+          u[i] = u[i + 1];
+          u[i + 1] = w;
+          const int y = x[i];
+          x[i] = x[i + 1];
+          x[i + 1] = y;
+        }
+  }
+  uint32_t best = u[0];
+  int at = x[0], id = -1;
+  auto look = [&] {
+    best = u[0];
+    at = 0;
+#pragma unroll
+    for (int i = 1; i < V; ++i)
+      if (u[i] > best) {
+        best = u[i];
+        at = i;
+      }
+  };
+  if (!SORTED) look();
+  const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+  uint32_t most = top, mine = 0;
+  for (int j = 0; j < p.k && most; ++j) {   // (0: nothing left that can be chosen)
+    const uint32_t me = (uint32_t)(lane + 32 * at), e = __reduce_min_sync(0xffffffffu, best == most ? me : 0xffffffffu);
     if (lane == j) {
       id = (int)e;
-      w = above(most, top);
+      mine = most;
     }
-  }
-  if (p.normalise) {
-    all = w;
+    if (e == me) {
+      if (SORTED) {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+        for (int i = 0; i + 1 < V; ++i) {
+          u[i] = u[i + 1];
+          x[i] = x[i + 1];
+        }
+        u[V - 1] = 0;
+        best = u[0];
+        at = x[0];
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (i == at) u[i] = 0;
+        look();
+      }
+    }
+    most = __reduce_max_sync(0xffffffffu, best);
   }
+  const float largest = unordered(top), w = id < 0 ? 0.f : above(unordered(mine), largest);
+  float all = p.normalise ? w : 0.f;
+  if (!p.normalise) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) all += v[i] > -CUDART_INF_F ? above(v[i], largest) : 0.f;
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
   if (lane < p.k) {
     p.ids[(size_t)t * p.k + lane] = id;
     p.weights[(size_t)t * p.k + lane] = id < 0 ? 0.f : w / all;
@@ -93,7 +138,7 @@ __device__ __forceinline__ void choose(const RouteParams& p, int t, uint32_t* ma
 
 // Exclusive sums of count[0..E) in place, by the whole CTA; returns the total.
 __device__ int scan_counts(int* count, int E, int* part) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = RT_WARPS * 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = (int)blockDim.x, warps = n >> 5;
   int base = 0;
   for (int e0 = 0; e0 < E; e0 += n) {
     const int e = e0 + (int)threadIdx.x, v = e < E ? count[e] : 0;
@@ -105,13 +150,15 @@ __device__ int scan_counts(int* count, int E, int* part) {
     }
     if (lane == 31) part[warp] = upto;
     __syncthreads();
-    int before = base, all = base;
-    for (int w = 0; w < RT_WARPS; ++w) {
-      if (w < warp) before += part[w];
-      all += part[w];
+    int sums = lane < warps ? part[lane] : 0;   // (each warp adds up the warps' sums for itself)
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, sums, d);
+      if (lane >= d) sums += o;
     }
-    if (e < E) count[e] = before + upto - v;
-    base = all;
+    const int before = __shfl_sync(0xffffffffu, sums, max(warp - 1, 0));
+    if (e < E) count[e] = base + (warp ? before : 0) + upto - v;
+    base += __shfl_sync(0xffffffffu, sums, 31);
     __syncthreads();
   }
   return base;
@@ -119,8 +166,8 @@ __device__ int scan_counts(int* count, int E, int* part) {
 
 // Rows and slots of the CTA's tokens: start[e] is the first row of the CTA's choices of expert e, the mask says which of its tokens
 // come before.
-__device__ void place(const RouteParams& p, const uint32_t* mask, const int* start, int t0, int tokens) {
-  for (int i = threadIdx.x; i < tokens * p.k; i += RT_WARPS * 32) {
+__device__ __forceinline__ void place(const RouteParams& p, const uint32_t* mask, const int* start, int t0, int tokens) {
+  for (int i = threadIdx.x; i < tokens * p.k; i += (int)blockDim.x) {
     const int local = i / p.k, id = p.ids[(size_t)t0 * p.k + i];
     int slot = -1;
     if (id >= 0) {
@@ -135,18 +182,30 @@ __device__ void place(const RouteParams& p, const uint32_t* mask, const int* sta
 // First launch: each CTA's tokens choose, and the CTA counts its choices of each expert.  With one CTA that is all there is to count, and it
 // goes on to place them.
 template <int V>
-__global__ void __launch_bounds__(RT_WARPS * 32) route_choose_kernel(const RouteParams p) {
+__global__ void __launch_bounds__(RT_CHOOSE_WARPS * 32) route_choose_kernel(const RouteParams p) {
+  const int threads = (int)blockDim.x;
   __shared__ uint32_t mask[2 * 32 * V];
-  __shared__ int count[32 * V], part[RT_WARPS];
+  __shared__ int count[32 * V], part[RT_CHOOSE_WARPS];
   const int t0 = (int)blockIdx.x * RT_BLOCK, tokens = min(RT_BLOCK, p.T - t0), warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < 2 * p.E; i += RT_WARPS * 32) mask[i] = 0;
+  for (int i = threadIdx.x; i < 2 * p.E; i += threads) mask[i] = 0;
   grid_dep_wait();
   grid_dep_launch();
   __syncthreads();
-  for (int i = warp; i < tokens; i += RT_WARPS) choose<V>(p, t0 + i, mask, i);
+  float v[V];
+  if (warp < tokens) load_logits(p, t0 + warp, v);
+  const int step = threads >> 5;
+  for (int i = warp; i < tokens; i += step) {
+    float next[V];
+    const bool more = i + step < tokens;
+    if (more) load_logits(p, t0 + i + step, next);
+    choose<V>(p, t0 + i, v, mask, i);
+#pragma unroll
+    for (int q = 0; q < V; ++q)
+      if (more) v[q] = next[q];
+  }
   __syncthreads();
   const bool alone = gridDim.x == 1;
-  for (int e = threadIdx.x; e < p.E; e += RT_WARPS * 32) {
+  for (int e = threadIdx.x; e < p.E; e += threads) {
     const int n = __popc(mask[2 * e]) + __popc(mask[2 * e + 1]);
     if (alone) count[e] = n;
     else p.work[(size_t)blockIdx.x * p.E + e] = n;
@@ -154,14 +213,46 @@ __global__ void __launch_bounds__(RT_WARPS * 32) route_choose_kernel(const Route
   if (!alone) return;
   __syncthreads();
   const int total = scan_counts(count, p.E, part);
-  for (int e = threadIdx.x; e < p.E; e += RT_WARPS * 32) p.offsets[e] = count[e];
+  for (int e = threadIdx.x; e < p.E; e += threads) p.offsets[e] = count[e];
   if (threadIdx.x == 0) p.offsets[p.E] = total;
   place(p, mask, count, t0, tokens);
-  for (int i = total + (int)threadIdx.x; i < p.T * p.k; i += RT_WARPS * 32) p.rows[i] = -1;
+  for (int i = total + (int)threadIdx.x; i < p.T * p.k; i += threads) p.rows[i] = -1;
 }
 
-// Second launch: each CTA adds up all CTAs' counts, for the experts' first rows, and those of the CTAs before it, for its own.
-__global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteParams p) {
+// Between the two with many CTAs: the counts become sums over the CTAs before, and the totals follow behind the last.  A CTA has 32
+// experts, a lane one of them, each warp a run of the CTAs.
+__global__ void __launch_bounds__(1024) route_sum_kernel(int32_t* work, int E, int blocks) {
+  __shared__ int part[32][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = (int)blockIdx.x * 32 + lane;
+  const int each = (blocks + 31) / 32, b0 = min(blocks, warp * each), b1 = min(blocks, b0 + each);
+  grid_dep_wait();
+  grid_dep_launch();
+  int sum = 0;
+  if (e < E)
+#pragma unroll 8
+    for (int b = b0; b < b1; ++b) sum += work[(size_t)b * E + e];
+  part[warp][lane] = sum;
+  __syncthreads();
+  int before = 0;
+  for (int w = 0; w < warp; ++w) before += part[w][lane];
+  if (e < E) {
+    for (int b = b0; b < b1; b += 8) {
+      int v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = b + i < b1 ? work[(size_t)(b + i) * E + e] : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (b + i < b1) work[(size_t)(b + i) * E + e] = before;
+        before += v[i];
+      }
+    }
+    if (warp == 31) work[(size_t)blocks * E + e] = before;
+  }
+}
+
+// Last launch: where the experts' rows begin, and where this CTA's begin among them (all CTAs' counts, added up here if `direct`), then its
+// tokens' rows and slots.
+__global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteParams p, int direct) {
   extern __shared__ int sm[];
   int* const all = sm;                                                 // [E]
   int* const before = sm + p.E;                                        // [E]
@@ -176,12 +267,28 @@ __global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteP
     const int id = p.ids[(size_t)t0 * p.k + i], local = i / p.k;
     if (id >= 0) atomicOr(mask + 2 * id + (local >> 5), 1u << (local & 31));
   }
-  // (sums of whole numbers: any order gives the same)
-  for (int i = threadIdx.x; i < (int)gridDim.x * p.E; i += n) {
-    const int b = i / p.E, e = i - b * p.E, v = p.work[i];
-    if (v) {
-      atomicAdd(all + e, v);
-      if (b < (int)blockIdx.x) atomicAdd(before + e, v);
+  if (direct) {
+    // a thread has an expert and every `turns`-th CTA, eight loads on their way; the turns' sums meet (whole numbers: any order gives the same)
+    const int width = (min(p.E, n) + 31) & ~31, turns = n / width, turn = (int)threadIdx.x / width;
+    for (int e = (int)threadIdx.x - turn * width; turn < turns && e < p.E; e += width) {
+      int sum = 0, mine = 0;
+      for (int b0 = turn; b0 < (int)gridDim.x; b0 += 8 * turns) {
+        int v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = b0 + i * turns < (int)gridDim.x ? p.work[(size_t)(b0 + i * turns) * p.E + e] : 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sum += v[i];
+          if (b0 + i * turns < (int)blockIdx.x) mine += v[i];
+        }
+      }
+      atomicAdd(all + e, sum);
+      atomicAdd(before + e, mine);
+    }
+  } else {
+    for (int e = threadIdx.x; e < p.E; e += n) {
+      all[e] = p.work[(size_t)gridDim.x * p.E + e];
+      before[e] = p.work[(size_t)blockIdx.x * p.E + e];
     }
   }
   __syncthreads();
@@ -330,15 +437,19 @@ __global__ void __launch_bounds__(256) combine_odd_kernel(const CombineParams p)
 
 }  // namespace
 
-long long route_work_bytes(int T, int E) { return T <= RT_BLOCK ? 0 : (long long)((T + RT_BLOCK - 1) / RT_BLOCK) * E * 4; }
+long long route_work_bytes(int T, int E) {
+  if (T <= RT_BLOCK) return 0;
+  const long long blocks = (T + (long long)RT_BLOCK - 1) / RT_BLOCK;
+  return (blocks <= RT_DIRECT ? blocks : blocks + 1) * E * 4;
+}
 
 cudaError_t route_forward(const RouteCall& c, int* launched) {
   const RouteParams p{c.logits, c.ld, c.type, c.T, c.E, c.k, c.normalise, c.ids, c.weights, c.offsets, c.rows, c.slots, c.work};
   // (no tokens: one CTA writes the offsets)
-  const unsigned blocks = (unsigned)max(1, (c.T + RT_BLOCK - 1) / RT_BLOCK);
-  const int v = (c.E + 31) / 32;
+  const unsigned blocks = (unsigned)max(1ll, (c.T + (long long)RT_BLOCK - 1) / RT_BLOCK);
+  const int v = (c.E + 31) / 32, threads = 32 * min(RT_CHOOSE_WARPS, max(4, c.T));   // (few tokens: a small CTA begins sooner)
   cudaError_t e;
-#define SNN_CHOOSE(V) e = launch_dependent(route_choose_kernel<V>, blocks, RT_WARPS * 32, 0, c.stream, p)
+#define SNN_CHOOSE(V) e = launch_dependent(route_choose_kernel<V>, blocks, threads, 0, c.stream, p)
   if (v <= 1) SNN_CHOOSE(1);
   else if (v <= 2) SNN_CHOOSE(2);
   else if (v <= 4) SNN_CHOOSE(4);
@@ -348,8 +459,14 @@ cudaError_t route_forward(const RouteCall& c, int* launched) {
 #undef SNN_CHOOSE
   *launched += 1;
   if (e != cudaSuccess || blocks == 1) return e;
+  const bool direct = blocks <= RT_DIRECT;
+  if (!direct) {
+    e = launch_dependent(route_sum_kernel, (unsigned)((c.E + 31) / 32), 1024, 0, c.stream, c.work, c.E, (int)blocks);
+    *launched += 1;
+    if (e != cudaSuccess) return e;
+  }
   *launched += 1;
-  return launch_dependent(route_place_kernel, blocks, RT_WARPS * 32, (size_t)c.E * 16, c.stream, p);
+  return launch_dependent(route_place_kernel, blocks, RT_WARPS * 32, (size_t)c.E * 16, c.stream, p, (int)direct);
 }
 
 cudaError_t combine_forward(const CombineCall& c, int* launched) {

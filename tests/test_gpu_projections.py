@@ -291,6 +291,25 @@ def test_route_masks(snn, T, normalise):
     assert (r.offsets == 0).all() and (r.rows == -1).all()
 
 
+@pytest.mark.parametrize("T,E,k", [(16384, 20, 3), (16385, 40, 2), (40001, 300, 4)])
+def test_route_long(snn, T, E, k):
+    """Past 256 groups of 64 tokens the counts are summed up in a launch of their own; compared with sorts, all values being different."""
+    g = _gen(T)
+    logits = torch.rand(T, E, generator=g, device="cuda").argsort(1).float() / 8   # (no two equal in a row)
+    r = snn.route(logits, k)
+    top, ids = torch.sort(logits, dim=1, descending=True)
+    assert torch.equal(r.ids, ids[:, :k].to(torch.int32))
+    w = torch.softmax(top[:, :k].double(), 1)
+    assert ((r.weights.double() - w).abs() <= 2.0 ** -20 * w).all()   # (differences of eighths: exact; expf, k sums, a division)
+    order = torch.sort(ids[:, :k].reshape(-1), stable=True).indices
+    assert torch.equal(r.rows, (order // k).to(torch.int32))
+    counts = torch.bincount(ids[:, :k].reshape(-1), minlength=E)
+    assert torch.equal(r.offsets[1:], torch.cumsum(counts, 0).to(torch.int32)) and r.offsets[0] == 0
+    slots = torch.empty_like(order)
+    slots[order] = torch.arange(T * k, device="cuda")
+    assert torch.equal(r.slots.reshape(-1), slots.to(torch.int32))
+
+
 def test_route_strided_and_empty(snn):
     wide = torch.randn(70, 50, generator=_gen(1), device="cuda")
     logits = wide[:, 5:38]
