@@ -30,7 +30,7 @@ constexpr int TL_HALF = TL_N / 2;      // rows of a CTA
 constexpr int TL_B_BYTES = TL_HALF * 128;
 constexpr int TL_BOX = 32;            // rows of one TMA box
 // warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs (with adapters: 12-19)
-constexpr int TL_PENDING = 8;         // stages of copied rows on their way
+constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for each of the three warps that copy
 // Stages of rows, and bytes of the tile's rows' A x and of an adapter's B kept beside them (RANK: 0 without adapters, else a bound of
 // their rank).
 template <int RANK>
@@ -317,7 +317,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
     for (int e = e0; e < e1; ++e) R.end[e] = end += (R.n[e] + TL_N - 1) / TL_N;
   } else if (warp == 1 && lane == 0) {
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(smem_u32(&bars->b_full[i]), GATHER ? 6 : 1);
+      mbar_init(smem_u32(&bars->b_full[i]), GATHER ? 2 : 1);
       mbar_init(smem_u32(&bars->b_empty[i]), 1);
     }
     for (int i = 0; i < TL_A_STAGES; ++i) {
@@ -350,49 +350,54 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
 
   if (GATHER && (warp == 0 || warp == 2 || warp == 3)) {
     // ------------------------------------------------------------ rows by an index: 8 lanes copy 128 bytes of a row
-    const int first = 4 * (warp ? warp - 1 : 0) + (lane >> 3), chunk = lane & 7;   // rows first, first + 12, ... of the CTA's
+    // Each of the three warps has every third stage: what a stage costs beside its copies is a third of the time for each.
+    const int first = lane >> 3, chunk = lane & 7, turn = warp ? warp - 1 : 0;   // rows first, first + 4, ... of the CTA's
     const uint32_t dst = b_smem + (uint32_t)first * 128u;
-    int s = 0, issued = 0;
-    uint32_t phase = 0;
-    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
-      const int half = ((t.n + 31) & ~31) / 2, r0 = t.r0 + rank * half, n = t.n - rank * half;
-      int who[TL_HALF / 12];
+    const uint32_t swizzled[2] = {(uint32_t)((chunk ^ first) << 4), (uint32_t)((chunk ^ (first + 4)) << 4)};
+    uint32_t seq = 0;   // stages of the tiles before
+    int issued = 0;
+    uint32_t mine[TL_PENDING + 1] = {};   // the last stages this warp issued, the oldest first
+    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs, seq += (uint32_t)nk) {
+      const int half = ((t.n + 31) & ~31) / 2, r0 = t.r0 + rank * half, n = min(t.n - rank * half, half);
+      int who[TL_HALF / 4];
 #pragma unroll
-      for (int i = 0; i < TL_HALF / 12; ++i) {
-        const int c = first + 12 * i;
-        who[i] = c < min(n, half) ? p.rows[r0 + c] : -1;
+      for (int i = 0; i < TL_HALF / 4; ++i) {
+        const int c = first + 4 * i;
+        who[i] = c < n ? p.rows[r0 + c] : -1;
         if (who[i] >= p.act_rows) who[i] = -1;   // (outside: zeros)
       }
-      for (int kb = 0; kb < nk; ++kb) {
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->b_empty[s]), phase ^ 1u));
+      for (int kb = (int)((turn + 3u - seq % 3u) % 3u); kb < nk; kb += 3) {
+        const uint32_t at = seq + (uint32_t)kb, s = at % STAGES;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->b_empty[s]), (at / STAGES & 1u) ^ 1u));
         if (!ok) break;
         const int k = kb * 64 + chunk * 8;
         const uint16_t* const x = p.act + k;
         const bool in = k < p.C;
 #pragma unroll
-        for (int i = 0; i < TL_HALF / 12; ++i) {
-          const int c = first + 12 * i;
+        for (int i = 0; i < TL_HALF / 4; ++i) {
           const bool there = in && who[i] >= 0;
-          if (c < half) copy16(dst + s * TL_B_BYTES + i * 1536 + ((chunk ^ (c & 7)) << 4), there ? x + (size_t)who[i] * (size_t)p.ld_act : p.act, there);
+          if (4 * i < half) copy16(dst + s * TL_B_BYTES + i * 512 + swizzled[i & 1], there ? x + (size_t)who[i] * (size_t)p.ld_act : p.act, there);
         }
         copy_commit();
-        if (++s == STAGES) {
-          s = 0;
-          phase ^= 1u;
-        }
+#pragma unroll
+        for (int i = 0; i < TL_PENDING; ++i) mine[i] = mine[i + 1];
+        mine[TL_PENDING] = s;
         if (++issued > TL_PENDING) {   // the oldest stage on its way has landed
           copy_wait<TL_PENDING>();
           fence_proxy_async();
           __syncwarp();
-          if (lane == 0) arrive_at_first(smem_u32(&bars->b_full[(s + STAGES - 1 - TL_PENDING) % STAGES]));
+          if (lane == 0) arrive_at_first(smem_u32(&bars->b_full[mine[0]]));
         }
       }
     }
     copy_wait<0>();
     fence_proxy_async();
     __syncwarp();
-    if (lane == 0)
-      for (int i = min(issued, TL_PENDING); i > 0; --i) arrive_at_first(smem_u32(&bars->b_full[(s + STAGES - i) % STAGES]));
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 1; i <= TL_PENDING; ++i)
+        if (TL_PENDING - i < issued) arrive_at_first(smem_u32(&bars->b_full[mine[i]]));
+    }
     if (!ok && lane == 0) raise_status(p.status, 20);
   } else if (!GATHER && warp == 0) {
     // ------------------------------------------------------------ rows: one stage is 64 input channels of the tile's rows
