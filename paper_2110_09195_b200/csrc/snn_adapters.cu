@@ -19,42 +19,41 @@ struct ShrinkParams {
 // A CTA takes up to 8 NT neighbouring rows and 16 MT of the rank; its warps take different input channels, and their sums meet in shared
 // memory.  One pass for each adapter that the rows have (rows of one request lie together: mostly one); the rows of other adapters are
 // computed along and not written.  Bound by reading A: once for each CTA, so with few rows a CTA has few of them, and all of A's
-// readers run at once; with many rows 16, and A comes from L2.
-template <class T, int NT, int MT, int U>
-__global__ void __launch_bounds__(256) shrink_kernel(const ShrinkParams p) {
+// readers run at once; with many rows 32, and A comes from L2.
+template <class T, int NT, int MT, int U, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) shrink_kernel(const ShrinkParams p) {
   constexpr int N = 8 * NT, M = 16 * MT;
-  __shared__ float red[8][N][M + 1];
-  __shared__ int who[N];
+  extern __shared__ float red_raw[];
+  float (*const red)[N][M + 1] = reinterpret_cast<float (*)[N][M + 1]>(red_raw);   // [WARPS]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int r0 = (int)blockIdx.x * p.per_cta, n = min(p.per_cta, p.rows - r0), j0 = (int)blockIdx.y * M;
   grid_dep_wait();
   grid_dep_launch();   // (the projection's kernel begins with its own sums; it waits for these before it adds them)
-  if (threadIdx.x < N) {
-    const int a = (int)threadIdx.x < n ? p.adapter[r0 + threadIdx.x] : -1;
-    who[threadIdx.x] = a >= 0 && a < p.n ? a : -1;
-  }
-  __syncthreads();
+  // (each warp for itself: lane i has row i's adapter, and a bit for each adapter's first row)
+  int who = lane < n ? p.adapter[r0 + lane] : -1;
+  if (who < 0 || who >= p.n) who = -1;
+  const unsigned like_me = __match_any_sync(0xffffffffu, who);
+  unsigned todo = __ballot_sync(0xffffffffu, who >= 0 && (int)__ffs(like_me) - 1 == lane);
   const uint16_t* x[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) x[i] = 8 * i + g < n ? p.act + (size_t)(r0 + 8 * i + g) * (size_t)p.ld_act + 16 * t : nullptr;
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  for (int c = 0; c < n; ++c) {
-    const int a = who[c];
-    bool seen = a < 0;
-    for (int i = 0; i < c; ++i) seen = seen || who[i] == a;
-    if (seen) continue;
+  while (todo) {
+    const int c = __ffs(todo) - 1, a = __shfl_sync(0xffffffffu, who, c);
+    const unsigned same = __shfl_sync(0xffffffffu, like_me, c);
+    todo &= todo - 1;
     const uint16_t* w[2 * MT];
 #pragma unroll
     for (int i = 0; i < 2 * MT; ++i) w[i] = j0 + 8 * i < p.rank ? p.a + ((size_t)a * p.rank + j0 + 8 * i + g) * p.C + 16 * t : nullptr;
     float acc[MT][NT][4] = {};
     // U blocks of 64 input channels on their way, then their products
-    for (int k0 = warp * 64; k0 < p.C; k0 += 512 * U) {
+    for (int k0 = warp * 64; k0 < p.C; k0 += 64 * WARPS * U) {
       uint4 b[U][NT][2], u[U][2 * MT][2];
 #pragma unroll
       for (int v = 0; v < U; ++v)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int k = k0 + 512 * v + 8 * h;
+          const int k = k0 + 64 * WARPS * v + 8 * h;
           const bool in = k + 16 * t < p.C;
 #pragma unroll
           for (int i = 0; i < 2 * MT; ++i) u[v][i][h] = in && w[i] ? ld16(w[i] + k) : zero;
@@ -81,33 +80,36 @@ __global__ void __launch_bounds__(256) shrink_kernel(const ShrinkParams p) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) red[warp][8 * i + 2 * t + (q & 1)][16 * m + g + 8 * (q >> 1)] = acc[m][i][q];
     __syncthreads();
-    for (int i = threadIdx.x; i < n * M; i += 256) {
+    for (int i = threadIdx.x; i < n * M; i += 32 * WARPS) {
       const int row = i / M, j = i % M;
-      if (who[row] != a || j0 + j >= p.rank) continue;
+      if (!((same >> row) & 1u) || j0 + j >= p.rank) continue;
       float s = 0.f;
 #pragma unroll
-      for (int v = 0; v < 8; ++v) s += red[v][row][j];
+      for (int v = 0; v < WARPS; ++v) s += red[v][row][j];
       p.h[(size_t)(r0 + row) * p.rank + j0 + j] = p.scale[a] * s;
     }
     __syncthreads();
   }
 }
 
-template <class T, int NT, int MT, int U>
+template <class T, int NT, int MT, int U, int WARPS>
 cudaError_t shrink_launch(const ShrinkParams& p, cudaStream_t s) {
+  static unsigned long long done = 0;
+  const cudaError_t e = allow_max_smem(shrink_kernel<T, NT, MT, U, WARPS>, &done);
+  if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT)));
-  return launch_dependent(shrink_kernel<T, NT, MT, U>, grid, 256, 0, s, p);
+  return launch_dependent(shrink_kernel<T, NT, MT, U, WARPS>, grid, 32 * WARPS, (size_t)WARPS * 8 * NT * (16 * MT + 1) * 4, s, p);
 }
 
 template <class T>
 cudaError_t shrink_type(ShrinkParams p, cudaStream_t s) {
   const int sms = sm_count();
   if (p.rows >= 16 * sms) {
-    p.per_cta = 16;
-    return p.rank > 16 ? shrink_launch<T, 2, 2, 2>(p, s) : shrink_launch<T, 2, 1, 2>(p, s);
+    p.per_cta = 32;
+    return p.rank > 16 ? shrink_launch<T, 4, 2, 1, 16>(p, s) : shrink_launch<T, 4, 1, 1, 16>(p, s);
   }
   p.per_cta = max(1, min(8, p.rows / sms));
-  return shrink_launch<T, 1, 1, 4>(p, s);
+  return shrink_launch<T, 1, 1, 4, 8>(p, s);
 }
 
 }  // namespace
