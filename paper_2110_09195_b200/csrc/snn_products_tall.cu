@@ -35,11 +35,12 @@ constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for
 // their rank).
 template <int RANK>
 struct TallShape {
-  static constexpr int kStages = RANK == 128 ? 4 : RANK == 64 ? 10 : RANK == 32 ? 13 : RANK == 16 ? 15 : 16;
+  static constexpr int kStages = RANK == 128 ? 4 : RANK == 64 ? 7 : RANK == 32 ? 12 : RANK == 16 ? 14 : 16;
   static constexpr int kOutWarps = RANK ? 8 : 4;
   static constexpr int kThreads = 384 + 32 * kOutWarps;
   static constexpr int kH = RANK ? TL_N * (RANK + 4) * 4 : 0;       // fp32, rows in different banks
-  static constexpr int kB = RANK ? 256 * (RANK + 8) * 2 : 0;        // 16-bit, the same; each warp its own
+  static constexpr bool kWide = RANK <= 64;                          // B as fp32, too; else there is no room
+  static constexpr int kB = RANK ? 256 * (kWide ? (RANK + 4) * 4 : (RANK + 8) * 2) : 0;   // the same; each warp its own
 };
 
 // The same value in all lanes, known to be so
@@ -254,7 +255,8 @@ __device__ __forceinline__ float sum2(uint64_t v) {
   asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
   return a + b;
 }
-// 8 of the rank: b, of channels g, g + 8, g + 16, g + 24; h, of rows 2t and 2t + 1, h_row floats apart
+// 8 of the rank: b, of channels g, g + 8, g + 16, g + 24 (16-bit values, or pairs of fp32 values as they are in shared memory, which saves
+// as many instructions as the products take); h, of rows 2t and 2t + 1, h_row floats apart
 template <class T>
 __device__ __forceinline__ void lowrank_step(uint64_t (&d)[2][4], const uint4 (&b)[4], const float* h, int h_row) {
 #pragma unroll
@@ -272,6 +274,31 @@ __device__ __forceinline__ void lowrank_step(uint64_t (&d)[2][4], const uint4 (&
       }
     }
   }
+}
+__device__ __forceinline__ ulonglong2 lds16(uint32_t addr) {
+  ulonglong2 v;
+  asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "r"(addr));
+  return v;
+}
+// (addresses in shared memory; all loads before the first product: beside the pair's MMAs a load takes over a hundred cycles)
+__device__ __forceinline__ void lowrank_step_wide(uint64_t (&d)[2][4], uint32_t b, uint32_t b_row, uint32_t h, uint32_t h_row) {
+  ulonglong2 x[2][2], w[4][2];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i][half] = lds16(h + i * h_row + 16 * half);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c][half] = lds16(b + 8 * c * b_row + 16 * half);
+  }
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fma2(d[i][c], w[c][half].x, x[i][half].x);
+        fma2(d[i][c], w[c][half].y, x[i][half].y);
+      }
 }
 // ... added to the outputs of the rows whose bit is set
 __device__ __forceinline__ void add_lowrank(float (&v)[2][4], const uint64_t (&d)[2][4], uint32_t which) {
@@ -516,9 +543,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
     // ------------------------------------------------------------ outputs: thread m is channel m of the tile, a column is a row
     const int m = ((int)threadIdx.x - 384) & 127, turn = (warp - 12) >> 2;
     constexpr int OUTS = 32 * TallShape<RANK>::kOutWarps;
-    const int h_row = p.low.rank + 4, b_row = p.low.rank + 8;   // (elements)
+    constexpr bool WIDE = TallShape<RANK>::kWide;
+    const int h_row = p.low.rank + 4, b_row = p.low.rank + (WIDE ? 4 : 8);   // (elements)
     float* const h_smem = reinterpret_cast<float*>(smem + STAGES * TL_B_BYTES);
-    uint16_t* const b_smem_warp = reinterpret_cast<uint16_t*>(smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH) + (warp - 12) * 32 * b_row;
+    uint8_t* const b_smem_warp = smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH + (warp - 12) * 32 * b_row * (WIDE ? 4 : 2);
+    float* const b_wide = reinterpret_cast<float*>(b_smem_warp);
+    uint16_t* const b_narrow = reinterpret_cast<uint16_t*>(b_smem_warp);
     int *const who = bars->who, *const group = bars->group;
     constexpr int MIXED = -2;
     int d = 0;
@@ -580,17 +610,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
               held = a;
               __syncwarp();
               const int chunks = n_rank / 8, all = min(32, p.K - co0) * chunks;
-              for (int i = lane; i < all; i += 32)
-                *reinterpret_cast<uint4*>(b_smem_warp + (i / chunks) * b_row + 8 * (i % chunks)) = ld16(b_all + a * b_size + (size_t)co0 * n_rank + 8 * i);
+              for (int i = lane; i < all; i += 32) {
+                const uint4 u = ld16(b_all + a * b_size + (size_t)co0 * n_rank + 8 * i);
+                const int at = (i / chunks) * b_row + 8 * (i % chunks);
+                if (WIDE) {
+                  const float2 f0 = T::unpack(u.x), f1 = T::unpack(u.y), f2 = T::unpack(u.z), f3 = T::unpack(u.w);
+                  *reinterpret_cast<float4*>(b_wide + at) = make_float4(f0.x, f0.y, f1.x, f1.y);
+                  *reinterpret_cast<float4*>(b_wide + at + 4) = make_float4(f2.x, f2.y, f3.x, f3.y);
+                } else {
+                  *reinterpret_cast<uint4*>(b_narrow + at) = u;
+                }
+              }
               __syncwarp();
             }
             uint64_t low[2][4] = {};
-#pragma unroll 2
+#pragma unroll 1
             for (int j = 0; j < n_rank; j += 8) {
-              uint4 b[4];
+              if (WIDE) {
+                lowrank_step_wide(low, smem_u32(b_wide + g * b_row + j), 4u * (uint32_t)b_row, smem_u32(h + j), 4u * (uint32_t)h_row);
+              } else {
+                uint4 b[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) b[i] = *reinterpret_cast<const uint4*>(b_smem_warp + (8 * i + g) * b_row + j);
-              lowrank_step<T>(low, b, h + j, h_row);
+                for (int i = 0; i < 4; ++i) b[i] = *reinterpret_cast<const uint4*>(b_narrow + (8 * i + g) * b_row + j);
+                lowrank_step<T>(low, b, h + j, h_row);
+              }
             }
             add_lowrank(v, low, 3u);
           } else if (a == MIXED) {
