@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
   // The kernel before may be the one that writes A x: it has waited for what came before it, and so for the rows and all else that is read
   // or overwritten here.  Else this waits for whatever came before.
   if (!p.low.adapter) grid_dep_wait();
+  const Powers pow = in_registers(p.pow);
   const Pieces pieces = count_pieces(p.offsets, p.E, p.max_rows, SM_N);
   const long long items = (long long)pieces.total * n_groups;
   long long item = items * blockIdx.x / gridDim.x;
@@ -135,34 +136,38 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
       const int row = p.rows ? p.rows[r0 + g] : r0 + g;
       if (row >= 0 && row < p.act_rows) x = static_cast<const uint16_t*>(p.act) + (size_t)row * (size_t)p.ld_act + 16 * t;
     }
-    for (int group = group0; group < group1; ++group) {
+    const uint2* const bits = reinterpret_cast<const uint2*>(p.bits) + (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
+    uint2 w[2][2];   // [tile][odd blocks of 64]
+    auto load_bits = [&](int group, int pair, int kb) {
       // (tiles behind the last: the sums of the last pair there is, which nobody writes)
-      const int mt0 = 2 * MP * (group * m_warps + mw);
-      const uint2* const bits = reinterpret_cast<const uint2*>(p.bits) + (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
-      uint2 w[2][2];   // [tile][odd blocks of 64]
-      auto load_bits = [&](int pair, int kb) {
-        const int mt = min(mt0 + 2 * pair, p.n_mt - 2);
+      const int mt = min(2 * MP * (group * m_warps + mw) + 2 * pair, p.n_mt - 2);
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int o = 0; o < 2; ++o) w[m][o] = ld8(bits + ((size_t)(mt + m) * p.n_kb + kb) * 64 + 4 * o);
-      };
+        for (int o = 0; o < 2; ++o) w[m][o] = ld8(bits + ((size_t)(mt + m) * p.n_kb + kb) * 64 + 4 * o);
+    };
+    uint4 b[4][2];
+    auto load_rows = [&](int kb) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = kb * 256 + j * 64 + 8 * h;
+          b[j][h] = x && c + 16 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    load_bits(group0, 0, kw);
+    load_rows(kw);
+    for (int group = group0; group < group1; ++group) {
       float acc[2 * MP][4] = {};
-      load_bits(0, kw);
       for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
-        uint4 b[4][2];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int c = kb * 256 + j * 64 + 8 * h;
-            b[j][h] = x && c + 16 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
-          }
+        const bool last_kb = kb + p.k_warps >= p.n_kb;
 #pragma unroll
         for (int pair = 0; pair < MP; ++pair) {
           const uint32_t u[2][4] = {{w[0][0].x, w[0][1].x, w[0][0].y, w[0][1].y}, {w[1][0].x, w[1][1].x, w[1][0].y, w[1][1].y}};
-          if (pair + 1 < MP) load_bits(pair + 1, kb);
-          else if (kb + p.k_warps < p.n_kb) load_bits(0, kb + p.k_warps);
+          if (pair + 1 < MP) load_bits(group, pair + 1, kb);
+          else if (!last_kb) load_bits(group, 0, kb + p.k_warps);
+          else if (group + 1 < group1) load_bits(group + 1, 0, kw);
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -170,12 +175,15 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
               const uint4& v = b[j][s >> 1];
 #pragma unroll
               for (int m = 0; m < 2; ++m) {
-                const uint32_t a0 = plus_minus<T>(u[m][j], 15 - 2 * s, p.pow), a1 = plus_minus<T>(u[m][j], 7 - 2 * s, p.pow);
-                const uint32_t a2 = plus_minus<T>(u[m][j], 14 - 2 * s, p.pow), a3 = plus_minus<T>(u[m][j], 6 - 2 * s, p.pow);
+                const uint32_t a0 = plus_minus<T>(u[m][j], 15 - 2 * s, pow), a1 = plus_minus<T>(u[m][j], 7 - 2 * s, pow);
+                const uint32_t a2 = plus_minus<T>(u[m][j], 14 - 2 * s, pow), a3 = plus_minus<T>(u[m][j], 6 - 2 * s, pow);
                 mma_16x8<T>(acc[2 * pair + m], a0, a1, a2, a3, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
               }
             }
         }
+        // the next input channels', or, before the sums meet, the next strip's
+        if (!last_kb) load_rows(kb + p.k_warps);
+        else if (group + 1 < group1 && p.n_kb > p.k_warps) load_rows(kw);
       }
       float (*const red)[SM_N][M + 1] = red_both[turn];
       turn ^= 1;
@@ -190,9 +198,10 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
       for (int i = threadIdx.x; i < n * width; i += 256) {
         const int c = i / width, m = i % width, co = first + m;
         if (co >= p.K) continue;
+        const float alpha = p.alpha[(size_t)e * p.n_mt * 16 + co];
         float s = 0.f;
         for (int k = 0; k < p.k_warps; ++k) s += red[(m / M) * p.k_warps + k][c][m % M];
-        float v = p.alpha[(size_t)e * p.n_mt * 16 + co] * s;
+        float v = alpha * s;
         if (p.low.adapter) v += lowrank_term<T>(p.low, p.K, r0 + c, co);
         store_out(p.out, p.out_type, (long long)(r0 + c) * p.ld_out + co, v);
       }

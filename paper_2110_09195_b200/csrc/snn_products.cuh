@@ -42,23 +42,29 @@ __device__ __forceinline__ void mma_16x8<BF16>(float (&d)[4], uint32_t a0, uint3
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 2^i, from a kernel's parameters: a multiplication by a number that the compiler knows would become a shift.
+// 2, 4 and 8, from a kernel's parameters: a multiplication by a number that the compiler knows would become a shift.
 struct Powers {
-  uint32_t of[16];
+  uint32_t of[4];
 };
-inline Powers powers() {
-  Powers p;
-  for (int i = 0; i < 16; ++i) p.of[i] = 1u << i;
-  return p;
+inline Powers powers() { return Powers{{1, 2, 4, 8}}; }
+__device__ __forceinline__ Powers in_registers(const Powers& p) {
+  Powers r;
+  r.of[0] = 1;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) asm volatile("mov.u32 %0, %1;" : "=r"(r.of[i]) : "r"(p.of[i]));
+  return r;
 }
 // The two weights whose bits lie at 15 - shift and 31 - shift, as 16-bit +1 / -1: a mask, and a multiplication that brings the bits to the
-// signs and adds the ones.  One instruction of the integer units and one of the FMA units; a shift and an exclusive-or are two of the
-// former, which bounded both kernels (65 % busy for 64 tokens over 64 experts).
+// signs and adds the ones (every fourth pair's bits come to the signs by a shift for four pairs).  One instruction of the integer units and
+// one of the FMA units; a shift and an exclusive-or for each are two of the former, which bounded both kernels (65 % busy for 64
+// tokens over 64 experts).
 template <class T>
 __device__ __forceinline__ uint32_t plus_minus(uint32_t w, int shift, const Powers& pow) {
-  if (shift == 0) return (w & 0x80008000u) ^ T::kOne;
+  const uint32_t v = w << (shift & 12);
+  const int rest = shift & 3;
+  if (rest == 0) return (v & 0x80008000u) ^ T::kOne;
   uint32_t r;
-  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(r) : "r"(w & (0x80008000u >> shift)), "r"(pow.of[shift]), "r"(T::kOne));
+  asm("mad.lo.u32 %0, %1, %2, %3;" : "=r"(r) : "r"(v & (0x80008000u >> rest)), "r"(pow.of[rest]), "r"(T::kOne));
   return r;
 }
 

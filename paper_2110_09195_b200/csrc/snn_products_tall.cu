@@ -495,6 +495,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
     // ------------------------------------------------------------ weights: thread m of a warpgroup is channel m of the tile
     const int m = ((int)threadIdx.x - 128) & 127, group = (warp - 4) >> 2;   // blocks group, group + 2, ... of a tile
     const int shift = (m >> 3) & 1 ? 8 : 0;
+    const Powers pow = in_registers(p.pow);
     const uint32_t dst = tmem + ((uint32_t)(m & ~31) << 16);
     uint32_t base = 0;      // blocks of the tiles before
     uint32_t stored = ~0u;  // a block that is on its way to tensor memory; it is waited for when the next one has been expanded
@@ -516,7 +517,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[8 * q + j] = plus_minus<T>(w[i][q], 15 - j, p.pow);
+            for (int j = 0; j < 8; ++j) v[8 * q + j] = plus_minus<T>(w[i][q], 15 - j, pow);
           if (stored != ~0u) {
             tmem_st_wait();
             tc_fence_before();
