@@ -1,4 +1,7 @@
 // Projections of language models: rows of 16-bit activations times +1 / -1 weights, one bit each, grouped by expert.
+#include <cstdlib>
+#include <cstring>
+
 #include "snn_products.h"
 
 #include "snn_products.cuh"
@@ -239,8 +242,13 @@ cudaError_t small_forward(const Products& p, const ProductCall& c, int* launched
 // whatever the number of rows up to 192.  (Measured both ways: one expert of 4096 x 4096, 32 rows 9.8 and 15.6 us, 64 rows 15 and 16; 16
 // of them, 128 rows 41 and 51, 256 rows 65 and 51; 64 of 2048 x 2048, 512 rows 48 and 53, 1024 rows 78 and 54.  With adapters of rank 16, one of
 // 4096 x 4096 and requests of 50 rows, 64 rows 22 and 23, 256 rows 56 and 31; with an adapter for each row 22 and 40, 56 and 71.)
+// SNN_FORCE_ROWS=few or many in the environment takes one of them wherever it can run.
 bool many_rows(const Products& p, const ProductCall& c) {
-  if (c.act_rows < 1) return false;
+  if (c.act_rows < 1) return false;   // (no tensor to describe)
+  if (const char* f = getenv("SNN_FORCE_ROWS")) {
+    if (!strcmp(f, "few")) return false;
+    if (!strcmp(f, "many")) return true;
+  }
   const double pairs = sm_count() / 2.0, used = c.offsets ? min(p.E, c.max_rows) : 1, blocks = (p.C + 63) / 64, rows = fmin(192.0, c.max_rows / used);
   double few = 3.0 + (c.max_rows / 8.0 + (c.offsets ? 0.5 * used : 0.5)) * p.K * (double)p.C / 11e6;
   const double tiles = (c.max_rows < 192 * used ? used : c.max_rows / 192.0) * ((p.K + 255) / 256);
