@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(32 * WARPS) shrink_kernel(const ShrinkParams p
   unsigned todo = __ballot_sync(0xffffffffu, who >= 0 && (int)__ffs(like_me) - 1 == lane);
   const uint16_t* x[NT];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) x[i] = 8 * i + g < n ? p.act + (size_t)(r0 + 8 * i + g) * (size_t)p.ld_act + 16 * t : nullptr;
+  for (int i = 0; i < NT; ++i) x[i] = 8 * i + g < n ? p.act + (size_t)(r0 + 8 * i + g) * (size_t)p.ld_act + 8 * t : nullptr;
   const uint4 zero = make_uint4(0, 0, 0, 0);
   while (todo) {
     const int c = __ffs(todo) - 1, a = __shfl_sync(0xffffffffu, who, c);
@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(32 * WARPS) shrink_kernel(const ShrinkParams p
     todo &= todo - 1;
     const uint16_t* w[2 * MT];
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) w[i] = j0 + 8 * i < p.rank ? p.a + ((size_t)a * p.rank + j0 + 8 * i + g) * p.C + 16 * t : nullptr;
+    for (int i = 0; i < 2 * MT; ++i) w[i] = j0 + 8 * i < p.rank ? p.a + ((size_t)a * p.rank + j0 + 8 * i + g) * p.C + 8 * t : nullptr;
     float acc[MT][NT][4] = {};
     // U blocks of 64 input channels on their way, then their products
     for (int k0 = warp * 64; k0 < p.C; k0 += 64 * WARPS * U) {
@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(32 * WARPS) shrink_kernel(const ShrinkParams p
       for (int v = 0; v < U; ++v)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int k = k0 + 64 * WARPS * v + 8 * h;
-          const bool in = k + 16 * t < p.C;
+          const int k = k0 + 64 * WARPS * v + 32 * h;
+          const bool in = k + 8 * t < p.C;
 #pragma unroll
           for (int i = 0; i < 2 * MT; ++i) u[v][i][h] = in && w[i] ? ld16(w[i] + k) : zero;
 #pragma unroll

@@ -19,14 +19,17 @@ __global__ void products_layout_kernel(const uint32_t* __restrict__ planes, uint
   const int j = 2 * (int)(i & 1) + ((int)(i >> 3) & 1), t = (int)(i >> 1) & 3, g = (int)(i >> 4) & 7;
   const long long tile = i >> 7;
   const int kb = (int)(tile % n_kb), mt = (int)(tile / n_kb);
-  const int c0 = kb * 256 + j * 64 + t * 16;
   uint32_t word = 0;
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int k = mt * 16 + g + 8 * half;
-    if (k >= K || c0 >= C) continue;
-    uint32_t minus = ~(planes[(size_t)(c0 >> 5) * K + k] >> (c0 & 31)) & 0xffffu;
-    if (C - c0 < 16) minus &= (1u << (C - c0)) - 1u;
+    if (k >= K) continue;
+    uint32_t minus = 0;   // (channels come in eights)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = kb * 256 + j * 64 + 32 * q + 8 * t;
+      if (c < C) minus |= (~(planes[(size_t)(c >> 5) * K + k] >> (8 * t)) & 0xffu) << (8 * q);
+    }
 #pragma unroll
     for (int p = 0; p < 8; ++p) word |= (((minus >> (2 * p)) & 1u) | (((minus >> (2 * p + 1)) & 1u) << 16)) << (p + 8 * half);
   }
@@ -102,7 +105,7 @@ __device__ __forceinline__ void find_piece(const Pieces& all, const int32_t* off
 }
 
 // A warp computes 32 MP output channels times 8 rows over a share of the input channels: the weights, the M operand, are expanded from
-// bits in registers, the rows, the N operand, come straight from memory as the instruction wants them (a lane's 16 neighbouring
+// bits in registers, the rows, the N operand, come straight from memory as the instruction wants them (a lane's 16
 // channels are four steps' operands) and stay in registers for all of the warp's output channels (loaded for every 32 of them, they took
 // as many cycles of the L1 cache as the rest).  The warps of a CTA take different input channels (k_warps of them) and different output
 // channels; the former's sums meet in shared memory.  The work, pieces of rows times strips of output channels, is counted on the device and
@@ -137,7 +140,7 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
     const uint16_t* x = nullptr;
     if (g < n) {
       const int row = p.rows ? p.rows[r0 + g] : r0 + g;
-      if (row >= 0 && row < p.act_rows) x = static_cast<const uint16_t*>(p.act) + (size_t)row * (size_t)p.ld_act + 16 * t;
+      if (row >= 0 && row < p.act_rows) x = static_cast<const uint16_t*>(p.act) + (size_t)row * (size_t)p.ld_act + 8 * t;
     }
     const uint2* const bits = reinterpret_cast<const uint2*>(p.bits) + (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
     uint2 w[2][2];   // [tile][odd blocks of 64]
@@ -155,8 +158,8 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int c = kb * 256 + j * 64 + 8 * h;
-          b[j][h] = x && c + 16 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
+          const int c = kb * 256 + j * 64 + 32 * h;
+          b[j][h] = x && c + 8 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
         }
     };
     load_bits(group0, 0, kw);

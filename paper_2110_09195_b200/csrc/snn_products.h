@@ -10,8 +10,10 @@ namespace snn {
 
 // Weights of E projections [K x C], one bit each (set: -1), for both product kernels:
 //   bits [E][n_mt][n_kb][8 g][2 o][4 t][2 i]:  a tile of 16 output channels times 256 input channels is 512 bytes.
-//   Word (g, o, t, i): rows g and g + 8 of the tile, input channels 256 kb + 64 (2 i + o) + 16 t .. + 15, as 16 pairs of
-//   neighbouring channels, pair p of row g in bits p (the even one) and 16 + p, of row g + 8 in bits 8 + p and 24 + p.
+//   Word (g, o, t, i): rows g and g + 8 of the tile, of the 64 input channels from 256 kb + 64 (2 i + o) those from 8 t on and from
+//   32 + 8 t on, eight each, as eight pairs of neighbouring channels: pair p of row g in bits p (the even one) and 16 + p, of row
+//   g + 8 in bits 8 + p and 24 + p.  (Four lanes that load 16 bytes of activations each for their words then read 64 neighbouring bytes: whole
+//   sectors.)
 // (A lane 4g + t of the small kernel's warps reads two times 8 bytes, a thread of the tall kernel's two warpgroups, which take odd and
 // even blocks of 64, twice 16.)
 // A shift and a masked exclusive-or turn a pair into two 16-bit +1 / -1 in one register.  Rows and channels that do not

@@ -517,7 +517,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[8 * q + j] = plus_minus<T>(w[i][q], 15 - j, pow);
+            for (int j = 0; j < 8; ++j) v[(j < 4 ? 0 : 12) + 4 * q + j] = plus_minus<T>(w[i][q], 15 - j, pow);
           if (stored != ~0u) {
             tmem_st_wait();
             tc_fence_before();
