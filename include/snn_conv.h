@@ -298,7 +298,7 @@ SNN_API snn_status_t snn_conv_forward_static(const snn_conv_desc_t* desc, const 
  * SNN_OUT_F16 or SNN_OUT_BF16.  SNN_ACT_BF16, SNN_OUT_F16 and SNN_OUT_BF16 are for these entry points only.
  * Rows lie ld elements apart (ld >= the row's length); rows of activations are 16-byte aligned (pointer, and ld a
  * multiple of 8), rows of outputs aligned to their element.  Weights are +1 / -1, so an infinity or NaN in a row's
- * activations reaches that row's outputs and no others.
+ * activations reaches that row's outputs and no others.  What a call writes overlaps nothing that it reads.
  * All calls are asynchronous on cuda_stream (NULL: the default stream of the handle's device, or of `device`) and
  * allocate nothing; workspaces are the caller's, so calls on different streams, and captured graphs, share nothing
  * but what the caller lets them share.  Calls may overlap.  Errors: INVALID_ARG, UNSUPPORTED, CUDA, TIMEOUT (an
@@ -320,7 +320,8 @@ enum { SNN_OUT_F16 = 3, SNN_OUT_BF16 = 4 };
  * and rows_dev (DEVICE, max_rows ints) are read on the device, so a router's results need not visit the host.
  * offsets must not fall and lie in [0, max_rows]; what lies outside is taken for the nearest end.  An expert may have no rows.
  * Rows of the output below offsets[0] and from offsets[count] on are left as they are.  A row index outside
- * [0, act_rows) stands for a row of zeros.  (max_rows is a bound; only rows that experts have cost time.)
+ * [0, act_rows) stands for a row of zeros.  (max_rows is a bound; only rows that experts have cost time.  UNSUPPORTED: above
+ * 2^30 rows, or where 8 rows times 32 output channels cut the outputs into 2^31 pieces or more.)
  */
 #define SNN_EXPERTS_MAX 1024
 typedef struct snn_conv_experts snn_conv_experts_t; /* opaque; owned by the library */

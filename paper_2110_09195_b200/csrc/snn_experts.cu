@@ -67,7 +67,7 @@ snn_status_t check_rows(const Products& p, const void* act, int act_type, int ac
     return api_fail(SNN_ERR_INVALID_ARG, "rows of %lld activations and %lld outputs (c_in %d, c_out %d; the former a multiple of 8)",
                     (long long)ld_act, (long long)ld_out, p.C, p.K);
   // (the kernels count pieces of rows times strips of channels in 32 bits, whatever the offsets say)
-  if (((long long)rows / 8 + 1) * p.E >= (1ll << 31) || ((long long)rows / 8 + p.E) * ((p.K + 31) / 32) >= (1ll << 31))
+  if (rows > 1 << 30 || ((long long)rows / 8 + 1) * p.E >= (1ll << 31) || ((long long)rows / 8 + p.E) * ((p.K + 31) / 32) >= (1ll << 31))
     return api_fail(SNN_ERR_UNSUPPORTED, "%d rows of %d outputs over %d experts: split the call", rows, p.K, p.E);
   if (rows > 0 && (!out || (act_rows > 0 && !act))) return api_fail(SNN_ERR_INVALID_ARG, "null activation / output pointer");
   if (((uintptr_t)act & 15) || ((uintptr_t)out & (out_size(out_type) - 1)))

@@ -300,7 +300,8 @@ __global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteP
   if (blockIdx.x == 0 && threadIdx.x == 0) p.offsets[p.E] = total;
   __syncthreads();
   place(p, mask, all, t0, tokens);
-  for (int i = total + (int)blockIdx.x * n + (int)threadIdx.x; i < p.T * p.k; i += (int)gridDim.x * n) p.rows[i] = -1;
+  // (behind the last row by a CTA's threads may be behind 2^31)
+  for (long long i = total + (long long)blockIdx.x * n + (int)threadIdx.x; i < (long long)p.T * p.k; i += (long long)gridDim.x * n) p.rows[i] = -1;
 }
 
 // ---------------------------------------------------------------- combine
