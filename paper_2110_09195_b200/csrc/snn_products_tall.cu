@@ -29,18 +29,17 @@ constexpr int TL_D0 = TL_A_STAGES * TL_A_COLS;
 constexpr int TL_HALF = TL_N / 2;      // rows of a CTA
 constexpr int TL_B_BYTES = TL_HALF * 128;
 constexpr int TL_BOX = 32;            // rows of one TMA box
-// warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs (with adapters: 12-19)
+// warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs (with adapters: 3 the MMAs of their terms, 12-19 outputs)
 constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for each of the three warps that copy
-// Stages of rows, and bytes of the tile's rows' A x and of an adapter's B kept beside them (RANK: 0 without adapters, else a bound of
-// their rank).
-template <int RANK>
+// With adapters, for 32 of the rank: an adapter's B, [128 channels][32], and three parts of A x, [96 rows][32] each, as 32-bit values.
+constexpr int TL_LOW_A = 128 * 128, TL_LOW_B = TL_HALF * 128, TL_LOW_PARTS = 3;
+constexpr int TL_LOW_MOST = 8;        // different adapters in a tile, up to which the matrix instructions add them
+template <bool LOW>
 struct TallShape {
-  static constexpr int kStages = RANK == 128 ? 4 : RANK == 64 ? 7 : RANK == 32 ? 12 : RANK == 16 ? 14 : 16;
-  static constexpr int kOutWarps = RANK ? 8 : 4;
+  static constexpr int kStages = LOW ? 14 : 16;
+  static constexpr int kOutWarps = LOW ? 8 : 4;
   static constexpr int kThreads = 384 + 32 * kOutWarps;
-  static constexpr int kH = RANK ? TL_N * (RANK + 4) * 4 : 0;       // fp32, rows in different banks
-  static constexpr bool kWide = RANK <= 64;                          // B as fp32, too; else there is no room
-  static constexpr int kB = RANK ? 256 * (kWide ? (RANK + 4) * 4 : (RANK + 8) * 2) : 0;   // the same; each warp its own
+  static constexpr int kLow = LOW ? TL_LOW_A + TL_LOW_PARTS * TL_LOW_B : 0;   // bytes
 };
 
 // The same value in all lanes, known to be so
@@ -60,10 +59,9 @@ struct TallParams {
 };
 
 struct TallBars {
-  uint64_t b_full[16], b_empty[16], a_full[TL_A_STAGES], a_empty[TL_A_STAGES], d_full[2], d_empty[2], drain;
-  uint32_t tmem, pad;
-  int who[TL_N];         // adapters of the tile's rows, below 0: none
-  int group[TL_N / 8];   // of eight rows
+  uint64_t b_full[16], b_empty[16], a_full[TL_A_STAGES], a_empty[TL_A_STAGES], d_full[2], d_empty[2], drain, low_full, low_done;
+  uint32_t tmem;
+  int odd;   // some adapter's B had an infinity or NaN
 };
 
 // Issued by the lanes for which `on` is not 0: D[256 x N] (+)= A[256 x 64] * B[N x 64]^T in four steps of 16, A in tensor memory, then the
@@ -91,6 +89,24 @@ __device__ __forceinline__ void commit_on(uint32_t bar, uint32_t on) {
       "r"(on), "h"((uint16_t)3)
       : "memory");
 }
+// Up to four steps of 8 of the rank: D[256 x N] += B[256 x 8 steps] * H[N x 8 steps]^T, both 32-bit values of 10 bits (tf32) in shared memory.
+__device__ __forceinline__ void low_ss_tf32(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t steps, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q, q1, q2, q3;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "setp.ne.u32 q, %5, 0;\n\tsetp.gt.and.u32 q1, %4, 1, q;\n\tsetp.gt.and.u32 q2, %4, 2, q;\n\tsetp.gt.and.u32 q3, %4, 3, q;\n\t"
+      "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
+      "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::tf32 [%0], %1, %2, %3, 1;\n\t"
+      "@q1 tcgen05.mma.cta_group::2.kind::tf32 [%0], a1, b1, %3, 1;\n\t"
+      "@q2 tcgen05.mma.cta_group::2.kind::tf32 [%0], a2, b2, %3, 1;\n\t"
+      "@q3 tcgen05.mma.cta_group::2.kind::tf32 [%0], a3, b3, %3, 1;\n\t}" ::"r"(d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(steps), "r"(on)
+      : "memory");
+}
+// Rows of 128 bytes, the 16-byte pieces of eight rows in turn (the layout that TMA writes the rows of activations in)
+__device__ __forceinline__ uint64_t rows_desc(uint32_t addr) {
+  return ((uint64_t)2 << 61) | ((uint64_t)1 << 46) | ((uint64_t)64 << 32) | ((uint64_t)1 << 16) | (addr >> 4);
+}
 // 32 columns of the warp's 32 lanes; they are there after tmem_st_wait
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
   asm volatile(
@@ -102,16 +118,15 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// 8 columns of the warp's 32 lanes, a thread (g = lane / 4, t = lane % 4): columns 2t and 2t + 1 of lanes g and g + 8 (first four values),
-// g + 16 and g + 24.  Loads and wait are one statement.
-__device__ __forceinline__ void tmem_ld_16x8(uint32_t taddr, float (&v)[2][4]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%8];\n\t"
-      "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%4,%5,%6,%7}, [%9];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=f"(v[0][0]), "=f"(v[0][1]), "=f"(v[0][2]), "=f"(v[0][3]), "=f"(v[1][0]), "=f"(v[1][1]), "=f"(v[1][2]), "=f"(v[1][3])
-      : "r"(taddr), "r"(taddr + (16u << 16))
-      : "memory");
+// 4 columns; load and wait are one statement
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&v)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];\n\ttcgen05.wait::ld.sync.aligned;"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&v)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 // (the barrier: the pair's first CTA's)
 __device__ __forceinline__ void tma_rows(uint32_t dst, const void* map, int c, int row, uint32_t bar) {
@@ -189,131 +204,56 @@ __device__ __forceinline__ void store_column(O* out, long long ld, int n, float 
     if (c < n) to_out(out, alpha * __uint_as_float(v[c]));
 }
 
-// 32 channels from co0, up to 8 rows from r0, in the layout of tmem_ld_16x8.  16-bit outputs change hands first: a thread then has four
-// neighbouring channels of a row (twice), eight threads a row's 32 bytes.
-__device__ __forceinline__ uint32_t pack_out(int type, float lo, float hi) {
-  uint32_t r;
-  if (type == SNN_OUT_F16) {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    memcpy(&r, &h, 4);
-  } else {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    memcpy(&r, &h, 4);
-  }
-  return r;
-}
-__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
-  uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
-}
-__device__ __forceinline__ void store_16x8(const TallParams& p, int r0, int n, int co0, const float (&v)[2][4]) {
-  const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  if (p.out_type == SNN_OUT_F32) {
-    float* const out = static_cast<float*>(p.out) + (long long)(r0 + 2 * q) * p.ld_out + co0 + g;
+// The adapters of a tile's rows, by a warp: lane l has rows l, l + 32, ...; -1 for none.
+constexpr int NO_MORE = 0x7fffffff;
+struct Adapters {
+  int of[TL_N / 32];
+  __device__ __forceinline__ void load(const Lowrank& low, const Tile& t) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (2 * q + (i & 1) < n && co0 + g + 8 * (i >> 1) < p.K) out[(i & 1) * p.ld_out + 8 * (i >> 1)] = v[i >> 2][i & 3];
-    return;
-  }
-  uint32_t w[4];   // row g, channels 8 i + 2 q and the next
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = transpose_8x8(pack_out(p.out_type, v[i >> 1][2 * (i & 1)], v[i >> 1][2 * (i & 1) + 1]));
-#pragma unroll
-  for (int i = 0; i < 4; i += 2) {
-    // an even q gives its pair of the second eight for its neighbour's of the first
-    const uint32_t other = __shfl_xor_sync(0xffffffffu, q & 1 ? w[i] : w[i + 1], 1);
-    const uint32_t lo = q & 1 ? other : w[i], hi = q & 1 ? w[i + 1] : other;
-    const int co = co0 + 8 * (i + (q & 1)) + 2 * (q & 2);
-    if (g < n && co < p.K) {
-      uint16_t* const out = static_cast<uint16_t*>(p.out) + (long long)(r0 + g) * p.ld_out + co;
-      if (co + 4 <= p.K && ((uintptr_t)out & 7) == 0) {
-        *reinterpret_cast<uint2*>(out) = make_uint2(lo, hi);
-      } else {
-        const uint16_t part[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (co + k < p.K) out[k] = part[k];
-      }
+    for (int i = 0; i < TL_N / 32; ++i) {
+      const int a = lane + 32 * i < t.n ? low.adapter[t.r0 + lane + 32 * i] : -1;
+      of[i] = a < low.n ? a : -1;
     }
   }
-}
+  // the least above `a` (-1: the first), or NO_MORE
+  __device__ __forceinline__ int after(int a) const {
+    int least = NO_MORE;
+#pragma unroll
+    for (int i = 0; i < TL_N / 32; ++i)
+      if (of[i] > a) least = min(least, of[i]);
+    return __reduce_min_sync(0xffffffffu, least);
+  }
+  // how many there are, up to TL_LOW_MOST + 1
+  __device__ __forceinline__ int count() const {
+    int n = 0;
+    for (int a = after(-1); a != NO_MORE && n <= TL_LOW_MOST; a = after(a)) ++n;
+    return n;
+  }
+};
 
-// B (A x) in fp32 on the FMA units, two of the rank at a time, in the layout of tmem_ld_16x8: a thread has four channels and two rows of
-// eight, so that a value from shared memory serves two or four products.  Two warps for each 32 channels, which take turns at eight rows: one
-// alone is bound by latency, 142 us for 4096 rows of 4096 x 4096 and rank 32.  (On the warp's matrix instruction, with A x in three 16-bit or
-// two tf32 parts, each instruction waited for one of the pair's: 72 to 96 cycles.  With a channel a thread, and a load of A x for every two
-// products: 163 us.)
-__device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(d) : "l"(a), "l"(b)); }
-__device__ __forceinline__ uint64_t pack2(float2 v) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
-  return r;
-}
-__device__ __forceinline__ float sum2(uint64_t v) {
-  float a, b;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
-  return a + b;
-}
-// 8 of the rank: b, of channels g, g + 8, g + 16, g + 24 (16-bit values, or pairs of fp32 values as they are in shared memory, which saves
-// as many instructions as the products take); h, of rows 2t and 2t + 1, h_row floats apart
+// B (A x) of one output, of the rank's places where B is an infinity or NaN.
 template <class T>
-__device__ __forceinline__ void lowrank_step(uint64_t (&d)[2][4], const uint4 (&b)[4], const float* h, int h_row) {
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    ulonglong2 x[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = *reinterpret_cast<const ulonglong2*>(h + i * h_row + 4 * half);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const uint64_t w0 = pack2(T::unpack(half ? b[c].z : b[c].x)), w1 = pack2(T::unpack(half ? b[c].w : b[c].y));
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fma2(d[i][c], w0, x[i].x);
-        fma2(d[i][c], w1, x[i].y);
-      }
-    }
+__device__ float lowrank_odd_term(const Lowrank& low, int K, int row, int co) {
+  const int a = low.adapter[row];
+  if (a < 0 || a >= low.n) return 0.f;
+  const uint16_t* b = static_cast<const uint16_t*>(low.b) + ((size_t)a * K + co) * low.rank;
+  const float* h = low.h + (size_t)row * low.rank;
+  float s = 0.f;
+  for (int j = 0; j < low.rank; ++j) {
+    const float v = T::unpack(b[j]).x;
+    if (!isfinite(v)) s = fmaf(v, h[j], s);
   }
-}
-__device__ __forceinline__ ulonglong2 lds16(uint32_t addr) {
-  ulonglong2 v;
-  asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "r"(addr));
-  return v;
-}
-// (addresses in shared memory; all loads before the first product: beside the pair's MMAs a load takes over a hundred cycles)
-__device__ __forceinline__ void lowrank_step_wide(uint64_t (&d)[2][4], uint32_t b, uint32_t b_row, uint32_t h, uint32_t h_row) {
-  ulonglong2 x[2][2], w[4][2];
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) x[i][half] = lds16(h + i * h_row + 16 * half);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) w[c][half] = lds16(b + 8 * c * b_row + 16 * half);
-  }
-#pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fma2(d[i][c], w[c][half].x, x[i][half].x);
-        fma2(d[i][c], w[c][half].y, x[i][half].y);
-      }
-}
-// ... added to the outputs of the rows whose bit is set
-__device__ __forceinline__ void add_lowrank(float (&v)[2][4], const uint64_t (&d)[2][4], uint32_t which) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if ((which >> (i & 1)) & 1u) v[i >> 2][i & 3] += sum2(d[i & 1][i >> 1]);
+  return s;
 }
 
-// RANK: 0 without adapters, else a bound of their rank.
-template <class T, bool GATHER, int RANK>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kThreads, 1) products_tall_kernel(const TallParams p, const __grid_constant__ CUtensorMap map) {
-  constexpr int STAGES = TallShape<RANK>::kStages;
+template <class T, bool GATHER, bool LOW>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThreads, 1) products_tall_kernel(const TallParams p, const __grid_constant__ CUtensorMap map) {
+  constexpr int STAGES = TallShape<LOW>::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  TallBars* const bars = reinterpret_cast<TallBars*>(smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH + TallShape<RANK>::kB);
+  uint8_t* const low_smem = smem + STAGES * TL_B_BYTES;
+  TallBars* const bars = reinterpret_cast<TallBars*>(low_smem + TallShape<LOW>::kLow);
   Ranges R;
   R.lo = reinterpret_cast<int*>(bars + 1);
   R.n = R.lo + p.E;
@@ -323,7 +263,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
   const int rank = (int)(blockIdx.x & 1), first_tile = (int)(blockIdx.x >> 1), n_pairs = (int)(gridDim.x >> 1);
   // As in the kernel for few rows: after the one that writes A x, only the warps that read it wait.
   if (warp == 0) {
-    if (!RANK) grid_dep_wait();
+    if (!LOW) grid_dep_wait();
     // tiles of each expert, summed up: every lane a run of experts
     const int per = (p.E + 31) >> 5, e0 = lane * per, e1 = min(p.E, e0 + per);
     int count = 0;
@@ -353,18 +293,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&bars->d_full[i]), 1);
-      mbar_init(smem_u32(&bars->d_empty[i]), 2 * TallShape<RANK>::kOutWarps);
+      mbar_init(smem_u32(&bars->d_empty[i]), 2 * TallShape<LOW>::kOutWarps + (LOW ? 1 : 0));
     }
+    mbar_init(smem_u32(&bars->low_full), 2 * TallShape<LOW>::kOutWarps);
+    mbar_init(smem_u32(&bars->low_done), 1);
+    bars->odd = 0;
     mbar_init(smem_u32(&bars->drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   } else if (warp == 2) {
     // (not before the kernel before has ended: it may still have to get tensor memory of its own)
-    if (!RANK) grid_dep_wait();
+    if (!LOW) grid_dep_wait();
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars->tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  if (!RANK || warp >= 12) grid_dep_wait();
+  if (!LOW || warp >= 12 || warp == 3) grid_dep_wait();
   tc_fence_before();
   __syncthreads();
   pair_sync();
@@ -470,8 +413,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->b_full[s]), b_phase) && mbar_wait(smem_u32(&bars->a_full[a]), a_phase));
         if (!ok) break;
         tc_fence_after();
-        const uint64_t desc = ((uint64_t)2 << 61) | ((uint64_t)1 << 46) | ((uint64_t)64 << 32) | ((uint64_t)1 << 16) | ((b_smem + s * TL_B_BYTES) >> 4);
-        stage_ts_f16(acc, tmem_u + a * TL_A_COLS, desc, idesc, kb ? 1u : 0u, smem_u32(&bars->b_empty[s]), smem_u32(&bars->a_empty[a]), leader);
+        stage_ts_f16(acc, tmem_u + a * TL_A_COLS, rows_desc(b_smem + s * TL_B_BYTES), idesc, kb ? 1u : 0u, smem_u32(&bars->b_empty[s]), smem_u32(&bars->a_empty[a]), leader);
         __syncwarp();
         if (++s == STAGES) {
           s = 0;
@@ -491,6 +433,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
     __syncwarp();
     ok = mbar_wait(smem_u32(&bars->drain), 0) && ok;
     if (!ok && lane == 0) raise_status(p.status, 22);
+  } else if (LOW && warp == 3 && rank == 0) {
+    // ------------------------------------------------------------ MMA of the adapters' terms, for both CTAs
+    int d = 0;
+    uint32_t d_phase = 0, passes = 0;
+    const uint32_t leader = elect_one(), low_u = (uint32_t)uni((int)smem_u32(low_smem)), tmem_u = (uint32_t)uni((int)tmem);
+    Adapters who;
+    for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
+      who.load(p.low, t);
+      const uint32_t n32 = (uint32_t)(t.n + 31) & ~31u;
+      const uint32_t idesc = (1u << 4) | (2u << 7) | (2u << 10) | ((n32 >> 3) << 17) | ((256u >> 4) << 24);
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), d_phase));
+      if (who.count() <= TL_LOW_MOST) {
+        for (int a = who.after(-1); ok && a != NO_MORE; a = who.after(a))
+          for (int j = 0; j < p.low.rank; j += 32) {
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->low_full), passes & 1u));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t steps = (uint32_t)min(4, (p.low.rank - j) / 8);
+#pragma unroll
+            for (int part = 0; part < TL_LOW_PARTS; ++part)
+              low_ss_tf32(tmem_u + TL_D0 + d * TL_N, rows_desc(low_u), rows_desc(low_u + TL_LOW_A + part * TL_LOW_B), idesc, steps, leader);
+            commit_on(smem_u32(&bars->low_done), leader);
+            __syncwarp();
+            ++passes;
+          }
+      }
+      if (!ok) break;
+      __syncwarp();
+      if (lane == 0) arrive_at_first(smem_u32(&bars->d_empty[d]));
+      if ((d ^= 1) == 0) d_phase ^= 1u;
+    }
+    if (passes) ok = mbar_wait(smem_u32(&bars->low_done), (passes - 1) & 1u) && ok;
+    if (!ok && lane == 0) raise_status(p.status, 25);
   } else if (warp >= 4 && warp < 12) {
     // ------------------------------------------------------------ weights: thread m of a warpgroup is channel m of the tile
     const int m = ((int)threadIdx.x - 128) & 127, group = (warp - 4) >> 2;   // blocks group, group + 2, ... of a tile
@@ -542,123 +517,122 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<RANK>::kTh
     if (!ok && lane == 0) raise_status(p.status, 23);
   } else if (warp >= 12) {
     // ------------------------------------------------------------ outputs: thread m is channel m of the tile, a column is a row
-    const int m = ((int)threadIdx.x - 384) & 127, turn = (warp - 12) >> 2;
-    constexpr int OUTS = 32 * TallShape<RANK>::kOutWarps;
-    constexpr bool WIDE = TallShape<RANK>::kWide;
-    const int h_row = p.low.rank + 4, b_row = p.low.rank + (WIDE ? 4 : 8);   // (elements)
-    float* const h_smem = reinterpret_cast<float*>(smem + STAGES * TL_B_BYTES);
-    uint8_t* const b_smem_warp = smem + STAGES * TL_B_BYTES + TallShape<RANK>::kH + (warp - 12) * 32 * b_row * (WIDE ? 4 : 2);
-    float* const b_wide = reinterpret_cast<float*>(b_smem_warp);
-    uint16_t* const b_narrow = reinterpret_cast<uint16_t*>(b_smem_warp);
-    int *const who = bars->who, *const group = bars->group;
-    constexpr int MIXED = -2;
+    const int thread = (int)threadIdx.x - 384, m = thread & 127, turn = (warp - 12) >> 2;
+    constexpr int OUTS = 32 * TallShape<LOW>::kOutWarps, STEP = OUTS / 4;   // columns: 32 for each set of four warps in turn
     int d = 0;
-    uint32_t phase = 0;
+    uint32_t phase = 0, low_phase = 0;
+    // 32 of an adapter's B, of this CTA's channels, and of A x, of its rows (zeros: those of other adapters), as the instruction wants them
+    auto fill = [&](int a, int j0) {
+      const int n_rank = p.low.rank, chunks = min(4, (n_rank - j0) / 8), half = ((t.n + 31) & ~31) / 2;
+      const uint16_t* const b = static_cast<const uint16_t*>(p.low.b) + (size_t)a * p.K * n_rank + j0;
+      for (int i = thread; i < 128 * chunks; i += OUTS) {
+        const int row = i / chunks, c = i - row * chunks, co = t.ct * 128 + row;
+        const uint4 u = co < p.K ? ld16(b + (size_t)co * n_rank + 8 * c) : make_uint4(0, 0, 0, 0);
+        const float2 f[4] = {T::unpack(u.x), T::unpack(u.y), T::unpack(u.z), T::unpack(u.w)};
+        float v[8];
+        bool fine = true;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          v[q] = q & 1 ? f[q >> 1].y : f[q >> 1].x;
+          if (!isfinite(v[q])) {
+            v[q] = 0.f;   // (would reach the rows of other adapters; added by itself afterwards)
+            fine = false;
+          }
+        }
+        if (!fine) bars->odd = 1;
+        uint8_t* const to = low_smem + row * 128;
+        *reinterpret_cast<float4*>(to + (((2 * c) ^ (row & 7)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(to + (((2 * c + 1) ^ (row & 7)) << 4)) = make_float4(v[4], v[5], v[6], v[7]);
+      }
+      for (int i = thread; i < half * 2 * chunks; i += OUTS) {
+        const int row = i / (2 * chunks), c = i - row * 2 * chunks, at = rank * half + row;
+        uint4 h = make_uint4(0, 0, 0, 0);
+        if (at < t.n && p.low.adapter[t.r0 + at] == a) h = ld16(p.low.h + (size_t)(t.r0 + at) * n_rank + j0 + 4 * c);
+        uint32_t v[4] = {h.x, h.y, h.z, h.w};
+        // 11 bits of each value at a time (the differences are exact); an infinity or NaN in the first
+        uint8_t* const to = low_smem + TL_LOW_A + row * 128 + ((c ^ (row & 7)) << 4);
+#pragma unroll
+        for (int part = 0; part < TL_LOW_PARTS; ++part) {
+          uint32_t top[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            top[q] = v[q] & 0xffffe000u;
+            const float rest = __uint_as_float(v[q]) - __uint_as_float(top[q]);
+            v[q] = isfinite(rest) ? __float_as_uint(rest) : 0u;
+          }
+          *reinterpret_cast<uint4*>(to + part * TL_LOW_B) = make_uint4(top[0], top[1], top[2], top[3]);
+        }
+      }
+    };
     for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
       const int co = t.ct * 128 + m;
-      const float alpha = p.alpha[(size_t)t.e * p.n_mt * 16 + co];
-      int held = -1;
-      if (RANK) {   // the rows' adapters and A x, while the sums are under way
-        const int quads = p.low.rank / 4;
-        for (int i = (int)threadIdx.x - 384; i < t.n * quads; i += OUTS)
-          copy16(smem_u32(h_smem + (i / quads) * h_row + 4 * (i % quads)), p.low.h + (size_t)t.r0 * p.low.rank + 4 * i, true);
-        copy_commit();
-        for (int i = (int)threadIdx.x - 384; i < TL_N; i += OUTS) {
-          const int a = i < t.n ? p.low.adapter[t.r0 + i] : -1, one = a >= 0 && a < p.low.n ? a : -1;
-          who[i] = one;
-          // the adapter that the eight rows around this one have (those behind the last count with it)
-          const int lead = __shfl_sync(0xffffffffu, one, lane & 24);
-          const unsigned same = __ballot_sync(0xffffffffu, one == lead || i >= t.n);
-          if ((i & 7) == 0) group[i >> 3] = ((same >> (lane & 24)) & 255u) == 255u ? lead : MIXED;
-        }
-        copy_wait<0>();
+      float alpha = p.alpha[(size_t)t.e * p.n_mt * 16 + co];
+      Adapters who;
+      int n_low = 0, first = NO_MORE;
+      if (LOW) {   // while the sums are under way
+        who.load(p.low, t);
+        n_low = who.count();
+        first = who.after(-1);
+        if (n_low && n_low <= TL_LOW_MOST) fill(first, 0);
       }
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), phase));
-      if (RANK) ok = bar_all<1, OUTS>(ok);   // (everybody's part of A x has landed; the warps go on, or give up, together)
-      if (!ok) break;
       tc_fence_after();
       const uint32_t src = tmem + ((uint32_t)(m & ~31) << 16) + TL_D0 + d * TL_N;
-      const long long first = (long long)t.r0 * p.ld_out + co;
-      if (RANK == 0) {
-        for (int c0 = 0; c0 < t.n; c0 += 32) {
-          uint32_t v[32];
-          tmem_ld32(src + c0, v);
-          const int n = co < p.K ? min(32, t.n - c0) : 0;
-          const long long at = first + c0 * p.ld_out;
-          if (p.out_type == SNN_OUT_F32) store_column(static_cast<float*>(p.out) + at, p.ld_out, n, alpha, v);
-          else if (p.out_type == SNN_OUT_F16) store_column(static_cast<__half*>(p.out) + at, p.ld_out, n, alpha, v);
-          else store_column(static_cast<__nv_bfloat16*>(p.out) + at, p.ld_out, n, alpha, v);
-          __syncwarp();
-        }
-      } else {
-        // Eight rows at a time.  Rows of one request lie together, so they mostly have one adapter: its B stays in shared memory until the
-        // next one's.  Else there is a pass for each of their adapters.
-        const int n_rank = p.low.rank, g = lane >> 2, q = lane & 3, co0 = t.ct * 128 + (m & ~31);
-        float scale[4];
+      if (LOW) {
+        if (ok && n_low) {   // alpha S, back in place
+          for (int c0 = 32 * turn; c0 < t.n; c0 += STEP) {
+            uint32_t v[32];
+            tmem_ld32(src + c0, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) scale[i] = __shfl_sync(0xffffffffu, alpha, 8 * i + g);
-        const uint16_t* const b_all = static_cast<const uint16_t*>(p.low.b);
-        const size_t b_size = (size_t)p.K * n_rank;
-        for (int c0 = 8 * turn; c0 < t.n; c0 += 16) {
-          float v[2][4];
-          tmem_ld_16x8(src + c0, v);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] *= scale[i >> 1];
-          const float* const h = h_smem + (c0 + 2 * q) * h_row;
-          const int a = group[c0 >> 3];   // (the same for the whole warp)
-          if (a >= 0) {
-            if (a != held) {
-              held = a;
-              __syncwarp();
-              const int chunks = n_rank / 8, all = min(32, p.K - co0) * chunks;
-              for (int i = lane; i < all; i += 32) {
-                const uint4 u = ld16(b_all + a * b_size + (size_t)co0 * n_rank + 8 * i);
-                const int at = (i / chunks) * b_row + 8 * (i % chunks);
-                if (WIDE) {
-                  const float2 f0 = T::unpack(u.x), f1 = T::unpack(u.y), f2 = T::unpack(u.z), f3 = T::unpack(u.w);
-                  *reinterpret_cast<float4*>(b_wide + at) = make_float4(f0.x, f0.y, f1.x, f1.y);
-                  *reinterpret_cast<float4*>(b_wide + at + 4) = make_float4(f2.x, f2.y, f3.x, f3.y);
-                } else {
-                  *reinterpret_cast<uint4*>(b_narrow + at) = u;
-                }
-              }
-              __syncwarp();
-            }
-            uint64_t low[2][4] = {};
-#pragma unroll 1
-            for (int j = 0; j < n_rank; j += 8) {
-              if (WIDE) {
-                lowrank_step_wide(low, smem_u32(b_wide + g * b_row + j), 4u * (uint32_t)b_row, smem_u32(h + j), 4u * (uint32_t)h_row);
-              } else {
-                uint4 b[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = *reinterpret_cast<const uint4*>(b_narrow + (8 * i + g) * b_row + j);
-                lowrank_step<T>(low, b, h + j, h_row);
-              }
-            }
-            add_lowrank(v, low, 3u);
-          } else if (a == MIXED) {
-            const int mine = lane < 8 ? who[c0 + lane] : -1;
-            unsigned left = __ballot_sync(0xffffffffu, mine >= 0);
-            while (left) {
-              const int one = __shfl_sync(0xffffffffu, mine, __ffs(left) - 1);
-              const unsigned same = __ballot_sync(0xffffffffu, mine == one);
-              left &= ~same;
-              uint64_t low[2][4] = {};
-#pragma unroll 2
-              for (int j = 0; j < n_rank; j += 8) {
-                uint4 b[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = ld16(b_all + one * b_size + (size_t)min(co0 + 8 * i + g, p.K - 1) * n_rank + j);
-                lowrank_step<T>(low, b, h + j, h_row);
-              }
-              // (rows are apart: what other rows' A x gives with this B goes nowhere)
-              add_lowrank(v, low, (same >> (2 * q)) & 3u);
-            }
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(alpha * __uint_as_float(v[i]));
+            tmem_st32(src + c0, v);
           }
-          store_16x8(p, t.r0 + c0, t.n - c0, co0, v);
+          tmem_st_wait();
         }
-        bar_sync_some<1, OUTS>();   // (everybody has read A x)
+        if (n_low) alpha = 1.f;
+        if (n_low <= TL_LOW_MOST) {
+          for (int a = first; ok && a != NO_MORE; a = who.after(a))
+            for (int j = 0; ok && j < p.low.rank; j += 32) {
+              if (a != first || j) fill(a, j);
+              fence_proxy_async();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) arrive_at_first(smem_u32(&bars->low_full));
+              ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->low_done), low_phase));
+              low_phase ^= 1u;
+              tc_fence_after();
+            }
+        }
+        ok = bar_all<1, OUTS>(ok);   // (the warps go on, or give up, together; and all have said what is odd)
+        if (ok && n_low && (n_low > TL_LOW_MOST || *reinterpret_cast<volatile int*>(&bars->odd))) {
+          for (int c0 = 32 * turn; c0 < t.n; c0 += STEP)
+            for (int c = c0; c < min(c0 + 32, t.n); c += 4) {
+              uint32_t v[4];
+              tmem_ld4(src + c, v);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (co < p.K && c + i < t.n) {
+                  const int row = t.r0 + c + i;
+                  const float term = n_low > TL_LOW_MOST ? lowrank_term<T>(p.low, p.K, row, co) : lowrank_odd_term<T>(p.low, p.K, row, co);
+                  v[i] = __float_as_uint(__uint_as_float(v[i]) + term);
+                }
+              __syncwarp();
+              tmem_st4(src + c, v);
+            }
+          tmem_st_wait();
+        }
+      }
+      if (!ok) break;
+      const long long to = (long long)t.r0 * p.ld_out + co;
+      for (int c0 = 32 * turn; c0 < t.n; c0 += STEP) {
+        uint32_t v[32];
+        tmem_ld32(src + c0, v);
+        const int n = co < p.K ? min(32, t.n - c0) : 0;
+        const long long at = to + c0 * p.ld_out;
+        if (p.out_type == SNN_OUT_F32) store_column(static_cast<float*>(p.out) + at, p.ld_out, n, alpha, v);
+        else if (p.out_type == SNN_OUT_F16) store_column(static_cast<__half*>(p.out) + at, p.ld_out, n, alpha, v);
+        else store_column(static_cast<__nv_bfloat16*>(p.out) + at, p.ld_out, n, alpha, v);
+        __syncwarp();
       }
       tc_fence_before();
       __syncwarp();
@@ -693,27 +667,24 @@ MapEncoder map_encoder() {
   return f;
 }
 
-template <class T, bool GATHER, int RANK>
+template <class T, bool GATHER, bool LOW>
 cudaError_t tall_launch(const Products& p, const ProductCall& c, const CUtensorMap& map, int* launched) {
   static unsigned long long done = 0;
-  cudaError_t e = allow_max_smem(products_tall_kernel<T, GATHER, RANK>, &done);
+  cudaError_t e = allow_max_smem(products_tall_kernel<T, GATHER, LOW>, &done);
   if (e != cudaSuccess) return e;
   const TallParams q{p.bits, p.alpha, static_cast<const uint16_t*>(c.act), c.rows, c.offsets, c.out, c.ld_act, c.ld_out, c.act_rows, c.max_rows, p.E, p.C, p.K, p.n_mt, p.n_kb, c.out_type,
                      (p.K + 255) / 256, p.status_dev, c.low, powers()};
   const long long tiles = ((long long)c.max_rows / TL_N + (c.offsets ? min(p.E, c.max_rows) : 1)) * q.n_cp;
-  const size_t smem = 1024 + TallShape<RANK>::kStages * TL_B_BYTES + TallShape<RANK>::kH + TallShape<RANK>::kB + sizeof(TallBars) + (size_t)p.E * 12;
+  const size_t smem = 1024 + TallShape<LOW>::kStages * TL_B_BYTES + TallShape<LOW>::kLow + sizeof(TallBars) + (size_t)p.E * 12;
   *launched += 1;
-  return launch_dependent(products_tall_kernel<T, GATHER, RANK>, 2u * (unsigned)min(tiles, (long long)max(1, sm_count() / 2)), TallShape<RANK>::kThreads, smem,
+  return launch_dependent(products_tall_kernel<T, GATHER, LOW>, 2u * (unsigned)min(tiles, (long long)max(1, sm_count() / 2)), TallShape<LOW>::kThreads, smem,
                           c.stream, q, map);
 }
 
 template <class T>
 cudaError_t tall_kind(const Products& p, const ProductCall& c, const CUtensorMap& map, int* launched) {
-  if (!c.low.adapter) return c.rows ? tall_launch<T, true, 0>(p, c, map, launched) : tall_launch<T, false, 0>(p, c, map, launched);
-  if (c.low.rank <= 16) return tall_launch<T, false, 16>(p, c, map, launched);
-  if (c.low.rank <= 32) return tall_launch<T, false, 32>(p, c, map, launched);
-  if (c.low.rank <= 64) return tall_launch<T, false, 64>(p, c, map, launched);
-  return tall_launch<T, false, 128>(p, c, map, launched);
+  if (c.low.adapter) return tall_launch<T, false, true>(p, c, map, launched);
+  return c.rows ? tall_launch<T, true, false>(p, c, map, launched) : tall_launch<T, false, false>(p, c, map, launched);
 }
 
 }  // namespace
