@@ -38,7 +38,11 @@ __global__ void __launch_bounds__(32 * WARPS) shrink_kernel(const ShrinkParams p
 #pragma unroll
   for (int i = 0; i < NT; ++i) x[i] = 8 * i + g < n ? p.act + (size_t)(r0 + 8 * i + g) * (size_t)p.ld_act + 8 * t : nullptr;
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  while (todo) {
+  for (int pass = 0; todo; ++pass) {
+    if (pass % (int)gridDim.z != (int)blockIdx.z) {
+      todo &= todo - 1;
+      continue;
+    }
     const int c = __ffs(todo) - 1, a = __shfl_sync(0xffffffffu, who, c);
     const unsigned same = __shfl_sync(0xffffffffu, like_me, c);
     todo &= todo - 1;
@@ -97,7 +101,7 @@ cudaError_t shrink_launch(const ShrinkParams& p, cudaStream_t s) {
   static unsigned long long done = 0;
   const cudaError_t e = allow_max_smem(shrink_kernel<T, NT, MT, U, WARPS>, &done);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT)));
+  const dim3 grid((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT)), NT > 1 ? 2u : 1u);
   return launch_dependent(shrink_kernel<T, NT, MT, U, WARPS>, grid, 32 * WARPS, (size_t)WARPS * 8 * NT * (16 * MT + 1) * 4, s, p);
 }
 
@@ -106,7 +110,8 @@ cudaError_t shrink_type(ShrinkParams p, cudaStream_t s) {
   const int sms = sm_count();
   if (p.rows >= 16 * sms) {
     p.per_cta = 32;
-    return p.rank > 16 ? shrink_launch<T, 4, 2, 1, 16>(p, s) : shrink_launch<T, 4, 1, 1, 16>(p, s);
+    if (p.rank > 32) return shrink_launch<T, 4, 4, 1, 8>(p, s);
+    return p.rank > 16 ? shrink_launch<T, 4, 2, 1, 16>(p, s) : shrink_launch<T, 4, 1, 2, 16>(p, s);
   }
   p.per_cta = max(1, min(8, p.rows / sms));
   return shrink_launch<T, 1, 1, 4, 8>(p, s);

@@ -31,15 +31,16 @@ constexpr int TL_B_BYTES = TL_HALF * 128;
 constexpr int TL_BOX = 32;            // rows of one TMA box
 // warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs (with adapters: 3 the MMAs of their terms, 12-19 outputs)
 constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for each of the three warps that copy
-// With adapters, for 32 of the rank: an adapter's B, [128 channels][32], and three parts of A x, [96 rows][32] each, as 32-bit values.
-constexpr int TL_LOW_A = 128 * 128, TL_LOW_B = TL_HALF * 128, TL_LOW_PARTS = 3;
-constexpr int TL_LOW_MOST = 8;        // different adapters in a tile, up to which the matrix instructions add them
+// With adapters, for 32 of the rank: their B, [128 channels][32], and three parts of A x, [96 rows][32] each, as 32-bit values; twice, so
+// that the next are written while the matrix instructions read these.
+constexpr int TL_LOW_A = 128 * 128, TL_LOW_B = TL_HALF * 128, TL_LOW_PARTS = 3, TL_LOW_BYTES = TL_LOW_A + TL_LOW_PARTS * TL_LOW_B;
+constexpr int TL_LOW_MOST = 24;       // different adapters in a tile, up to which the matrix instructions add them
 template <bool LOW>
 struct TallShape {
-  static constexpr int kStages = LOW ? 14 : 16;
+  static constexpr int kStages = LOW ? 10 : 16;
   static constexpr int kOutWarps = LOW ? 8 : 4;
   static constexpr int kThreads = 384 + 32 * kOutWarps;
-  static constexpr int kLow = LOW ? TL_LOW_A + TL_LOW_PARTS * TL_LOW_B : 0;   // bytes
+  static constexpr int kLow = LOW ? 2 * TL_LOW_BYTES : 0;   // bytes
 };
 
 // The same value in all lanes, known to be so
@@ -59,7 +60,7 @@ struct TallParams {
 };
 
 struct TallBars {
-  uint64_t b_full[16], b_empty[16], a_full[TL_A_STAGES], a_empty[TL_A_STAGES], d_full[2], d_empty[2], drain, low_full, low_done;
+  uint64_t b_full[16], b_empty[16], a_full[TL_A_STAGES], a_empty[TL_A_STAGES], d_full[2], d_empty[2], drain, low_full[2], low_done[2];
   uint32_t tmem;
   int odd;   // some adapter's B had an infinity or NaN
 };
@@ -232,6 +233,53 @@ struct Adapters {
   }
 };
 
+// The passes in which the adapters' terms are added: 32 of an adapter's rank at a time, or, of ranks up to 16, as many adapters as fit into 32;
+// for the rows from the first to the last that has one of them, in 32s.
+struct Passes {
+  int rank, each, a[4], n, j, row0, rows;
+  __device__ __forceinline__ bool take(const Adapters& who, int after) {
+    j = n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      a[i] = i < each && after != NO_MORE ? who.after(after) : NO_MORE;
+      after = a[i];
+      if (after != NO_MORE) ++n;
+    }
+    const int lane = threadIdx.x & 31;
+    int lo = TL_N, hi = -1;
+#pragma unroll
+    for (int i = 0; i < TL_N / 32; ++i) {
+      const int o = who.of[i];
+      if (o >= 0 && (o == a[0] || o == a[1] || o == a[2] || o == a[3])) {
+        lo = min(lo, lane + 32 * i);
+        hi = lane + 32 * i;
+      }
+    }
+    row0 = __reduce_min_sync(0xffffffffu, lo) & ~31;
+    rows = ((__reduce_max_sync(0xffffffffu, hi) + 32) & ~31) - row0;
+    return n > 0;
+  }
+  __device__ __forceinline__ bool begin(const Adapters& who, int r) {
+    rank = r;
+    each = r <= 16 ? 32 / r : 1;
+    return take(who, -1);
+  }
+  __device__ __forceinline__ bool next(const Adapters& who) {
+    if (each == 1 && j + 32 < rank) {
+      j += 32;
+      return true;
+    }
+    return take(who, each == 1 ? a[0] : each == 2 ? a[1] : a[3]);
+  }
+  // eights of the rank in this pass, and the adapter and place of one of them
+  __device__ __forceinline__ int eights() const { return each == 1 ? min(4, (rank - j) / 8) : n * rank / 8; }
+  __device__ __forceinline__ int adapter(int c) const {
+    const int i = each == 1 ? 0 : each == 2 ? c >> 1 : c;
+    return i == 0 ? a[0] : i == 1 ? a[1] : i == 2 ? a[2] : a[3];
+  }
+  __device__ __forceinline__ int place(int c) const { return each == 1 ? j + 8 * c : each == 2 ? 8 * (c & 1) : 0; }
+};
+
 // B (A x) of one output, of the rank's places where B is an infinity or NaN.
 template <class T>
 __device__ float lowrank_odd_term(const Lowrank& low, int K, int row, int co) {
@@ -295,8 +343,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
       mbar_init(smem_u32(&bars->d_full[i]), 1);
       mbar_init(smem_u32(&bars->d_empty[i]), 2 * TallShape<LOW>::kOutWarps + (LOW ? 1 : 0));
     }
-    mbar_init(smem_u32(&bars->low_full), 2 * TallShape<LOW>::kOutWarps);
-    mbar_init(smem_u32(&bars->low_done), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&bars->low_full[i]), 2 * TallShape<LOW>::kOutWarps);
+      mbar_init(smem_u32(&bars->low_done[i]), 1);
+    }
     bars->odd = 0;
     mbar_init(smem_u32(&bars->drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -439,32 +489,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
     uint32_t d_phase = 0, passes = 0;
     const uint32_t leader = elect_one(), low_u = (uint32_t)uni((int)smem_u32(low_smem)), tmem_u = (uint32_t)uni((int)tmem);
     Adapters who;
+    Passes pass;
     for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
       who.load(p.low, t);
-      const uint32_t n32 = (uint32_t)(t.n + 31) & ~31u;
-      const uint32_t idesc = (1u << 4) | (2u << 7) | (2u << 10) | ((n32 >> 3) << 17) | ((256u >> 4) << 24);
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), d_phase));
       if (who.count() <= TL_LOW_MOST) {
-        for (int a = who.after(-1); ok && a != NO_MORE; a = who.after(a))
-          for (int j = 0; j < p.low.rank; j += 32) {
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->low_full), passes & 1u));
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t steps = (uint32_t)min(4, (p.low.rank - j) / 8);
+        for (bool more = pass.begin(who, p.low.rank); ok && more; more = pass.next(who), ++passes) {
+          const uint32_t slot = passes & 1u, b = low_u + slot * TL_LOW_BYTES;
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->low_full[slot]), passes >> 1 & 1u));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t idesc = (1u << 4) | (2u << 7) | (2u << 10) | ((uint32_t)(pass.rows >> 3) << 17) | ((256u >> 4) << 24);
 #pragma unroll
-            for (int part = 0; part < TL_LOW_PARTS; ++part)
-              low_ss_tf32(tmem_u + TL_D0 + d * TL_N, rows_desc(low_u), rows_desc(low_u + TL_LOW_A + part * TL_LOW_B), idesc, steps, leader);
-            commit_on(smem_u32(&bars->low_done), leader);
-            __syncwarp();
-            ++passes;
-          }
+          for (int part = 0; part < TL_LOW_PARTS; ++part)
+            low_ss_tf32(tmem_u + TL_D0 + d * TL_N + pass.row0, rows_desc(b), rows_desc(b + TL_LOW_A + part * TL_LOW_B), idesc, (uint32_t)pass.eights(), leader);
+          commit_on(smem_u32(&bars->low_done[slot]), leader);
+          __syncwarp();
+        }
       }
       if (!ok) break;
       __syncwarp();
       if (lane == 0) arrive_at_first(smem_u32(&bars->d_empty[d]));
       if ((d ^= 1) == 0) d_phase ^= 1u;
     }
-    if (passes) ok = mbar_wait(smem_u32(&bars->low_done), (passes - 1) & 1u) && ok;
+    if (passes) ok = mbar_wait(smem_u32(&bars->low_done[(passes - 1) & 1u]), (passes - 1) >> 1 & 1u) && ok;
     if (!ok && lane == 0) raise_status(p.status, 25);
   } else if (warp >= 4 && warp < 12) {
     // ------------------------------------------------------------ weights: thread m of a warpgroup is channel m of the tile
@@ -520,15 +568,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
     const int thread = (int)threadIdx.x - 384, m = thread & 127, turn = (warp - 12) >> 2;
     constexpr int OUTS = 32 * TallShape<LOW>::kOutWarps, STEP = OUTS / 4;   // columns: 32 for each set of four warps in turn
     int d = 0;
-    uint32_t phase = 0, low_phase = 0;
-    // 32 of an adapter's B, of this CTA's channels, and of A x, of its rows (zeros: those of other adapters), as the instruction wants them
-    auto fill = [&](int a, int j0) {
-      const int n_rank = p.low.rank, chunks = min(4, (n_rank - j0) / 8), half = ((t.n + 31) & ~31) / 2;
-      const uint16_t* const b = static_cast<const uint16_t*>(p.low.b) + (size_t)a * p.K * n_rank + j0;
-      for (int i = thread; i < 128 * chunks; i += OUTS) {
-        const int row = i / chunks, c = i - row * chunks, co = t.ct * 128 + row;
-        const uint4 u = co < p.K ? ld16(b + (size_t)co * n_rank + 8 * c) : make_uint4(0, 0, 0, 0);
-        const float2 f[4] = {T::unpack(u.x), T::unpack(u.y), T::unpack(u.z), T::unpack(u.w)};
+    uint32_t phase = 0, passes = 0;
+    // A pass's B, of this CTA's channels, and A x, of its half of the rows (zeros: those of other adapters): from memory, and as the instruction
+    // wants them.
+    uint4 u[128 * 4 / OUTS], h[TL_HALF * 8 / OUTS];
+    auto load = [&](const Passes& pass) {
+      const int eights = pass.eights(), half = pass.rows / 2;
+#pragma unroll
+      for (int i = 0; i < 128 * 4 / OUTS; ++i) {
+        const int row = (thread + i * OUTS) >> 2, c = thread & 3, co = t.ct * 128 + row;
+        u[i] = make_uint4(0, 0, 0, 0);
+        if (c < eights && co < p.K) u[i] = ld16(static_cast<const uint16_t*>(p.low.b) + ((size_t)pass.adapter(c) * p.K + co) * pass.rank + pass.place(c));
+      }
+#pragma unroll
+      for (int i = 0; i < TL_HALF * 8 / OUTS; ++i) {
+        const int row = (thread + i * OUTS) >> 3, c = thread & 7, at = pass.row0 + rank * half + row;
+        h[i] = make_uint4(0, 0, 0, 0);
+        if (row < half && at < t.n && (c >> 1) < eights && p.low.adapter[t.r0 + at] == pass.adapter(c >> 1))
+          h[i] = ld16(p.low.h + (size_t)(t.r0 + at) * pass.rank + pass.place(c >> 1) + 4 * (c & 1));
+      }
+    };
+    auto store = [&](int half, uint32_t slot) {
+      uint8_t* const to = low_smem + slot * TL_LOW_BYTES;
+#pragma unroll
+      for (int i = 0; i < 128 * 4 / OUTS; ++i) {
+        const int row = (thread + i * OUTS) >> 2, c = thread & 3;
+        const float2 f[4] = {T::unpack(u[i].x), T::unpack(u[i].y), T::unpack(u[i].z), T::unpack(u[i].w)};
         float v[8];
         bool fine = true;
 #pragma unroll
@@ -540,17 +605,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
           }
         }
         if (!fine) bars->odd = 1;
-        uint8_t* const to = low_smem + row * 128;
-        *reinterpret_cast<float4*>(to + (((2 * c) ^ (row & 7)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(to + (((2 * c + 1) ^ (row & 7)) << 4)) = make_float4(v[4], v[5], v[6], v[7]);
+        *reinterpret_cast<float4*>(to + row * 128 + (((2 * c) ^ (row & 7)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(to + row * 128 + (((2 * c + 1) ^ (row & 7)) << 4)) = make_float4(v[4], v[5], v[6], v[7]);
       }
-      for (int i = thread; i < half * 2 * chunks; i += OUTS) {
-        const int row = i / (2 * chunks), c = i - row * 2 * chunks, at = rank * half + row;
-        uint4 h = make_uint4(0, 0, 0, 0);
-        if (at < t.n && p.low.adapter[t.r0 + at] == a) h = ld16(p.low.h + (size_t)(t.r0 + at) * n_rank + j0 + 4 * c);
-        uint32_t v[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+      for (int i = 0; i < TL_HALF * 8 / OUTS; ++i) {
+        const int row = (thread + i * OUTS) >> 3, c = thread & 7;
+        if (row >= half) break;
+        uint32_t v[4] = {h[i].x, h[i].y, h[i].z, h[i].w};
         // 11 bits of each value at a time (the differences are exact); an infinity or NaN in the first
-        uint8_t* const to = low_smem + TL_LOW_A + row * 128 + ((c ^ (row & 7)) << 4);
 #pragma unroll
         for (int part = 0; part < TL_LOW_PARTS; ++part) {
           uint32_t top[4];
@@ -560,22 +623,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
             const float rest = __uint_as_float(v[q]) - __uint_as_float(top[q]);
             v[q] = isfinite(rest) ? __float_as_uint(rest) : 0u;
           }
-          *reinterpret_cast<uint4*>(to + part * TL_LOW_B) = make_uint4(top[0], top[1], top[2], top[3]);
+          *reinterpret_cast<uint4*>(to + TL_LOW_A + part * TL_LOW_B + row * 128 + ((c ^ (row & 7)) << 4)) = make_uint4(top[0], top[1], top[2], top[3]);
         }
       }
     };
+    // (the slot is free once the pass before the last has been added)
+    auto slot_free = [&] { return __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->low_done[passes & 1u]), (passes >> 1 & 1u) ^ 1u)); };
     for (int index = first_tile; ok && tall_tile(R, p.E, p.n_cp, index, rank, t); index += n_pairs) {
       const int co = t.ct * 128 + m;
       float alpha = p.alpha[(size_t)t.e * p.n_mt * 16 + co];
       Adapters who;
-      int n_low = 0, first = NO_MORE;
+      Passes pass;
+      int n_low = 0;
       if (LOW) {   // while the sums are under way
         who.load(p.low, t);
         n_low = who.count();
-        first = who.after(-1);
-        if (n_low && n_low <= TL_LOW_MOST) fill(first, 0);
+        if (n_low && n_low <= TL_LOW_MOST) {
+          pass.begin(who, p.low.rank);
+          load(pass);
+          ok = slot_free();
+          if (ok) store(pass.rows / 2, passes & 1u);
+        }
       }
-      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), phase));
+      ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(&bars->d_full[d]), phase));
       tc_fence_after();
       const uint32_t src = tmem + ((uint32_t)(m & ~31) << 16) + TL_D0 + d * TL_N;
       if (LOW) {
@@ -590,18 +660,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
           tmem_st_wait();
         }
         if (n_low) alpha = 1.f;
-        if (n_low <= TL_LOW_MOST) {
-          for (int a = first; ok && a != NO_MORE; a = who.after(a))
-            for (int j = 0; ok && j < p.low.rank; j += 32) {
-              if (a != first || j) fill(a, j);
-              fence_proxy_async();
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) arrive_at_first(smem_u32(&bars->low_full));
-              ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->low_done), low_phase));
-              low_phase ^= 1u;
-              tc_fence_after();
+        if (n_low && n_low <= TL_LOW_MOST) {
+          for (bool more = true; ok && more;) {   // (this pass is in its slot)
+            const uint32_t slot = passes++ & 1u;
+            fence_proxy_async();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at_first(smem_u32(&bars->low_full[slot]));
+            more = pass.next(who);
+            if (more) {
+              load(pass);
+              ok = slot_free();
+              if (ok) store(pass.rows / 2, passes & 1u);
             }
+          }
+          ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(&bars->low_done[(passes - 1) & 1u]), (passes - 1) >> 1 & 1u));
+          tc_fence_after();
         }
         ok = bar_all<1, OUTS>(ok);   // (the warps go on, or give up, together; and all have said what is odd)
         if (ok && n_low && (n_low > TL_LOW_MOST || *reinterpret_cast<volatile int*>(&bars->odd))) {
