@@ -18,8 +18,9 @@ struct ShrinkParams {
 
 // A CTA takes up to 8 NT neighbouring rows and 16 MT of the rank; its warps take different input channels, and their sums meet in shared
 // memory.  One pass for each adapter that the rows have (rows of one request lie together: mostly one); the rows of other adapters are
-// computed along and not written.  Bound by reading A: once for each CTA, so with few rows a CTA has few of them, and all of A's
-// readers run at once; with many rows 32, and A comes from L2.
+// computed along and not written.  The CTAs of a column of the grid have the same rows and take their adapters in turn: mostly only the first has
+// any, and where two requests meet neither CTA takes twice as long as the rest (4096 rows of 4096, rank 32: 17.7 us, with one CTA after the other 25.3).
+// Bound by reading A and x, each CTA both, mostly from L2 and 16 bytes a lane at a time.
 template <class T, int NT, int MT, int U, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS) shrink_kernel(const ShrinkParams p) {
   constexpr int N = 8 * NT, M = 16 * MT;
@@ -96,15 +97,21 @@ __global__ void __launch_bounds__(32 * WARPS) shrink_kernel(const ShrinkParams p
   }
 }
 
+constexpr unsigned SH_TURNS = 4;
+
 template <class T, int NT, int MT, int U, int WARPS>
 cudaError_t shrink_launch(const ShrinkParams& p, cudaStream_t s) {
   static unsigned long long done = 0;
   const cudaError_t e = allow_max_smem(shrink_kernel<T, NT, MT, U, WARPS>, &done);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT)), NT > 1 ? 2u : 1u);
+  const dim3 grid((unsigned)((p.rows + p.per_cta - 1) / p.per_cta), (unsigned)((p.rank + 16 * MT - 1) / (16 * MT)), NT > 1 ? SH_TURNS : 1u);
   return launch_dependent(shrink_kernel<T, NT, MT, U, WARPS>, grid, 32 * WARPS, (size_t)WARPS * 8 * NT * (16 * MT + 1) * 4, s, p);
 }
 
+// How many rows and how much of the rank a CTA takes: the more, the less is read again; as long as there are CTAs for all SMs.  (4096 rows of
+// 4096 values, rank 64: 16 of the rank and 32 rows 36 us, 32 and 32 30 us, 64 and 32 26 us; 1000 rows: 16 and 6 19 us, 32 and 16 13 us,
+// 16 and 32 16 us; 500 rows: 16 and 3 14.4 us, 32 and 16 8.5 us; rank 16 and 4096 rows, two blocks of input channels on their way 13.7 us,
+// one 14.6.)
 template <class T>
 cudaError_t shrink_type(ShrinkParams p, cudaStream_t s) {
   const int sms = sm_count();
@@ -112,6 +119,10 @@ cudaError_t shrink_type(ShrinkParams p, cudaStream_t s) {
     p.per_cta = 32;
     if (p.rank > 32) return shrink_launch<T, 4, 4, 1, 8>(p, s);
     return p.rank > 16 ? shrink_launch<T, 4, 2, 1, 16>(p, s) : shrink_launch<T, 4, 1, 2, 16>(p, s);
+  }
+  if (p.rows >= 2 * sms) {
+    p.per_cta = 16;
+    return shrink_launch<T, 2, 2, 1, 16>(p, s);
   }
   p.per_cta = max(1, min(8, p.rows / sms));
   return shrink_launch<T, 1, 1, 4, 8>(p, s);

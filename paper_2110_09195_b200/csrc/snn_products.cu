@@ -243,8 +243,10 @@ cudaError_t small_forward(const Products& p, const ProductCall& c, int* launched
 // Which kernel, by the time that each would take on 148 SMs (us).  Few rows: each piece of 8 expands all of its expert's weights, 11 G
 // weights a ms.  Many rows: tiles of 256 output channels in turns of a tile for each pair of SMs, 0.16 to 0.24 us for 64 input channels,
 // whatever the number of rows up to 192.  (Measured both ways: one expert of 4096 x 4096, 32 rows 9.8 and 15.6 us, 64 rows 15 and 16; 16
-// of them, 128 rows 41 and 51, 256 rows 65 and 51; 64 of 2048 x 2048, 512 rows 48 and 53, 1024 rows 78 and 54.  With adapters of rank 16, one of
-// 4096 x 4096 and requests of 50 rows, 64 rows 22 and 23, 256 rows 56 and 31; with an adapter for each row 22 and 40, 56 and 71.)
+// of them, 128 rows 41 and 51, 256 rows 65 and 51; 64 of 2048 x 2048, 512 rows 48 and 53, 1024 rows 78 and 54.  With adapters the
+// time of many rows depends on how many adapters the rows of a tile have, which the host does not know: 16 adapters on 4096 x 4096, requests of
+// 50 rows, rank 16, 64 rows 22 and 21, 128 rows 37 and 25, rank 64 31 and 26, 56 and 35; an adapter for each row, rank 16 21 and 30, 36 and 35,
+// rank 64 31 and 56, 55 and 69.)
 // SNN_FORCE_ROWS=few or many in the environment takes one of them wherever it can run.
 bool many_rows(const Products& p, const ProductCall& c) {
   if (c.act_rows < 1) return false;   // (no tensor to describe)
@@ -257,8 +259,8 @@ bool many_rows(const Products& p, const ProductCall& c) {
   const double tiles = (c.max_rows < 192 * used ? used : c.max_rows / 192.0) * ((p.K + 255) / 256);
   double many = 5.5 + blocks * (tiles <= pairs ? 0.16 + 0.0002 * rows : tiles / pairs * (0.2 + 0.0002 * rows));
   if (c.low.adapter) {
-    few += 0.02 * c.max_rows;
-    many += 6.0 + 0.04 * rows;
+    few += 8.5e-7 * c.max_rows * c.low.rank * p.K;
+    many += 2.0 + (0.04 + 0.003 * c.low.rank) * rows;
   }
   return many < few;
 }

@@ -21,7 +21,16 @@ namespace {
 // half.  TMA brings the rows; rows named by an index come by 16-byte asynchronous copies of three warps (TMA's gather of four rows an
 // instruction took 2900 cycles for 192 rows of 128 bytes, seven times the instructions that they feed).
 // 512 columns: four stages of weights (32 columns each) and two accumulators of 192, so that one is written out while the next is
-// being summed.
+// being summed.  (4096 rows, one expert of 4096 x 4096, bf16: 88 us, 1550 TFLOP/s; 8192 rows by an index 1360 TFLOP/s over 8 such experts.)
+//
+// With adapters, D = alpha S + B (A x), A x in fp32 from the kernel before: the warps of the outputs multiply the sums by alpha in place, in
+// tensor memory, and the matrix instructions add the second term, as tf32: B's 16-bit values are such numbers, and A x is the sum of three (11
+// bits each, so that nothing is rounded).  A pass adds 32 of the rank, of one adapter or of several small ones, to the rows between the first and the
+// last that have them; rows of others have zeros there.  Two slots: the warps write the next pass's operands while this one is being added.  On
+// the FMA units, from shared memory, the same took longer than the sums themselves (4096 rows of 4096 x 4096 and rank 32 141 us, now 111;
+// rank 64 208 and 123, rank 128 312 and 149); as 16-bit or tf32 products of the warps' own matrix instruction each waited for one of the
+// pair's, 72 to 96 cycles.  Tiles with more than TL_LOW_MOST adapters, nearly one for each row, take the FMA units all the same (rank 16: 36 us a
+// tile, a pass 1.5 us, two adapters in each; 4096 rows, an adapter of 32 for each row 344 and 415 us, of 100 575 and 466).
 constexpr int TL_N = 192;             // rows of a tile, at most
 constexpr int TL_A_STAGES = 4;
 constexpr int TL_A_COLS = 32;         // 64 input channels, two to a column
@@ -34,7 +43,7 @@ constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for
 // With adapters, for 32 of the rank: their B, [128 channels][32], and three parts of A x, [96 rows][32] each, as 32-bit values; twice, so
 // that the next are written while the matrix instructions read these.
 constexpr int TL_LOW_A = 128 * 128, TL_LOW_B = TL_HALF * 128, TL_LOW_PARTS = 3, TL_LOW_BYTES = TL_LOW_A + TL_LOW_PARTS * TL_LOW_B;
-constexpr int TL_LOW_MOST = 24;       // different adapters in a tile, up to which the matrix instructions add them
+constexpr int TL_LOW_MOST = 48;       // different adapters in a tile, up to which the matrix instructions add them
 template <bool LOW>
 struct TallShape {
   static constexpr int kStages = LOW ? 10 : 16;
