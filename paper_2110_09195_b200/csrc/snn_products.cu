@@ -222,22 +222,26 @@ long long most_pieces(const Products& p, const ProductCall& c) {
 }
 
 template <class T, int MP>
-cudaError_t small_launch(const Products& p, const ProductCall& c, int* launched) {
-  SmallParams q{p.bits, p.alpha, c.act, c.rows, c.offsets, c.out, c.ld_act, c.ld_out, c.act_rows, c.max_rows, p.E, p.C, p.K, p.n_mt, p.n_kb,
-                c.out_type, 8, c.low, powers()};
-  // all warps on one strip of output channels, unless there are not so many blocks of 256 input channels: small pieces of work
-  while (q.k_warps > p.n_kb) q.k_warps /= 2;
-  const int width = 32 * MP * (8 / q.k_warps);
+cudaError_t small_launch(const Products& p, const ProductCall& c, int k_warps, unsigned ctas, int* launched) {
+  const SmallParams q{p.bits, p.alpha, c.act, c.rows, c.offsets, c.out, c.ld_act, c.ld_out, c.act_rows, c.max_rows, p.E, p.C, p.K, p.n_mt, p.n_kb,
+                      c.out_type, k_warps, c.low, powers()};
   *launched += 1;
-  return launch_dependent(products_small_kernel<T, MP>, (unsigned)min(2ll * sm_count(), most_pieces(p, c) * ((p.K + width - 1) / width)), 256, 0, c.stream, q);
+  return launch_dependent(products_small_kernel<T, MP>, ctas, 256, 0, c.stream, q);
 }
 
 template <class T>
 cudaError_t small_forward(const Products& p, const ProductCall& c, int* launched) {
-  // 64 output channels a warp where that leaves work for the SMs (one token over an expert of 4096 x 4096: 5.6 us with 32, 6.6 with 64; 32
-  // tokens 11.4 and 9.8; 64 tokens over 64 experts of 2048 x 2048 39 and 33)
-  if (2 * most_pieces(p, c) * (p.K / 64) >= 3ll * sm_count()) return small_launch<T, 2>(p, c, launched);
-  return small_launch<T, 1>(p, c, launched);
+  // all warps on one strip of output channels, unless there are not so many blocks of 256 input channels: small pieces of work
+  int k_warps = 8;
+  while (k_warps > p.n_kb) k_warps /= 2;
+  // 32 or 64 output channels a warp: a strip of 64 takes 1.86 times as long as one of 32, and what counts is how many of them a CTA has one
+  // after the other (one expert of 4096 x 4096: 16 rows 6.7 us with 32, 32 rows 10.5 and 9.8, 48 rows 14.2 and 16.3, 64 rows 17.7 and
+  // 16.4; 64 tokens over 64 experts of 2048 x 2048 39 and 33)
+  const long long ctas = 2ll * sm_count(), pieces = most_pieces(p, c);
+  auto items = [&](int m) { return pieces * ((p.K + 8 / k_warps * m - 1) / (8 / k_warps * m)); };
+  auto turns = [&](int m) { return (items(m) + ctas - 1) / ctas; };
+  if (186 * turns(64) <= 100 * turns(32)) return small_launch<T, 2>(p, c, k_warps, (unsigned)min(ctas, items(64)), launched);
+  return small_launch<T, 1>(p, c, k_warps, (unsigned)min(ctas, items(32)), launched);
 }
 
 // Which kernel, by the time that each would take on 148 SMs (us).  Few rows: each piece of 8 expands all of its expert's weights, 11 G
