@@ -12,12 +12,14 @@ namespace {
 constexpr int RT_BLOCK = 64;   // tokens of a CTA: two words of a mask for each expert
 constexpr int RT_CHOOSE_WARPS = 32;   // two tokens a warp
 constexpr int RT_WARPS = 16;
-constexpr int RT_DIRECT = 32;         // CTAs up to which each adds up the others' counts by itself (8191 tokens, 128 CTAs: 20.8 us; 16385 with sums of their own 18.3)
+// CTAs up to which each adds up the others' counts by itself (128 experts, 8 each, 4000 tokens 9.4 us, with sums in a launch of their own 11.6; 6000
+// tokens 10.7 and 12.1; 8191 tokens 16.9 and 12.7).
+constexpr int RT_DIRECT = 96;
 
 struct RouteParams {
   const void* logits;
   long long ld;
-  int type, T, E, k, normalise;
+  int type, T, E, k, normalise, direct;
   int32_t* ids;
   float* weights;
   int32_t *offsets, *rows, *slots, *work;
@@ -179,8 +181,8 @@ __device__ __forceinline__ void place(const RouteParams& p, const uint32_t* mask
   }
 }
 
-// First launch: each CTA's tokens choose, and the CTA counts its choices of each expert.  With one CTA that is all there is to count, and it
-// goes on to place them.
+// First launch: each CTA's tokens choose, and the CTA counts its choices of each expert, in bytes where every CTA of the last launch reads all
+// of them.  With one CTA that is all there is to count, and it goes on to place them.
 template <int V>
 __global__ void __launch_bounds__(RT_CHOOSE_WARPS * 32) route_choose_kernel(const RouteParams p) {
   const int threads = (int)blockDim.x;
@@ -205,10 +207,15 @@ __global__ void __launch_bounds__(RT_CHOOSE_WARPS * 32) route_choose_kernel(cons
   }
   __syncthreads();
   const bool alone = gridDim.x == 1;
+  auto chosen = [&](int e) { return e < p.E ? __popc(mask[2 * e]) + __popc(mask[2 * e + 1]) : 0; };   // (at most 64)
+  if (!alone && p.direct) {
+    for (int w = threadIdx.x; 4 * w < p.E; w += threads)
+      p.work[(size_t)blockIdx.x * ((p.E + 3) / 4) + w] = chosen(4 * w) | chosen(4 * w + 1) << 8 | chosen(4 * w + 2) << 16 | chosen(4 * w + 3) << 24;
+    return;
+  }
   for (int e = threadIdx.x; e < p.E; e += threads) {
-    const int n = __popc(mask[2 * e]) + __popc(mask[2 * e + 1]);
-    if (alone) count[e] = n;
-    else p.work[(size_t)blockIdx.x * p.E + e] = n;
+    if (alone) count[e] = chosen(e);
+    else p.work[(size_t)blockIdx.x * p.E + e] = chosen(e);
   }
   if (!alone) return;
   __syncthreads();
@@ -252,7 +259,7 @@ __global__ void __launch_bounds__(1024) route_sum_kernel(int32_t* work, int E, i
 
 // Last launch: where the experts' rows begin, and where this CTA's begin among them (all CTAs' counts, added up here if `direct`), then its
 // tokens' rows and slots.
-__global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteParams p, int direct) {
+__global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteParams p) {
   extern __shared__ int sm[];
   int* const all = sm;                                                 // [E]
   int* const before = sm + p.E;                                        // [E]
@@ -267,23 +274,31 @@ __global__ void __launch_bounds__(RT_WARPS * 32) route_place_kernel(const RouteP
     const int id = p.ids[(size_t)t0 * p.k + i], local = i / p.k;
     if (id >= 0) atomicOr(mask + 2 * id + (local >> 5), 1u << (local & 31));
   }
-  if (direct) {
-    // a thread has an expert and every `turns`-th CTA, eight loads on their way; the turns' sums meet (whole numbers: any order gives the same)
-    const int width = (min(p.E, n) + 31) & ~31, turns = n / width, turn = (int)threadIdx.x / width;
-    for (int e = (int)threadIdx.x - turn * width; turn < turns && e < p.E; e += width) {
-      int sum = 0, mine = 0;
+  if (p.direct) {
+    // a thread has four experts and every `turns`-th CTA, eight loads on their way, two sums in a register; the turns' sums meet (whole numbers:
+    // any order gives the same)
+    const int words = (p.E + 3) / 4, width = (words + 31) & ~31, turns = n / width, turn = (int)threadIdx.x / width, w = (int)threadIdx.x - turn * width;
+    if (turn < turns && w < words) {
+      uint32_t sum[2] = {}, mine[2] = {};   // experts 4w and 4w + 2, 4w + 1 and 4w + 3
       for (int b0 = turn; b0 < (int)gridDim.x; b0 += 8 * turns) {
-        int v[8];
+        uint32_t v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = b0 + i * turns < (int)gridDim.x ? p.work[(size_t)(b0 + i * turns) * p.E + e] : 0;
+        for (int i = 0; i < 8; ++i) v[i] = b0 + i * turns < (int)gridDim.x ? (uint32_t)p.work[(size_t)(b0 + i * turns) * words + w] : 0u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          sum += v[i];
-          if (b0 + i * turns < (int)blockIdx.x) mine += v[i];
-        }
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t two = (v[i] >> (8 * h)) & 0x00ff00ffu;
+            sum[h] += two;
+            if (b0 + i * turns < (int)blockIdx.x) mine[h] += two;
+          }
       }
-      atomicAdd(all + e, sum);
-      atomicAdd(before + e, mine);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (4 * w + i < p.E) {
+          atomicAdd(all + 4 * w + i, (int)((sum[i & 1] >> (8 * (i & 2))) & 0xffffu));
+          atomicAdd(before + 4 * w + i, (int)((mine[i & 1] >> (8 * (i & 2))) & 0xffffu));
+        }
     }
   } else {
     for (int e = threadIdx.x; e < p.E; e += n) {
@@ -445,9 +460,10 @@ long long route_work_bytes(int T, int E) {
 }
 
 cudaError_t route_forward(const RouteCall& c, int* launched) {
-  const RouteParams p{c.logits, c.ld, c.type, c.T, c.E, c.k, c.normalise, c.ids, c.weights, c.offsets, c.rows, c.slots, c.work};
   // (no tokens: one CTA writes the offsets)
   const unsigned blocks = (unsigned)max(1ll, (c.T + (long long)RT_BLOCK - 1) / RT_BLOCK);
+  const bool direct = blocks <= RT_DIRECT;
+  const RouteParams p{c.logits, c.ld, c.type, c.T, c.E, c.k, c.normalise, direct, c.ids, c.weights, c.offsets, c.rows, c.slots, c.work};
   const int v = (c.E + 31) / 32, threads = 32 * min(RT_CHOOSE_WARPS, max(4, c.T));   // (few tokens: a small CTA begins sooner)
   cudaError_t e;
 #define SNN_CHOOSE(V) e = launch_dependent(route_choose_kernel<V>, blocks, threads, 0, c.stream, p)
@@ -460,14 +476,13 @@ cudaError_t route_forward(const RouteCall& c, int* launched) {
 #undef SNN_CHOOSE
   *launched += 1;
   if (e != cudaSuccess || blocks == 1) return e;
-  const bool direct = blocks <= RT_DIRECT;
   if (!direct) {
     e = launch_dependent(route_sum_kernel, (unsigned)((c.E + 31) / 32), 1024, 0, c.stream, c.work, c.E, (int)blocks);
     *launched += 1;
     if (e != cudaSuccess) return e;
   }
   *launched += 1;
-  return launch_dependent(route_place_kernel, blocks, RT_WARPS * 32, (size_t)c.E * 16, c.stream, p, (int)direct);
+  return launch_dependent(route_place_kernel, blocks, RT_WARPS * 32, (size_t)c.E * 16, c.stream, p);
 }
 
 cudaError_t combine_forward(const CombineCall& c, int* launched) {

@@ -161,3 +161,23 @@ def test_branches_of_one_graph(snn):
             _check_route(captured[i][0], logits[i], k, True)
             assert torch.equal(captured[i][1], alone[1]) and torch.equal(captured[i][2], alone[2])
         assert torch.equal(captured[2], captured[0][2] + captured[1][2])
+
+
+@pytest.mark.parametrize("T", [128, 6143, 6144, 6145, 9999])
+@pytest.mark.parametrize("E,k", [(1, 1), (3, 2), (37, 4), (130, 8), (1023, 3)])
+def test_counts_of_many_groups_of_tokens(snn, T, E, k):
+    """Up to 96 groups of 64 tokens every group adds up the others' counts, four experts' in a word; beyond, a launch of their own does."""
+    g = _gen(T + E)
+    logits = torch.rand(T, E, generator=g, device="cuda").argsort(1).float()   # (no two equal in a row)
+    logits[torch.rand(T, generator=g, device="cuda") < 0.1] = float("-inf")    # (nobody for a tenth of the tokens)
+    r = snn.route(logits, k)
+    able = torch.isfinite(logits[:, 0])
+    ids = torch.sort(logits, dim=1, descending=True).indices[:, :k]
+    assert torch.equal(r.ids, torch.where(able[:, None], ids, -1).to(torch.int32))
+    key = torch.where(able[:, None], ids, E).reshape(-1)
+    order, n = torch.sort(key, stable=True).indices, int(able.sum()) * k
+    assert torch.equal(r.rows[:n], (order[:n] // k).to(torch.int32)) and (r.rows[n:] == -1).all()
+    assert torch.equal(r.offsets[1:], torch.cumsum(torch.bincount(key, minlength=E + 1)[:E], 0).to(torch.int32)) and r.offsets[0] == 0
+    slots = torch.full((T * k,), -1, device="cuda")
+    slots[order[:n]] = torch.arange(n, device="cuda")
+    assert torch.equal(r.slots.reshape(-1), slots.to(torch.int32))
