@@ -28,8 +28,8 @@ namespace {
 // tensor memory, and the matrix instructions add the second term, as tf32: B's 16-bit values are such numbers, and A x is the sum of three (11
 // bits each, so that nothing is rounded).  A pass adds 32 of the rank, of one adapter or of several small ones, to the rows between the first and the
 // last that have them; rows of others have zeros there.  Two slots: the warps write the next pass's operands while this one is being added.  On
-// the FMA units, from shared memory, the same took longer than the sums themselves (4096 rows of 4096 x 4096 and rank 32 141 us, now 111;
-// rank 64 208 and 123, rank 128 312 and 149); as 16-bit or tf32 products of the warps' own matrix instruction each waited for one of the
+// the FMA units, from shared memory, the same took longer than the sums themselves (4096 rows of 4096 x 4096 and rank 32 141 us, now 106;
+// rank 64 208 and 122, rank 128 312 and 149); as 16-bit or tf32 products of the warps' own matrix instruction each waited for one of the
 // pair's, 72 to 96 cycles.  Tiles with more than TL_LOW_MOST adapters, nearly one for each row, take the FMA units all the same (rank 16: 36 us a
 // tile, a pass 1.5 us, two adapters in each; 4096 rows, an adapter of 32 for each row 344 and 415 us, of 100 575 and 466).
 constexpr int TL_N = 192;             // rows of a tile, at most
@@ -39,16 +39,17 @@ constexpr int TL_D0 = TL_A_STAGES * TL_A_COLS;
 constexpr int TL_HALF = TL_N / 2;      // rows of a CTA
 constexpr int TL_B_BYTES = TL_HALF * 128;
 constexpr int TL_BOX = 32;            // rows of one TMA box
-// warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs (with adapters: 3 the MMAs of their terms, 12-19 outputs)
+// warps: 0 rows (with an index: 0, 2 and 3), 1 MMA, 2 tensor memory, 4-11 weights, 12-15 outputs (with adapters: 3 the MMAs of their terms, and 12-19 outputs where there
+// are many passes)
 constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for each of the three warps that copy
 // With adapters, for 32 of the rank: their B, [128 channels][32], and three parts of A x, [96 rows][32] each, as 32-bit values; twice, so
 // that the next are written while the matrix instructions read these.
 constexpr int TL_LOW_A = 128 * 128, TL_LOW_B = TL_HALF * 128, TL_LOW_PARTS = 3, TL_LOW_BYTES = TL_LOW_A + TL_LOW_PARTS * TL_LOW_B;
 constexpr int TL_LOW_MOST = 48;       // different adapters in a tile, up to which the matrix instructions add them
-template <bool LOW>
+template <int LOW>   // 0, or with adapters the number of warps that write the outputs
 struct TallShape {
   static constexpr int kStages = LOW ? 10 : 16;
-  static constexpr int kOutWarps = LOW ? 8 : 4;
+  static constexpr int kOutWarps = LOW ? LOW : 4;
   static constexpr int kThreads = 384 + 32 * kOutWarps;
   static constexpr int kLow = LOW ? 2 * TL_LOW_BYTES : 0;   // bytes
 };
@@ -305,7 +306,7 @@ __device__ float lowrank_odd_term(const Lowrank& low, int K, int row, int co) {
   return s;
 }
 
-template <class T, bool GATHER, bool LOW>
+template <class T, bool GATHER, int LOW>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThreads, 1) products_tall_kernel(const TallParams p, const __grid_constant__ CUtensorMap map) {
   constexpr int STAGES = TallShape<LOW>::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -751,7 +752,7 @@ MapEncoder map_encoder() {
   return f;
 }
 
-template <class T, bool GATHER, bool LOW>
+template <class T, bool GATHER, int LOW>
 cudaError_t tall_launch(const Products& p, const ProductCall& c, const CUtensorMap& map, int* launched) {
   static unsigned long long done = 0;
   cudaError_t e = allow_max_smem(products_tall_kernel<T, GATHER, LOW>, &done);
@@ -767,8 +768,10 @@ cudaError_t tall_launch(const Products& p, const ProductCall& c, const CUtensorM
 
 template <class T>
 cudaError_t tall_kind(const Products& p, const ProductCall& c, const CUtensorMap& map, int* launched) {
-  if (c.low.adapter) return tall_launch<T, false, true>(p, c, map, launched);
-  return c.rows ? tall_launch<T, true, false>(p, c, map, launched) : tall_launch<T, false, false>(p, c, map, launched);
+  // Four warps of outputs leave the weights' more of the SM, eight are faster at the operands of the passes (4096 rows of 4096 x 4096, four requests, rank
+  // 16 101 and 106 us, rank 64 119 and 122, rank 128 161 and 149; an adapter of 16 for each row, rank 16 264 and 237, rank 64 616 and 518).
+  if (c.low.adapter) return c.low.rank <= 32 ? tall_launch<T, false, 4>(p, c, map, launched) : tall_launch<T, false, 8>(p, c, map, launched);
+  return c.rows ? tall_launch<T, true, 0>(p, c, map, launched) : tall_launch<T, false, 0>(p, c, map, launched);
 }
 
 }  // namespace
