@@ -30,8 +30,8 @@ namespace {
 // last that have them; rows of others have zeros there.  Two slots: the warps write the next pass's operands while this one is being added.  On
 // the FMA units, from shared memory, the same took longer than the sums themselves (4096 rows of 4096 x 4096 and rank 32 141 us, now 106;
 // rank 64 208 and 122, rank 128 312 and 149); as 16-bit or tf32 products of the warps' own matrix instruction each waited for one of the
-// pair's, 72 to 96 cycles.  Tiles with more than TL_LOW_MOST adapters, nearly one for each row, take the FMA units all the same (rank 16: 36 us a
-// tile, a pass 1.5 us, two adapters in each; 4096 rows, an adapter of 32 for each row 344 and 415 us, of 100 575 and 466).
+// pair's, 72 to 96 cycles.  Tiles with more than TL_LOW_MOST adapters, nearly one for each row, take the FMA units all the same (4096 rows, an adapter of
+// 48 for each row, rank 16 483 and 628 us, rank 64 1006 and 1191; of 100, 669 and 669, 1515 and 1328).
 constexpr int TL_N = 192;             // rows of a tile, at most
 constexpr int TL_A_STAGES = 4;
 constexpr int TL_A_COLS = 32;         // 64 input channels, two to a column
@@ -45,7 +45,7 @@ constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for
 // With adapters, for 32 of the rank: their B, [128 channels][32], and three parts of A x, [96 rows][32] each, as 32-bit values; twice, so
 // that the next are written while the matrix instructions read these.
 constexpr int TL_LOW_A = 128 * 128, TL_LOW_B = TL_HALF * 128, TL_LOW_PARTS = 3, TL_LOW_BYTES = TL_LOW_A + TL_LOW_PARTS * TL_LOW_B;
-constexpr int TL_LOW_MOST = 48;       // different adapters in a tile, up to which the matrix instructions add them
+constexpr int TL_LOW_MOST = 72;       // different adapters in a tile, up to which the matrix instructions add them
 template <int LOW>   // 0, or with adapters the number of warps that write the outputs
 struct TallShape {
   static constexpr int kStages = LOW ? 10 : 16;

@@ -63,3 +63,24 @@ def test_second_factor_with_infinities(snn, rank, n, bad):
         assert (torch.sign(y[bad_row][:, 3])[last != 0] == torch.sign(last)[last != 0]).all()
     # A x = (infinity, then x_0 * 0 and such): infinite or NaN wherever B's first value says so
     assert not torch.isfinite(y[inf_row]).any()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_second_factor_with_infinities_beside_more_adapters_than_passes(snn, bad):
+    test_second_factor_with_infinities(snn, 16, 150, bad)
+
+
+@pytest.mark.parametrize("rank", [8, 16, 40])
+@pytest.mark.parametrize("n", [71, 72, 73, 74])
+def test_as_many_adapters_as_passes_are_made_for(snn, rank, n):
+    """192 rows, a tile, with n adapters in turn: exactly n different ones."""
+    c_in, c_out, R = 128, 130, 192
+    g = _gen(60 + n)
+    layers, w, _ = _layers(snn, 1, c_in, c_out, 5, 2100, alpha=0.5)
+    x = _whole(g, 2, R, c_in).to(F16)
+    a, b = _whole(g, 1, n, rank, c_in).to(F16), _whole(g, 1, n, c_out, rank).to(F16)
+    adapter = (torch.arange(R, device="cuda") % n).to(torch.int32)
+    y = snn.SnnConvAdapters(layers[0]).forward(x, adapter, a, b, torch.ones(n, device="cuda"), out_type=snn.OUT_F32)
+    h = torch.einsum("rc,rjc->rj", x.double(), a.double()[adapter.long()])
+    ref = 0.5 * (x.double() @ w[0].T) + torch.einsum("rj,rkj->rk", h, b.double()[adapter.long()])
+    assert torch.equal(y, ref.float())
