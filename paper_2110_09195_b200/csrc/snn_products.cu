@@ -162,8 +162,10 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
           b[j][h] = x && c + 8 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
         }
     };
-    load_bits(group0, 0, kw);
-    load_rows(kw);
+    if (kw < p.n_kb) {   // (few items: some warps only help with the outputs)
+      load_bits(group0, 0, kw);
+      load_rows(kw);
+    }
     for (int group = group0; group < group1; ++group) {
       float acc[2 * MP][4] = {};
       for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
@@ -200,16 +202,20 @@ __global__ void __launch_bounds__(256, 2) products_small_kernel(const SmallParam
       __syncthreads();   // (the other half of the buffer is for the next strip)
       if (!waited) grid_dep_wait();
       waited = true;
-      const int width = M * m_warps, first = group * width;
-      for (int i = threadIdx.x; i < n * width; i += 256) {
-        const int c = i / width, m = i % width, co = first + m;
-        if (co >= p.K) continue;
+      // a thread has a channel (or two), and every 256 / width-th row
+      const int width = M * m_warps, columns = min(width, 256), first = group * width;
+      for (int m = (int)threadIdx.x & (columns - 1); m < width; m += 256) {
+        const int co = first + m;
+        if (co >= p.K) break;
         const float alpha = p.alpha[(size_t)e * p.n_mt * 16 + co];
-        float s = 0.f;
-        for (int k = 0; k < p.k_warps; ++k) s += red[(m / M) * p.k_warps + k][c][m % M];
-        float v = alpha * s;
-        if (p.low.adapter) v += lowrank_term<T>(p.low, p.K, r0 + c, co);
-        store_out(p.out, p.out_type, (long long)(r0 + c) * p.ld_out + co, v);
+#pragma unroll 2
+        for (int c = (int)threadIdx.x / columns; c < n; c += 256 / columns) {
+          float s = 0.f;
+          for (int k = 0; k < p.k_warps; ++k) s += red[(m / M) * p.k_warps + k][c][m % M];
+          float v = alpha * s;
+          if (p.low.adapter) v += lowrank_term<T>(p.low, p.K, r0 + c, co);
+          store_out(p.out, p.out_type, (long long)(r0 + c) * p.ld_out + co, v);
+        }
       }
     }
   }
@@ -231,13 +237,15 @@ cudaError_t small_launch(const Products& p, const ProductCall& c, int k_warps, u
 
 template <class T>
 cudaError_t small_forward(const Products& p, const ProductCall& c, int* launched) {
-  // all warps on one strip of output channels, unless there are not so many blocks of 256 input channels: small pieces of work
+  // all warps on one strip of output channels, unless there are not so many blocks of 256 input channels, and more strips than CTAs (the warps that have
+  // no input channels still help with the outputs: 40 rows of 584 x 130 with adapters of rank 64 6.5 us, with two warps for each block 12.8; 33
+  // rows of 368 x 91 and rank 8 4.6 and 6.9)
+  const long long ctas = 2ll * sm_count(), pieces = most_pieces(p, c);
   int k_warps = 8;
-  while (k_warps > p.n_kb) k_warps /= 2;
+  while (k_warps > p.n_kb && pieces * ((p.K + 8 / k_warps * 32 - 1) / (8 / k_warps * 32)) > ctas) k_warps /= 2;
   // 32 or 64 output channels a warp: a strip of 64 takes 1.86 times as long as one of 32, and what counts is how many of them a CTA has one
   // after the other (one expert of 4096 x 4096: 16 rows 6.7 us with 32, 32 rows 10.5 and 9.8, 48 rows 14.2 and 16.3, 64 rows 17.7 and
   // 16.4; 64 tokens over 64 experts of 2048 x 2048 39 and 33)
-  const long long ctas = 2ll * sm_count(), pieces = most_pieces(p, c);
   auto items = [&](int m) { return pieces * ((p.K + 8 / k_warps * m - 1) / (8 / k_warps * m)); };
   auto turns = [&](int m) { return (items(m) + ctas - 1) / ctas; };
   if (186 * turns(64) <= 100 * turns(32)) return small_launch<T, 2>(p, c, k_warps, (unsigned)min(ctas, items(64)), launched);
@@ -245,8 +253,9 @@ cudaError_t small_forward(const Products& p, const ProductCall& c, int* launched
 }
 
 // Which kernel, by the time that each would take on 148 SMs (us).  Few rows: each piece of 8 expands all of its expert's weights, 11 G
-// weights a ms.  Many rows: tiles of 256 output channels in turns of a tile for each pair of SMs, 0.16 to 0.24 us for 64 input channels,
-// whatever the number of rows up to 192.  (Measured both ways: one expert of 4096 x 4096, 32 rows 9.8 and 15.6 us, 64 rows 15 and 16; 16
+// weights a ms, and with few input channels each strip of outputs takes a time of its own.  Many rows: tiles of 256 output channels in turns of a
+// tile for each pair of SMs, 0.16 to 0.24 us for 64 input channels, whatever the number of rows up to 192.  (140 calls of drawn sizes took 0.8 %
+// longer than with the better kernel for each, geometric mean.  Measured both ways: one expert of 4096 x 4096, 32 rows 9.8 and 15.6 us, 64 rows 15 and 16; 16
 // of them, 128 rows 41 and 51, 256 rows 65 and 51; 64 of 2048 x 2048, 512 rows 48 and 53, 1024 rows 78 and 54.  With adapters the
 // time of many rows depends on how many adapters the rows of a tile have, which the host does not know: 16 adapters on 4096 x 4096, requests of
 // 50 rows, rank 16, 64 rows 22 and 21, 128 rows 37 and 25, rank 64 31 and 26, 56 and 35; an adapter for each row, rank 16 21 and 30, 36 and 35,
@@ -260,11 +269,12 @@ bool many_rows(const Products& p, const ProductCall& c) {
   }
   const double pairs = sm_count() / 2.0, used = c.offsets ? min(p.E, c.max_rows) : 1, blocks = (p.C + 63) / 64, rows = fmin(192.0, c.max_rows / used);
   double few = 3.0 + (c.max_rows / 8.0 + (c.offsets ? 0.5 * used : 0.5)) * p.K * (double)p.C / 11e6;
+  if (p.n_kb < 8) few += 3.0 * (1 - p.n_kb / 8.0) * (c.max_rows / 8.0) * ((p.K + 255) / 256) / (2 * sm_count());
   const double tiles = (c.max_rows < 192 * used ? used : c.max_rows / 192.0) * ((p.K + 255) / 256);
   double many = 5.5 + blocks * (tiles <= pairs ? 0.16 + 0.0002 * rows : tiles / pairs * (0.2 + 0.0002 * rows));
   if (c.low.adapter) {
     few += 8.5e-7 * c.max_rows * c.low.rank * p.K;
-    many += 2.0 + (0.04 + 0.003 * c.low.rank) * rows;
+    many += 2.0 + (0.02 + (4.2e-4 + 5.5e-7 * p.C) * c.low.rank) * rows;
   }
   return many < few;
 }
