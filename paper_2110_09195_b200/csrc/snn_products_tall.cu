@@ -46,6 +46,10 @@ constexpr int TL_PENDING = 3;         // stages of copied rows on their way, for
 // that the next are written while the matrix instructions read these.
 constexpr int TL_LOW_A = 128 * 128, TL_LOW_B = TL_HALF * 128, TL_LOW_PARTS = 3, TL_LOW_BYTES = TL_LOW_A + TL_LOW_PARTS * TL_LOW_B;
 constexpr int TL_LOW_MOST = 72;       // different adapters in a tile, up to which the matrix instructions add them
+// What stands for an infinity or NaN of B in the matrix instructions, with its sign: the rows of other adapters have 0 there and get 0, an infinite
+// A x gives its infinity (a 0 here would make it NaN, which nothing added later takes back), and a finite one at most 2^28, beside
+// the infinity or NaN that is added to this output afterwards.
+constexpr float TL_LOW_ODD = 0x1p-100f;
 template <int LOW>   // 0, or with adapters the number of warps that write the outputs
 struct TallShape {
   static constexpr int kStages = LOW ? 10 : 16;
@@ -623,8 +627,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           v[q] = q & 1 ? f[q >> 1].y : f[q >> 1].x;
-          if (!isfinite(v[q])) {
-            v[q] = 0.f;   // (would reach the rows of other adapters; added by itself afterwards)
+          if (!isfinite(v[q])) {   // (would reach the rows of other adapters; added by itself afterwards)
+            v[q] = copysignf(TL_LOW_ODD, v[q]);
             fine = false;
           }
         }
