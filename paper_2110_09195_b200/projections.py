@@ -35,10 +35,16 @@ def _dtype(out_type):
         raise SnnError(1, f"out_type={out_type} is not OUT_F32, OUT_F16 or OUT_BF16") from None
 
 
-def _matrix(t, name, device, columns=None, aligned=False):
-    """Elements between the rows of a matrix whose rows are dense."""
+def _here(t, name, device):
     if t.get_device() != device:
         raise SnnError(1, f"{name} must live on cuda:{device}")
+    if t.is_neg():   # (the imaginary part of a conjugated tensor)
+        raise SnnError(1, f"{name} is a view of negated memory: resolve_neg() copies it")
+
+
+def _matrix(t, name, device, columns=None, aligned=False):
+    """Elements between the rows of a matrix whose rows are dense."""
+    _here(t, name, device)
     if t.dim() != 2 or (columns is not None and t.shape[1] != columns):
         raise SnnError(1, f"{name} must have the shape (rows, {columns if columns is not None else 'columns'})")
     n = t.shape[1]
@@ -54,14 +60,16 @@ def _matrix(t, name, device, columns=None, aligned=False):
 
 def _ints(t, name, device, *shape):
     import torch
-    if t.get_device() != device or t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+    _here(t, name, device)
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
         raise SnnError(1, f"{name} must be a contiguous int32 tensor of shape {shape} on cuda:{device}")
     return t.data_ptr()
 
 
 def _floats(t, name, device, *shape):
     import torch
-    if t.get_device() != device or t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+    _here(t, name, device)
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
         raise SnnError(1, f"{name} must be a contiguous float32 tensor of shape {shape} on cuda:{device}")
     return t.data_ptr()
 
@@ -281,7 +289,8 @@ class SnnConvAdapters:
             raise SnnError(1, "a must be (adapters, rank, c_in) and b (adapters, c_out, rank)")
         n, rank = int(a.shape[0]), int(a.shape[1])
         for t, name, shape in ((a, "a", (n, rank, self.c_in)), (b, "b", (n, self.c_out, rank))):
-            if t.get_device() != self.device or t.dtype != x.dtype or tuple(t.shape) != shape or not t.is_contiguous():
+            _here(t, name, self.device)
+            if t.dtype != x.dtype or tuple(t.shape) != shape or not t.is_contiguous():
                 raise SnnError(1, f"{name} must be a contiguous tensor of x's type and shape {shape} on cuda:{self.device}")
         sp = _floats(scale, "scale", self.device, n)
         with _on(stream):
