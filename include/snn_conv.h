@@ -321,7 +321,8 @@ enum { SNN_OUT_F16 = 3, SNN_OUT_BF16 = 4 };
  * offsets must not fall and lie in [0, max_rows]; what lies outside is taken for the nearest end.  An expert may have no rows.
  * Rows of the output below offsets[0] and from offsets[count] on are left as they are.  A row index outside
  * [0, act_rows) stands for a row of zeros.  (max_rows is a bound; only rows that experts have cost time.  UNSUPPORTED: above
- * 2^30 rows, or where 8 rows times 32 output channels cut the outputs into 2^31 pieces or more.)
+ * 2^30 rows, or where (max_rows / 8 + 1) * count or (max_rows / 8 + count) * ceil(c_out / 32) reaches 2^31: pieces of 8
+ * rows are counted in 32 bits, whatever the offsets say.)
  */
 #define SNN_EXPERTS_MAX 1024
 typedef struct snn_conv_experts snn_conv_experts_t; /* opaque; owned by the library */
