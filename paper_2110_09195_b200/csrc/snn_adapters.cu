@@ -108,9 +108,9 @@ cudaError_t shrink_launch(const ShrinkParams& p, cudaStream_t s) {
   return launch_dependent(shrink_kernel<T, NT, MT, U, WARPS>, grid, 32 * WARPS, (size_t)WARPS * 8 * NT * (16 * MT + 1) * 4, s, p);
 }
 
-// How many rows and how much of the rank a CTA takes: the more, the less is read again; as long as there are CTAs for all SMs.  (4096 rows of
-// 4096 values, rank 64: 16 of the rank and 32 rows 36 us, 32 and 32 30 us, 64 and 32 26 us; 1000 rows: 16 and 6 19 us, 32 and 16 13 us,
-// 16 and 32 16 us; 500 rows: 16 and 3 14.4 us, 32 and 16 8.5 us; rank 16 and 4096 rows, two blocks of input channels on their way 13.7 us,
+// How many rows and how much of the rank a CTA takes: the more, the less is read again; as long as there are CTAs for all SMs, so one row up to
+// two for each SM.  (4096 rows of 4096 values, rank 64: 16 of the rank and 32 rows 36 us, 32 and 32 30 us, 64 and 32 26 us; 1000 rows: 16 and 6
+// 19 us, 32 and 16 13 us, 16 and 32 16 us; 500 rows: 16 and 3 14.4 us, 32 and 16 8.5 us; rank 16 and 4096 rows, two blocks of input channels on their way 13.7 us,
 // one 14.6.)
 template <class T>
 cudaError_t shrink_type(ShrinkParams p, cudaStream_t s) {
@@ -124,7 +124,7 @@ cudaError_t shrink_type(ShrinkParams p, cudaStream_t s) {
     p.per_cta = 16;
     return shrink_launch<T, 2, 2, 1, 16>(p, s);
   }
-  p.per_cta = max(1, min(8, p.rows / sms));
+  p.per_cta = 1;   // (a CTA for each row still is less than two for each SM; its row is one of the instruction's eight columns)
   return shrink_launch<T, 1, 1, 4, 8>(p, s);
 }
 
