@@ -109,9 +109,11 @@ __device__ __forceinline__ void find_piece(const Pieces& all, const int32_t* off
 // channels are four steps' operands) and stay in registers for all of the warp's output channels (loaded for every 32 of them, they took
 // as many cycles of the L1 cache as the rest).  The warps of a CTA take different input channels (k_warps of them) and different output
 // channels; the former's sums meet in shared memory.  The work, pieces of rows times strips of output channels, is counted on the device and
-// shared out evenly: a CTA has a run of strips, mostly of one piece.  Bound by latency where there are few weights, else by the
+// shared out evenly: a CTA has a run of strips, mostly of one piece.  Bound by latency where there are few weights, else mostly by the
 // expansion: 16 masks and 15 multiplications, at half rate each, for four of the instructions (64 tokens over 64 experts of 2048 x 2048, 4
-// each: half of the issue slots used).  16 rows a warp were no faster for any number of rows (16 experts of 4096 x 4096, 128 rows: 47 us
+// each, 31 us: 52 % of the issue slots and 47 % of the integer units used, none of them full; the rest is waits, a barrier and a sum over the warps for
+// each strip among them).  With adapters of many rows the second term is more than all else: a row's adapter, then its B, eight of the rank at a time
+// one behind the other (419 rows of 400 x 1912, rank 32, runs of 2 rows 42 us, 9 where no row has an adapter).  16 rows a warp were no faster for any number of rows (16 experts of 4096 x 4096, 128 rows: 47 us
 // against 41, 256 rows: 76 against 65).
 constexpr int SM_N = 8;
 template <class T, int MP>
@@ -255,7 +257,9 @@ cudaError_t small_forward(const Products& p, const ProductCall& c, int* launched
 // Which kernel, by the time that each would take on 148 SMs (us).  Few rows: each piece of 8 expands all of its expert's weights, 11 G
 // weights a ms, and with few input channels each strip of outputs takes a time of its own.  Many rows: tiles of 256 output channels in turns of a
 // tile for each pair of SMs, 0.16 to 0.24 us for 64 input channels, whatever the number of rows up to 192.  (140 calls of drawn sizes took 0.8 %
-// longer than with the better kernel for each, geometric mean.  Measured both ways: one expert of 4096 x 4096, 32 rows 9.8 and 15.6 us, 64 rows 15 and 16; 16
+// longer than with the better kernel for each, geometric mean.  The worst: 419 rows of 400 x 1912, 16 adapters of rank 32 in runs of 2 rows, 42.0 us by
+// the kernel taken, few rows, and 26.5 by the other; 2860 rows of 160 x 253 with one adapter of rank 8, 20.2 and 14.1; the other 138 at most
+// 13 % longer.  The number of adapters is not used, nor is the time of their first factor.  Measured both ways: one expert of 4096 x 4096, 32 rows 9.8 and 15.6 us, 64 rows 15 and 16; 16
 // of them, 128 rows 41 and 51, 256 rows 65 and 51; 64 of 2048 x 2048, 512 rows 48 and 53, 1024 rows 78 and 54.  With adapters the
 // time of many rows depends on how many adapters the rows of a tile have, which the host does not know: 16 adapters on 4096 x 4096, requests of
 // 50 rows, rank 16, 64 rows 22 and 21, 128 rows 37 and 25, rank 64 31 and 26, 56 and 35; an adapter for each row, rank 16 21 and 30, 36 and 35,

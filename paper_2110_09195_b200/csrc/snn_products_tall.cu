@@ -21,15 +21,16 @@ namespace {
 // half.  TMA brings the rows; rows named by an index come by 16-byte asynchronous copies of three warps (TMA's gather of four rows an
 // instruction took 2900 cycles for 192 rows of 128 bytes, seven times the instructions that they feed).
 // 512 columns: four stages of weights (32 columns each) and two accumulators of 192, so that one is written out while the next is
-// being summed.  (4096 rows, one expert of 4096 x 4096, bf16: 88 us, 1550 TFLOP/s; 8192 rows by an index, 8
-// experts of 2048 x 8192, 198 us, 1390 TFLOP/s.)
+// being summed.  (Times here are a call's in a graph of twelve, a run too short for the power limit; among seconds of calls the clock is lower and the
+// long ones take up to 1.17 times as long.  4096 rows, one expert of 4096 x 4096, bf16: 90 us, 1530 TFLOP/s; 8192 rows by an index, 8
+// experts of 2048 x 8192, 200 us, 1380 TFLOP/s, and 233 us.)
 //
 // With adapters, D = alpha S + B (A x), A x in fp32 from the kernel before: the warps of the outputs multiply the sums by alpha in place, in
 // tensor memory, and the matrix instructions add the second term, as tf32: B's 16-bit values are such numbers, and A x is the sum of three (11
 // bits each, so that nothing is rounded).  A pass adds 32 of the rank, of one adapter or of several small ones, to the rows between the first and the
 // last that have them; rows of others have zeros there.  Two slots: the warps write the next pass's operands while this one is being added.  On
-// the FMA units, from shared memory, the same took longer than the sums themselves (4096 rows of 4096 x 4096 and rank 32 141 us, now 106;
-// rank 64 208 and 122, rank 128 312 and 149); as 16-bit or tf32 products of the warps' own matrix instruction each waited for one of the
+// the FMA units, from shared memory, the same took longer than the sums themselves (4096 rows of 4096 x 4096 and rank 32 141 us, now 105, among
+// seconds of calls 121; rank 64 208 and 125, rank 128 312 and 153); as 16-bit or tf32 products of the warps' own matrix instruction each waited for one of the
 // pair's, 72 to 96 cycles.  Tiles with more than TL_LOW_MOST adapters, nearly one for each row, take the FMA units all the same (4096 rows, an adapter of
 // 48 for each row, rank 16 483 and 628 us, rank 64 1006 and 1191; of 100, 669 and 669, 1515 and 1328).
 constexpr int TL_N = 192;             // rows of a tile, at most
