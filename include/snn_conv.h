@@ -384,6 +384,87 @@ SNN_API snn_status_t snn_conv_adapters_forward(snn_conv_adapters_t* h, const voi
                                                int32_t out_type, int64_t ld_out, void* cuda_stream);
 SNN_API snn_status_t snn_conv_adapters_destroy(snn_conv_adapters_t* h);
 
+/*
+ * What stands between the two projections of a feed-forward block: an activation function, with a gate or without.
+ *   GELU is v * Phi(v), Phi the normal distribution's function (not the approximation by tanh).  What the formula makes of an
+ *   infinity is what comes out: SILU and GELU of -infinity are NaN.
+ * snn_conv_experts_activate: out[r][c] = fn(gate[r][c]) * up[r][c], or fn(up[r][c]) where gate_dev is NULL, in fp32, one
+ * rounding to out_type.  gate and up are of one type (`type`; both and out_type SNN_OUT_F32, SNN_OUT_F16 or SNN_OUT_BF16); rows
+ * lie ld elements apart, each aligned to its element.  out may be gate or up itself where type, pointer and ld are the same.
+ */
+enum { SNN_FN_NONE = 0, SNN_FN_RELU = 1, SNN_FN_SILU = 2, SNN_FN_GELU = 3 };
+SNN_API snn_status_t snn_conv_experts_activate(const void* gate_dev, int64_t ld_gate, const void* up_dev, int64_t ld_up,
+                                               int32_t type, int32_t rows, int32_t columns, int32_t fn, void* out_dev,
+                                               int32_t out_type, int64_t ld_out, int32_t device, void* cuda_stream);
+
+/*
+ * A whole mixture of experts for a few tokens, where launches and the reading of weights are all that counts:
+ *   ids, w = router(logits[t])                               (as snn_conv_experts_route)
+ *   h_j    = fn(gate_e(act[t])) * up_e(act[t])               e = ids[j];  fn(up_e(act[t])) without a gate
+ *   out[t] = sum_j w_j * down_e(h_j)                         zeros where no expert can be chosen
+ * in two launches (three above SNN_MOE_FUSED_TOKENS tokens: the router's comes first).  Sums are fp32; h is kept as the sum of
+ * bf16 parts, three of them (all of its 24 bits) for SNN_OUT_F32, two (16 or more) for 16-bit outputs; one rounding to out_type.
+ * The order of the sums depends on the sizes alone.  An infinity or NaN in a token's activations reaches that token's outputs
+ * and no others.  For more tokens call route, experts, activate, experts and combine, with the same handles.
+ *
+ * snn_conv_moe_create: three experts handles (gate may be NULL) of one count on one device; gate and up of one c_in and c_out, down's c_in = up's
+ * c_out.  They are kept by reference and must outlive the mixture.
+ * snn_conv_moe_forward: act [tokens] rows of SNN_ACT_F16 or SNN_ACT_BF16, tokens up to SNN_MOE_TOKENS_MAX (UNSUPPORTED above); logits, type and top_k
+ * as for the router.  work_dev: snn_conv_moe_work(...) bytes, 16-byte aligned, written by the call.  May be called at the same time on
+ * several streams with a workspace each.
+ */
+#define SNN_MOE_TOKENS_MAX 64
+#define SNN_MOE_FUSED_TOKENS 8
+typedef struct snn_conv_moe snn_conv_moe_t; /* opaque; owned by the library */
+SNN_API snn_status_t snn_conv_moe_create(snn_conv_experts_t* gate, snn_conv_experts_t* up, snn_conv_experts_t* down, int32_t fn,
+                                         snn_conv_moe_t** out);
+SNN_API int64_t snn_conv_moe_work(const snn_conv_moe_t* m, int32_t tokens, int32_t top_k); /* -1: not allowed */
+SNN_API snn_status_t snn_conv_moe_forward(snn_conv_moe_t* m, const void* act_dev, int32_t act_type, int32_t tokens, int64_t ld_act,
+                                          const void* logits_dev, int32_t logits_type, int64_t ld_logits, int32_t top_k,
+                                          int32_t normalise, void* work_dev, void* out_dev, int32_t out_type, int64_t ld_out,
+                                          void* cuda_stream);
+/* Frees the mixture (not the experts).  NULL is a no-op. */
+SNN_API snn_status_t snn_conv_moe_destroy(snn_conv_moe_t* m);
+
+/*
+ * Projections that stay at 8 bits (in networks of this kind the first and the last layers, and what does not bear one bit): values
+ * in e4m3 (1 sign, 4 exponent, 3 fraction bits; largest 448, no infinity, 0x7f and 0xff NaN) with an fp32 scale for each block of
+ * SNN_SCALED_BLOCK: of a row of activations 128 neighbouring channels, of the weights 128 x 128.  (The last blocks may be smaller.)
+ *   out[r][co] = sum_b  xs[r][b] * ws[co / 128][b] * sum_(ci in b) x[r][ci] * w[co][ci]
+ * Products and sums are fp32 (a block's sum is scaled once), one rounding to out_type (SNN_OUT_F32, SNN_OUT_F16, SNN_OUT_BF16).
+ *
+ * snn_conv_scaled_create: `count` (1..SNN_EXPERTS_MAX) projections; weights_dev [count][c_out][c_in] e4m3 and scales_dev
+ * [count][ceil(c_out / 128)][ceil(c_in / 128)] are dense DEVICE arrays, read in the order of cuda_stream and copied into a layout of their own, c_in and
+ * c_out padded to multiples of 128 (device memory owned by the handle).  c_in is a multiple of 16.  Synchronous.
+ *
+ * snn_conv_scaled_forward: act_dev [act_rows][c_in] e4m3, rows ld_act bytes apart (a multiple of 16, as the pointer is), act_scales_dev [act_rows][ceil(c_in / 128)] fp32,
+ * rows ld_scales apart.  Row i belongs to projection e with offsets[e] <= i < offsets[e + 1] (DEVICE, count + 1 ints, as the router
+ * writes them; what lies outside [0, act_rows] is taken for the nearest end); offsets_dev NULL: all rows are projection 0's.  Rows of the
+ * output without a projection are left as they are.  Infinite or NaN values or scales of a row reach that row's outputs and no others.
+ * Calls may overlap.  UNSUPPORTED: above 2^30 rows, or where (act_rows / 8 + count) * ceil(c_out / 16) reaches 2^31.
+ */
+#define SNN_SCALED_BLOCK 128
+typedef struct snn_conv_scaled snn_conv_scaled_t; /* opaque; owned by the library */
+SNN_API snn_status_t snn_conv_scaled_create(const void* weights_dev, const float* scales_dev, int32_t count, int32_t c_in,
+                                            int32_t c_out, int32_t device, void* cuda_stream, snn_conv_scaled_t** out);
+SNN_API snn_status_t snn_conv_scaled_forward(snn_conv_scaled_t* h, const void* act_dev, int64_t ld_act, const float* act_scales_dev,
+                                             int64_t ld_scales, const int32_t* offsets_dev, int32_t act_rows, void* out_dev,
+                                             int32_t out_type, int64_t ld_out, void* cuda_stream);
+SNN_API snn_status_t snn_conv_scaled_destroy(snn_conv_scaled_t* h);
+
+/*
+ * Rows into that form:  s = max(m / 448, 2^-70) with m the largest magnitude among the finite values of a block, and each value e4m3(v / s):
+ * the fp32 quotient, rounded to nearest even.  An infinity or NaN becomes NaN, and leaves the rest of its block as it is without it.
+ * v is up[r][c], or behind an activation fn(up[r][c]) or fn(gate[r][c]) * up[r][c], in fp32.  Output row i is of input row rows[i] (DEVICE, out_rows ints; an
+ * index outside [0, in_rows) stands for a row of zeros), or without rows_dev of row i (out_rows = in_rows).
+ * values_dev [out_rows] rows ld_values bytes apart, scales_dev [out_rows][ceil(columns / 128)] fp32, rows ld_scales apart; nothing is written
+ * between the rows.
+ */
+SNN_API snn_status_t snn_conv_scaled_quantise(const void* gate_dev, int64_t ld_gate, const void* up_dev, int64_t ld_up, int32_t type,
+                                              int32_t in_rows, const int32_t* rows_dev, int32_t out_rows, int32_t columns, int32_t fn,
+                                              void* values_dev, int64_t ld_values, float* scales_dev, int64_t ld_scales, int32_t device,
+                                              void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,3 +8,6 @@ from .binding import (  # noqa: F401
 from .projections import (  # noqa: F401
     ACT_BF16, OUT_BF16, OUT_F16, Route, SnnConvAdapters, SnnConvExperts, alloc_route, combine, route,
 )
+from .mixture import (  # noqa: F401
+    FN_GELU, FN_NONE, FN_RELU, FN_SILU, MOE_TOKENS_MAX, Quantised, SnnConvMoe, SnnConvScaled, activate, alloc_quantised, quantise,
+)

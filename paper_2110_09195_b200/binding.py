@@ -36,6 +36,9 @@ EXPORTED_SYMBOLS = (
     "snn_conv_experts_create", "snn_conv_experts_forward", "snn_conv_experts_destroy",
     "snn_conv_experts_route", "snn_conv_experts_route_work", "snn_conv_experts_combine",
     "snn_conv_adapters_create", "snn_conv_adapters_forward", "snn_conv_adapters_destroy",
+    "snn_conv_experts_activate",
+    "snn_conv_moe_create", "snn_conv_moe_work", "snn_conv_moe_forward", "snn_conv_moe_destroy",
+    "snn_conv_scaled_create", "snn_conv_scaled_forward", "snn_conv_scaled_destroy", "snn_conv_scaled_quantise",
 )
 
 
@@ -125,6 +128,24 @@ def load_library():
     lib.snn_conv_adapters_forward.argtypes = [vp, vp, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp, i32, i64, vp]
     lib.snn_conv_adapters_destroy.restype = i32
     lib.snn_conv_adapters_destroy.argtypes = [vp]
+    lib.snn_conv_experts_activate.restype = i32
+    lib.snn_conv_experts_activate.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, i32, i64, i32, vp]
+    lib.snn_conv_moe_create.restype = i32
+    lib.snn_conv_moe_create.argtypes = [vp, vp, vp, i32, ctypes.POINTER(vp)]
+    lib.snn_conv_moe_work.restype = i64
+    lib.snn_conv_moe_work.argtypes = [vp, i32, i32]
+    lib.snn_conv_moe_forward.restype = i32
+    lib.snn_conv_moe_forward.argtypes = [vp, vp, i32, i32, i64, vp, i32, i64, i32, i32, vp, vp, i32, i64, vp]
+    lib.snn_conv_moe_destroy.restype = i32
+    lib.snn_conv_moe_destroy.argtypes = [vp]
+    lib.snn_conv_scaled_create.restype = i32
+    lib.snn_conv_scaled_create.argtypes = [vp, vp, i32, i32, i32, i32, vp, ctypes.POINTER(vp)]
+    lib.snn_conv_scaled_forward.restype = i32
+    lib.snn_conv_scaled_forward.argtypes = [vp, vp, i64, vp, i64, vp, i32, vp, i32, i64, vp]
+    lib.snn_conv_scaled_destroy.restype = i32
+    lib.snn_conv_scaled_destroy.argtypes = [vp]
+    lib.snn_conv_scaled_quantise.restype = i32
+    lib.snn_conv_scaled_quantise.argtypes = [vp, i64, vp, i64, i32, i32, vp, i32, i32, i32, vp, i64, vp, i64, i32, vp]
     lib.snn_microbench.restype = i32
     lib.snn_microbench.argtypes = [i32, i32, ctypes.POINTER(ctypes.c_double)]
     _lib = lib

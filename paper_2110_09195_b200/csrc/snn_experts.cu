@@ -1,27 +1,15 @@
 // Host side of the projections of language models in include/snn_conv.h: argument checks, handles and launches.
 #include <new>
 
-#include "snn_handle.h"
-#include "snn_products.h"
+#include "snn_checks.h"
 
 using namespace snn;
 
-struct snn_conv_experts {
-  Products p;
-};
 struct snn_conv_adapters {
   Products p;
 };
 
 namespace {
-
-snn_status_t cuda_failed(cudaError_t e, const char* what) {
-  cudaGetLastError();
-  return api_fail(e == cudaErrorMemoryAllocation ? SNN_ERR_OOM : SNN_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-}
-bool act_ok(int type) { return type == SNN_ACT_F16 || type == SNN_ACT_BF16; }
-bool out_ok(int type) { return type == SNN_OUT_F32 || type == SNN_OUT_F16 || type == SNN_OUT_BF16; }
-size_t out_size(int type) { return type == SNN_OUT_F32 ? 4 : 2; }
 
 snn_status_t check_layers(snn_conv_t* const* layers, int count, const LayerDev** L) {
   for (int i = 0; i < count; ++i) {
@@ -78,26 +66,13 @@ snn_status_t check_rows(const Products& p, const void* act, int act_type, int ac
 snn_status_t forward(Products& p, const ProductCall& c, const ShrinkCall* first, const char* what) {
   DeviceGuard guard(p.device);
   if (!guard.ok) return api_fail(SNN_ERR_CUDA, "cannot select device %d", p.device);
-  if (*p.status_host) {
-    const int code = *p.status_host;
-    *p.status_host = 0;
-    return api_fail(SNN_ERR_TIMEOUT, "an earlier launch gave up a bounded wait (code %d)", code);
-  }
+  const snn_status_t st = earlier_timeout(p.status_host);
+  if (st != SNN_OK) return st;
   int launched = 0;
   cudaError_t e = first ? shrink_forward(*first, &launched) : cudaSuccess;
   if (e == cudaSuccess) e = products_forward(p, c, &launched);
   api_count_launches(launched);
   return e == cudaSuccess ? SNN_OK : cuda_failed(e, what);
-}
-
-snn_status_t select_device(int device) {
-  int n = 0;
-  if (cudaGetDeviceCount(&n) != cudaSuccess || n < 1) {
-    cudaGetLastError();
-    return api_fail(SNN_ERR_CUDA, "no CUDA device available (this library has no CPU path)");
-  }
-  if (device < 0 || device >= n) return api_fail(SNN_ERR_INVALID_ARG, "device %d of %d", device, n);
-  return SNN_OK;
 }
 
 }  // namespace

@@ -50,60 +50,6 @@ struct SmallParams {
   Powers pow;
 };
 
-// Pieces of at most `most` rows of an expert, counted over the experts in their order, by each warp for itself: every lane counts the
-// pieces of a run of experts, and a scan over the lanes says whose run a piece is in.
-struct Pieces {
-  int upto, count, total;   // this lane's, and of all
-};
-__device__ __forceinline__ int pieces_of(const int32_t* offsets, int e, int R, int most, int* lo_out, int* hi_out) {
-  const int lo = clamp_offset(offsets[e], R), hi = clamp_offset(offsets[e + 1], R);
-  *lo_out = lo;
-  *hi_out = hi;
-  return (max(hi - lo, 0) + most - 1) / most;
-}
-__device__ __forceinline__ Pieces count_pieces(const int32_t* offsets, int E, int R, int most) {
-  if (!offsets) return Pieces{0, 0, (R + most - 1) / most};
-  const int lane = threadIdx.x & 31, per = (E + 31) >> 5, e0 = lane * per, e1 = min(E, e0 + per);
-  Pieces r{0, 0, 0};
-  int lo, hi;
-  for (int e = e0; e < e1; ++e) r.count += pieces_of(offsets, e, R, most, &lo, &hi);
-  r.upto = r.count;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, r.upto, d);
-    if (lane >= d) r.upto += v;
-  }
-  r.total = __shfl_sync(0xffffffffu, r.upto, 31);
-  return r;
-}
-// Expert, first row and rows of a piece below the total.
-__device__ __forceinline__ void find_piece(const Pieces& all, const int32_t* offsets, int E, int R, int most, int piece, int* e_out, int* r_out, int* n_out) {
-  if (!offsets) {
-    *e_out = 0;
-    *r_out = piece * most;
-    *n_out = min(most, R - piece * most);
-    return;
-  }
-  const int lane = threadIdx.x & 31, per = (E + 31) >> 5, e0 = lane * per, e1 = min(E, e0 + per);
-  const int src = __ffs(__ballot_sync(0xffffffffu, piece < all.upto)) - 1;
-  int e = 0, r = 0, n = 0;
-  if (lane == src) {
-    int left = piece - (all.upto - all.count), lo, hi;
-    for (e = e0; e < e1; ++e) {
-      const int pieces = pieces_of(offsets, e, R, most, &lo, &hi);
-      if (left < pieces) {
-        r = lo + left * most;
-        n = min(most, hi - r);
-        break;
-      }
-      left -= pieces;
-    }
-  }
-  *e_out = __shfl_sync(0xffffffffu, e, src);
-  *r_out = __shfl_sync(0xffffffffu, r, src);
-  *n_out = __shfl_sync(0xffffffffu, n, src);
-}
-
 // A warp computes 32 MP output channels times 8 rows over a share of the input channels: the weights, the M operand, are expanded from
 // bits in registers, the rows, the N operand, come straight from memory as the instruction wants them (a lane's 16
 // channels are four steps' operands) and stay in registers for all of the warp's output channels (loaded for every 32 of them, they took

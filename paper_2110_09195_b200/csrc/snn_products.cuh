@@ -119,5 +119,121 @@ __device__ __forceinline__ float lowrank_term(const Lowrank& low, int K, int row
 
 __device__ __forceinline__ int clamp_offset(int v, int most) { return min(max(v, 0), most); }
 
+// Pieces of at most `most` rows of an expert, counted over the experts in their order, by each warp for itself: every lane counts the
+// pieces of a run of experts, and a scan over the lanes says whose run a piece is in.
+struct Pieces {
+  int upto, count, total;   // this lane's, and of all
+};
+__device__ __forceinline__ int pieces_of(const int32_t* offsets, int e, int R, int most, int* lo_out, int* hi_out) {
+  const int lo = clamp_offset(offsets[e], R), hi = clamp_offset(offsets[e + 1], R);
+  *lo_out = lo;
+  *hi_out = hi;
+  return (max(hi - lo, 0) + most - 1) / most;
+}
+__device__ __forceinline__ Pieces count_pieces(const int32_t* offsets, int E, int R, int most) {
+  if (!offsets) return Pieces{0, 0, (R + most - 1) / most};
+  const int lane = threadIdx.x & 31, per = (E + 31) >> 5, e0 = lane * per, e1 = min(E, e0 + per);
+  Pieces r{0, 0, 0};
+  int lo, hi;
+  for (int e = e0; e < e1; ++e) r.count += pieces_of(offsets, e, R, most, &lo, &hi);
+  r.upto = r.count;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, r.upto, d);
+    if (lane >= d) r.upto += v;
+  }
+  r.total = __shfl_sync(0xffffffffu, r.upto, 31);
+  return r;
+}
+// Expert, first row and rows of a piece below the total.
+__device__ __forceinline__ void find_piece(const Pieces& all, const int32_t* offsets, int E, int R, int most, int piece, int* e_out, int* r_out, int* n_out) {
+  if (!offsets) {
+    *e_out = 0;
+    *r_out = piece * most;
+    *n_out = min(most, R - piece * most);
+    return;
+  }
+  const int lane = threadIdx.x & 31, per = (E + 31) >> 5, e0 = lane * per, e1 = min(E, e0 + per);
+  const int src = __ffs(__ballot_sync(0xffffffffu, piece < all.upto)) - 1;
+  int e = 0, r = 0, n = 0;
+  if (lane == src) {
+    int left = piece - (all.upto - all.count), lo, hi;
+    for (e = e0; e < e1; ++e) {
+      const int pieces = pieces_of(offsets, e, R, most, &lo, &hi);
+      if (left < pieces) {
+        r = lo + left * most;
+        n = min(most, hi - r);
+        break;
+      }
+      left -= pieces;
+    }
+  }
+  *e_out = __shfl_sync(0xffffffffu, e, src);
+  *r_out = __shfl_sync(0xffffffffu, r, src);
+  *n_out = __shfl_sync(0xffffffffu, n, src);
+}
+
+// 8 neighbouring values as fp32, and their 16 or 32 bytes: read once, so they are the first to leave the caches.
+template <class Y>
+struct Eight;
+template <>
+struct Eight<float> {
+  uint4 lo, hi;
+  __device__ __forceinline__ void load(const float* p) {
+    lo = ld16_stream(p);
+    hi = ld16_stream(p + 4);
+  }
+  __device__ __forceinline__ void zero() { lo = hi = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ float2 pair(int i) const {
+    const uint4& v = i < 2 ? lo : hi;
+    return i & 1 ? make_float2(__uint_as_float(v.z), __uint_as_float(v.w)) : make_float2(__uint_as_float(v.x), __uint_as_float(v.y));
+  }
+};
+template <class T>
+struct Eight16 {
+  uint4 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = ld16_stream(p); }
+  __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ float2 pair(int i) const { return T::unpack(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
+};
+template <>
+struct Eight<F16> : Eight16<F16> {};
+template <>
+struct Eight<BF16> : Eight16<BF16> {};
+template <class Y>
+struct Element {
+  using type = uint16_t;
+};
+template <>
+struct Element<float> {
+  using type = float;
+};
+
+__device__ __forceinline__ uint32_t pack_pair(int type, float2 v) {
+  uint32_t r;
+  if (type == SNN_OUT_F16) {
+    const __half2 h = __floats2half2_rn(v.x, v.y);
+    memcpy(&r, &h, 4);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+    memcpy(&r, &h, 4);
+  }
+  return r;
+}
+
+__device__ __forceinline__ float value(const void* y, int type, long long i) {
+  if (type == SNN_OUT_F32) return static_cast<const float*>(y)[i];
+  if (type == SNN_OUT_F16) return __half2float(static_cast<const __half*>(y)[i]);
+  return __bfloat162float(static_cast<const __nv_bfloat16*>(y)[i]);
+}
+
+// What stands between two projections (SNN_FN_*): with a gate, fn(gate) * up.
+__device__ __forceinline__ float activated(int fn, float v) {
+  if (fn == SNN_FN_SILU) return v / (1.f + expf(-v));
+  if (fn == SNN_FN_GELU) return v * normcdff(v);   // (no 1 + erf(v): that loses the digits of a negative v)
+  if (fn == SNN_FN_RELU) return v < 0.f ? 0.f : v;   // (NaN stays)
+  return v;
+}
+
 }  // namespace
 }  // namespace snn

@@ -94,4 +94,75 @@ struct CombineCall {
 };
 cudaError_t combine_forward(const CombineCall& c, int* launched);
 
+// (gate null: none; rows null: all in their order)
+struct ActivateCall {
+  const void *gate, *up;
+  long long ld_gate, ld_up;
+  int type, rows, columns, fn;
+  void* out;
+  int out_type;
+  long long ld_out;
+  cudaStream_t stream;
+};
+cudaError_t activate_forward(const ActivateCall& c, int* launched);
+struct QuantiseCall {
+  const void *gate, *up;
+  long long ld_gate, ld_up;
+  int type, in_rows;
+  const int32_t* rows;
+  int out_rows, columns, fn;
+  uint8_t* values;
+  long long ld_values;
+  float* scales;
+  long long ld_scales;
+  cudaStream_t stream;
+};
+cudaError_t quantise_forward(const QuantiseCall& c, int* launched);
+
+// A mixture of experts for few tokens (snn_moe.cu); gate null: none.
+struct MoeCall {
+  const Products *gate, *up, *down;
+  int fn;
+  const void* act;
+  int act_type, tokens;
+  long long ld_act;
+  const void* logits;
+  int logits_type;
+  long long ld_logits;
+  int top_k, normalise;
+  void* work;
+  void* out;
+  int out_type;
+  long long ld_out;
+  cudaStream_t stream;
+};
+long long moe_work_bytes(const Products& up, int tokens, int top_k);
+cudaError_t moe_forward(const MoeCall& c, int* launched);
+
+// E projections [K x C] in e4m3, padded to multiples of 128: tiles [E][n_kt][n_kb] of 128 output times 128 input channels, 16 KB each.  Row r of a tile
+// is 128 bytes from 128 r on, its 16-byte pieces in the order piece ^ (r mod 8): as TMA would write them for the matrix instructions.
+struct Scaled {
+  int device = 0, E = 0, C = 0, K = 0;
+  int n_kt = 0, n_kb = 0;
+  uint8_t* tiles = nullptr;
+  float* scales = nullptr;      // [E][n_kt][n_kb]
+  int* status_host = nullptr;   // pinned, written by a kernel that gave up a bounded wait
+  int* status_dev = nullptr;
+};
+cudaError_t scaled_create(const uint8_t* weights, const float* scales, int E, int C, int K, cudaStream_t s, Scaled* out, int* launched);
+void scaled_destroy(Scaled* p);
+struct ScaledCall {
+  const uint8_t* act;
+  long long ld_act;
+  const float* scales;
+  long long ld_scales;
+  const int32_t* offsets;   // or null: all rows are projection 0's
+  int rows;
+  void* out;
+  int out_type;
+  long long ld_out;
+  cudaStream_t stream;
+};
+cudaError_t scaled_forward(const Scaled& p, const ScaledCall& c, int* launched);
+
 }  // namespace snn
