@@ -18,7 +18,7 @@ FAST_SOURCE = CSRC / "snn_fast.cpp"
 FAST_TORCH = PKG / "_build" / "_snn_fast.torch"   # the version of torch it was built for
 SOURCES = ["snn_api.cu", "snn_decode.cu", "snn_popc.cu", "snn_reuse.cu", "snn_reuse_f16.cu", "snn_tcg.cu", "snn_microbench.cu", "snn_static.cu",
            "snn_products.cu", "snn_products_tall.cu", "snn_adapters.cu", "snn_route.cu", "snn_experts.cu", "snn_rows.cu",
-           "snn_moe.cu", "snn_scaled.cu", "snn_mixture.cu"]
+           "snn_moe.cu", "snn_scaled.cu", "snn_scaled_tall.cu", "snn_mixture.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", f"-I{INCLUDE}", f"-I{CSRC}",

@@ -164,5 +164,6 @@ struct ScaledCall {
   cudaStream_t stream;
 };
 cudaError_t scaled_forward(const Scaled& p, const ScaledCall& c, int* launched);
+cudaError_t scaled_tall(const Scaled& p, const ScaledCall& c, int shape, int* launched);   // (snn_scaled_tall.cu: many rows; output channels of a tile)
 
 }  // namespace snn

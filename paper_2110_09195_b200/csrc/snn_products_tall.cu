@@ -5,6 +5,7 @@
 
 #include "snn_products.h"
 
+#include "snn_pairs.cuh"
 #include "snn_products.cuh"
 #include "snn_tc_common.cuh"
 
@@ -59,9 +60,6 @@ struct TallShape {
   static constexpr int kLow = LOW ? 2 * TL_LOW_BYTES : 0;   // bytes
 };
 
-// The same value in all lanes, known to be so
-__device__ __forceinline__ int uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
-
 struct TallParams {
   const uint32_t* bits;
   const float* alpha;
@@ -99,13 +97,6 @@ __device__ __forceinline__ void stage_ts_f16(uint32_t d, uint32_t a, uint64_t bd
       "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(bar0), "r"(bar1), "r"(on), "h"((uint16_t)3)
       : "memory");
 }
-__device__ __forceinline__ void commit_on(uint32_t bar, uint32_t on) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}" ::"r"(bar),
-      "r"(on), "h"((uint16_t)3)
-      : "memory");
-}
 // Up to four steps of 8 of the rank: D[256 x N] += B[256 x 8 steps] * H[N x 8 steps]^T, both 32-bit values of 10 bits (tf32) in shared memory.
 __device__ __forceinline__ void low_ss_tf32(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t steps, uint32_t on) {
   asm volatile(
@@ -119,10 +110,6 @@ __device__ __forceinline__ void low_ss_tf32(uint32_t d, uint64_t adesc, uint64_t
       "@q3 tcgen05.mma.cta_group::2.kind::tf32 [%0], a3, b3, %3, 1;\n\t}" ::"r"(d),
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(steps), "r"(on)
       : "memory");
-}
-// Rows of 128 bytes, the 16-byte pieces of eight rows in turn (the layout that TMA writes the rows of activations in)
-__device__ __forceinline__ uint64_t rows_desc(uint32_t addr) {
-  return ((uint64_t)2 << 61) | ((uint64_t)1 << 46) | ((uint64_t)64 << 32) | ((uint64_t)1 << 16) | (addr >> 4);
 }
 // 32 columns of the warp's 32 lanes; they are there after tmem_st_wait
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
@@ -145,12 +132,6 @@ __device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t (&v)[4]) {
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t (&v)[4]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
-// (the barrier: the pair's first CTA's)
-__device__ __forceinline__ void tma_rows(uint32_t dst, const void* map, int c, int row, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(c),
-               "r"(row), "r"(bar)
-               : "memory");
-}
 // 16 bytes, or zeros
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -160,21 +141,6 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// The address of the pair's first CTA's copy of a variable in shared memory, and an arrival there.  What the arrival stands for is in tensor
-// memory or in the SM's own shared memory, after wait::st, wait::ld or a proxy fence, and is read by the MMA unit: no wider release is needed
-// (one of cluster scope, with waits that acquire at that scope, made every stage take 900 cycles, whatever its size).
-__device__ __forceinline__ uint32_t at_first(uint32_t addr) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
-  return r;
-}
-__device__ __forceinline__ void arrive_at_first(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(at_first(bar)) : "memory");
-}
-__device__ __forceinline__ void pair_sync() {
-  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
-}
-
 // Barrier ID among THREADS of the CTA's threads, whole warps; whether all of them say so.
 template <int ID, int THREADS>
 __device__ __forceinline__ bool bar_all(bool v) {
@@ -752,22 +718,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(TallShape<LOW>::kThr
   pair_sync();
   tc_fence_after();
   if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
-}
-
-using MapEncoder = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-// The driver's tensor-map encoder, looked up once (the library does not link the driver).
-MapEncoder map_encoder() {
-  static const MapEncoder f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      p = nullptr;
-    }
-    return reinterpret_cast<MapEncoder>(p);
-  }();
-  return f;
 }
 
 template <class T, bool GATHER, int LOW>

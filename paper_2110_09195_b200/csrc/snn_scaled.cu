@@ -1,4 +1,7 @@
 // Projections in 8-bit floating point with a scale for each block of 128: layout of the weights, and the kernel for few rows.
+#include <cstdlib>
+#include <cstring>
+
 #include "snn_products.h"
 
 #include "snn_products.cuh"
@@ -255,6 +258,16 @@ void scaled_destroy(Scaled* p) {
 
 cudaError_t scaled_forward(const Scaled& p, const ScaledCall& c, int* launched) {
   const long long each = c.offsets ? ((long long)c.rows + min(p.E, c.rows) - 1) / min(p.E, c.rows) : c.rows;
+  bool many = each > 16;
+  int shape = each > 256 ? 256 : each > 64 ? 128 : 64;
+  if (const char* f = getenv("SNN_FORCE_ROWS")) {
+    many = strcmp(f, "few") && (!strcmp(f, "many") || many);
+    if (!strcmp(f, "256") || !strcmp(f, "128") || !strcmp(f, "64")) {
+      many = true;
+      shape = atoi(f);
+    }
+  }
+  if (many) return scaled_tall(p, c, shape, launched);
   if (each <= 8) return few_launch<1>(p, c, launched);
   return each <= 16 ? few_launch<2>(p, c, launched) : few_launch<4>(p, c, launched);
 }

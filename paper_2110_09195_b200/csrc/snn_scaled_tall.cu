@@ -1,0 +1,439 @@
+// Projections in 8-bit floating point with a scale for each block of 128, many rows: the 5th-generation tensor cores.
+#include "snn_products.h"
+
+#include "snn_pairs.cuh"
+#include "snn_products.cuh"
+#include "snn_tc_common.cuh"
+
+namespace snn {
+namespace {
+
+// out[row, co] = sum over blocks of 128 input channels of  xs[row, b] ws[co / 128, b] (x w)[row, co, b]:  D[128 or 256 rows x N channels] = x (M operand) * w^T (N
+// operand) for one block at a time, each into a buffer of its own in tensor memory, from where eight warps add it, times its scales, to sums in
+// registers (fp32).  Rows are the M operand so that a thread has one row: one factor for all of its channels of a block.  While they add one block up,
+// the next ones are multiplied: two buffers of 256 columns, or four.  Both operands come by TMA, the weights in the layout that they are kept in.
+//   CG = 2, N = 256: a pair of CTAs (one instruction for both), 128 rows and half of the channels' weights in each.  An SM then reads 64 bytes a cycle of
+//   operands, and as many arrive; alone with 128 x 256 it would be 96 and 96, more than shared memory gives.
+//   CG = 1, N = 128 or 64: fewer rows, more tiles, for problems that would leave SMs without any.
+constexpr int ST_ROWS = 128;          // of a CTA's tile
+constexpr int ST_A_BYTES = ST_ROWS * 128;
+constexpr int ST_BOX = 32;            // rows of one TMA box
+constexpr int ST_MAX_STAGES = 10;
+constexpr int ST_OUT_WARPS = 8;
+constexpr int ST_STAGING = 4096;      // of a warp: 32 rows of 128 bytes
+// warps: 0 copies, 1 MMA, 2 tensor memory, 4-11 sums and outputs
+
+struct TallScaledParams {
+  const float *w_scales, *x_scales;
+  const int32_t* offsets;
+  void* out;
+  long long ld_scales, ld_out;
+  int rows, E, C, K, n_kt, n_kb, out_type, n_ct, stages, fours, eights;   // fours, eights: scales and outputs by 16 bytes
+  int* status;
+};
+struct TallScaledBars {
+  uint64_t full[ST_MAX_STAGES], empty[ST_MAX_STAGES], d_full[4], d_empty[4], drain;
+  uint32_t tmem;
+};
+template <int CG, int N>
+struct TallScaledShape {
+  static constexpr int kBRows = N / CG;                            // of the weights, in each CTA
+  static constexpr int kStage = ST_A_BYTES + kBRows * 128;
+  static constexpr int kBuffers = N == 256 ? 2 : 4;
+  static constexpr int kColumns = N * kBuffers;                    // of tensor memory: 512, 512, 256
+  static constexpr int kFixed = 1024 + ST_OUT_WARPS * ST_STAGING + (int)sizeof(TallScaledBars);
+};
+
+// Issued by the lanes for which `on` is not 0: D = A * B^T over 128 input channels in four steps of 32, then the commits: the stage is free, the buffer is full.
+template <int CG>
+__device__ __forceinline__ void block_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on);
+template <>
+__device__ __forceinline__ void block_e4m3<2>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "setp.ne.b32 q, %6, 0;\n\t"
+      "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
+      "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, 0;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a1, b1, %3, 1;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a2, b2, %3, 1;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a3, b3, %3, 1;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], %7;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], %7;\n\t}" ::"r"(d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on), "h"((uint16_t)3)
+      : "memory");
+}
+template <>
+__device__ __forceinline__ void block_e4m3<1>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "setp.ne.b32 q, %6, 0;\n\t"
+      "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
+      "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a1, b1, %3, 1;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a2, b2, %3, 1;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a3, b3, %3, 1;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on)
+      : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void commit_drain(uint32_t bar, uint32_t on) {
+  if (CG == 2) commit_on(bar, on);
+  else if (on) tc_commit(bar);
+}
+template <int CG>
+__device__ __forceinline__ void copy_box(uint32_t dst, const void* map, int c, int row, uint32_t bar) {
+  if (CG == 2) tma_rows(dst, map, c, row, at_first(bar));
+  else
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(c), "r"(row), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ uint4 lds16_at(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float ld_plain(const float* p) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
+
+struct ScaledTile {
+  int e, r0, n, ct;   // expert, first row, rows, channel tile
+};
+struct ScaledRanges {
+  int *lo, *n, *end;   // end[e] counts the row tiles up to and with expert e
+};
+// Tile `index` of the launch, channels of the same rows one after the other; `t.e` is where the search begins (indices rise).
+template <int CG>
+__device__ __forceinline__ bool scaled_tile(const ScaledRanges& R, int E, int n_ct, int index, ScaledTile& t) {
+  const int q = index / n_ct;
+  int e = t.e;
+  while (e < E && q >= R.end[e]) ++e;
+  t.e = uni(e);
+  if (t.e >= E) return false;
+  const int k = q - (t.e ? R.end[t.e - 1] : 0);
+  t.ct = index - q * n_ct;
+  t.r0 = uni(R.lo[t.e] + k * CG * ST_ROWS);
+  t.n = uni(min(CG * ST_ROWS, R.n[t.e] - k * CG * ST_ROWS));
+  return true;
+}
+
+template <int CG, int N>
+__device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, const CUtensorMap& x_map, const CUtensorMap& w_map) {
+  using S = TallScaledShape<CG, N>;
+  constexpr int NB = S::kBuffers;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint8_t* const staging = smem + p.stages * S::kStage;
+  TallScaledBars* const bars = reinterpret_cast<TallScaledBars*>(staging + ST_OUT_WARPS * ST_STAGING);
+  ScaledRanges R;
+  R.lo = reinterpret_cast<int*>(bars + 1);
+  R.n = R.lo + p.E;
+  R.end = R.n + p.E;
+  const int warp = uni(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const uint32_t base = smem_u32(smem);
+  const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, first_tile = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
+  if (warp == 0) {
+    grid_dep_wait();
+    // tiles of each expert, summed up: every lane a run of experts
+    const int per = (p.E + 31) >> 5, e0 = lane * per, e1 = min(p.E, e0 + per);
+    int count = 0;
+    for (int e = e0; e < e1; ++e) {
+      const int lo = p.offsets ? clamp_offset(p.offsets[e], p.rows) : 0;
+      const int n = p.offsets ? max(clamp_offset(p.offsets[e + 1], p.rows) - lo, 0) : e ? 0 : p.rows;
+      R.lo[e] = lo;
+      R.n[e] = n;
+      count += (n + CG * ST_ROWS - 1) / (CG * ST_ROWS);
+    }
+    int upto = count;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += v;
+    }
+    int end = upto - count;
+    for (int e = e0; e < e1; ++e) R.end[e] = end += (R.n[e] + CG * ST_ROWS - 1) / (CG * ST_ROWS);
+  } else if (warp == 1 && lane == 0) {
+    for (int i = 0; i < p.stages; ++i) {
+      mbar_init(smem_u32(&bars->full[i]), 1);
+      mbar_init(smem_u32(&bars->empty[i]), 1);
+    }
+    for (int i = 0; i < NB; ++i) {
+      mbar_init(smem_u32(&bars->d_full[i]), 1);
+      mbar_init(smem_u32(&bars->d_empty[i]), CG * ST_OUT_WARPS);
+    }
+    mbar_init(smem_u32(&bars->drain), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_proxy_async();
+  } else if (warp == 2) {
+    // (not before the kernel before has ended: it may still have to get tensor memory of its own)
+    grid_dep_wait();
+    if (CG == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "n"(S::kColumns) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bars->tmem)), "n"(S::kColumns) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  if (warp > 2 || warp == 1) grid_dep_wait();
+  tc_fence_before();
+  __syncthreads();
+  if (CG == 2) pair_sync();
+  tc_fence_after();
+  grid_dep_launch();   // (only now: a dependent that has tensor memory before this CTA does would wait for it for good)
+  const uint32_t tmem = bars->tmem;
+  const int nk = p.n_kb;
+  bool ok = true;
+  ScaledTile t{};
+
+  if (warp < 4) {
+    if (N == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0) {
+      // ------------------------------------------------------------ copies: a stage is 128 input channels of the rows and of the weights
+      int s = 0, filled = 0;
+      uint32_t phase = 0;
+      for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
+        auto boxes = [&](int r) { return (min(max(t.n - r * ST_ROWS, 0), ST_ROWS) + ST_BOX - 1) / ST_BOX; };
+        const int mine = boxes(rank);
+        const uint32_t bytes = (uint32_t)(boxes(0) + (CG == 2 ? boxes(1) : 0)) * (ST_BOX * 128) + CG * S::kBRows * 128;   // of both CTAs
+        const int kt = N == 256 ? min(2 * t.ct + rank, p.n_kt - 1) : N == 128 ? t.ct : t.ct >> 1;
+        const int w_row0 = (t.e * p.n_kt + kt) * nk, w_half = N == 64 ? (t.ct & 1) * 64 : 0;
+        for (int kb = 0; kb < nk; ++kb) {
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->empty[s]), phase ^ 1u));
+          if (!ok) break;
+          const uint32_t full = smem_u32(&bars->full[s]), dst = base + s * S::kStage;
+          if (rank == 0 && lane == 0) mbar_expect_tx(full, bytes);
+          __syncwarp();
+          if (lane < mine) copy_box<CG>(dst + lane * ST_BOX * 128, &x_map, kb * 128, t.r0 + rank * ST_ROWS + lane * ST_BOX, full);
+          else if (lane == 4) copy_box<CG>(dst + ST_A_BYTES, &w_map, 0, (w_row0 + kb) * 128 + w_half, full);
+          __syncwarp();
+          filled = min(filled + 1, p.stages);
+          if (++s == p.stages) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      // both CTAs' copies in flight land before the pair ends, whatever became of the other warps
+      for (int i = 0; rank == 0 && i < filled; ++i) {
+        if (--s < 0) {
+          s = p.stages - 1;
+          phase ^= 1u;
+        }
+        ok = mbar_wait(smem_u32(&bars->full[s]), phase) && ok;
+      }
+      if (!ok && lane == 0) raise_status(p.status, 31);
+    } else if (warp == 1 && rank == 0) {
+      // ------------------------------------------------------------ MMA, for both CTAs
+      int s = 0, d = 0;
+      uint32_t phase = 0, d_phase = 0;
+      const uint32_t leader = elect_one(), tmem_u = (uint32_t)uni((int)tmem);
+      const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(CG * ST_ROWS >> 4) << 24);   // fp32 sums of e4m3 values
+      for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
+        for (int kb = 0; kb < nk; ++kb) {
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_empty[d]), d_phase ^ 1u) && mbar_wait(smem_u32(&bars->full[s]), phase));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t a = base + s * S::kStage;
+          block_e4m3<CG>(tmem_u + d * N, rows_desc(a), rows_desc(a + ST_A_BYTES), idesc, smem_u32(&bars->empty[s]), smem_u32(&bars->d_full[d]), leader);
+          __syncwarp();
+          if (++s == p.stages) {
+            s = 0;
+            phase ^= 1u;
+          }
+          if (++d == NB) {
+            d = 0;
+            d_phase ^= 1u;
+          }
+        }
+      }
+      commit_drain<CG>(smem_u32(&bars->drain), leader);
+      __syncwarp();
+      ok = mbar_wait(smem_u32(&bars->drain), 0) && ok;
+      if (!ok && lane == 0) raise_status(p.status, 32);
+    }
+  } else {
+    // ------------------------------------------------------------ sums: a thread has a row and half of the tile's channels
+    if (N == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    constexpr int A = N / 2;
+    const int quarter = warp & 3, half = (warp - 4) >> 2, row = quarter * 32 + lane;
+    const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + half * A, stage = smem_u32(staging) + (warp - 4) * ST_STAGING;
+    int d = 0;
+    uint32_t d_phase = 0;
+    for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
+      const int n = t.n - rank * ST_ROWS, co0 = t.ct * N + half * A;   // rows of this CTA's (0 or less: none), first channel
+      const float* const xs = p.x_scales + (size_t)(t.r0 + min(rank * ST_ROWS + row, t.n - 1)) * (size_t)p.ld_scales;
+      const float* const ws = p.w_scales + ((size_t)t.e * p.n_kt + min(co0 >> 7, p.n_kt - 1)) * nk;
+      float next[4];
+      auto load = [&](int kb) {   // four blocks' factors
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p.fours) {
+          const uint4 u = ld16(xs + kb);
+          v = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+        } else {
+          v.x = ld_plain(xs + kb);
+          if (kb + 1 < nk) v.y = ld_plain(xs + kb + 1);
+          if (kb + 2 < nk) v.z = ld_plain(xs + kb + 2);
+          if (kb + 3 < nk) v.w = ld_plain(xs + kb + 3);
+        }
+        next[0] = v.x * ld_plain(ws + kb);
+        next[1] = kb + 1 < nk ? v.y * ld_plain(ws + kb + 1) : 0.f;
+        next[2] = kb + 2 < nk ? v.z * ld_plain(ws + kb + 2) : 0.f;
+        next[3] = kb + 3 < nk ? v.w * ld_plain(ws + kb + 3) : 0.f;
+      };
+      load(0);
+      float acc[A];
+#pragma unroll
+      for (int i = 0; i < A; ++i) acc[i] = 0.f;
+      for (int kb = 0; ok && kb < nk; kb += 4) {
+        const float f[4] = {next[0], next[1], next[2], next[3]};
+        if (kb + 4 < nk) load(kb + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (kb + i >= nk) break;
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), d_phase));
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < A; c += 32) {
+            uint32_t v[32];
+            tmem_ld32(src + d * N + c, v);
+            if (c + 32 == A) {   // (all of the buffer has been read)
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) {
+                if (CG == 2) arrive_at_first(smem_u32(&bars->d_empty[d]));
+                else mbar_arrive(smem_u32(&bars->d_empty[d]));
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) acc[c + j] = fmaf(f[i], __uint_as_float(v[j]), acc[c + j]);
+          }
+          if (++d == NB) {
+            d = 0;
+            d_phase ^= 1u;
+          }
+        }
+      }
+      if (!ok) break;
+      // Outputs through shared memory, 128 bytes of each row at a time (16-byte pieces, their order by the row: no bank twice), so that whole lines go out.
+      const long long to = (long long)(t.r0 + rank * ST_ROWS + quarter * 32) * p.ld_out;
+      const int rows = min(n - quarter * 32, 32);
+      auto pass = [&](auto words, int co, int each) {   // `each` values in 16 bytes
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sts16(stage + lane * 128 + ((q ^ (lane & 7)) << 4), words(q));
+        __syncwarp();
+        const int piece = lane & 7, c = co + piece * each, size = 16 / each;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = 4 * i + (lane >> 3);
+          const uint4 v = lds16_at(stage + r * 128 + ((piece ^ (r & 7)) << 4));
+          if (r >= rows) continue;
+          uint8_t* const at = static_cast<uint8_t*>(p.out) + (to + (long long)r * p.ld_out + c) * size;
+          if (p.eights && c + each <= p.K) *reinterpret_cast<uint4*>(at) = v;
+          else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (size == 4) {
+                if (c + j < p.K) reinterpret_cast<uint32_t*>(at)[j] = w[j];
+              } else {
+                if (c + 2 * j < p.K) reinterpret_cast<uint16_t*>(at)[2 * j] = (uint16_t)w[j];
+                if (c + 2 * j + 1 < p.K) reinterpret_cast<uint16_t*>(at)[2 * j + 1] = (uint16_t)(w[j] >> 16);
+              }
+          }
+        }
+      };
+      if (rows > 0 && co0 < p.K) {   // (the same for all lanes)
+        if (p.out_type == SNN_OUT_F32) {
+#pragma unroll
+          for (int c = 0; c < A; c += 32)
+            pass([&](int q) { return make_uint4(__float_as_uint(acc[c + 4 * q]), __float_as_uint(acc[c + 4 * q + 1]), __float_as_uint(acc[c + 4 * q + 2]), __float_as_uint(acc[c + 4 * q + 3])); },
+                 co0 + c, 4);
+        } else if (A >= 64) {
+#pragma unroll
+          for (int c = 0; c < A; c += 64)
+            pass([&](int q) {
+              uint32_t w[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, make_float2(acc[c + 8 * q + 2 * j], acc[c + 8 * q + 2 * j + 1]));
+              return make_uint4(w[0], w[1], w[2], w[3]);
+            }, co0 + c, 8);
+        } else {   // (32 channels: half of a pass, the other half is not there)
+          pass([&](int q) {
+            uint32_t w[4] = {};
+            if (q < 4)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, make_float2(acc[(8 * q + 2 * j) % A], acc[(8 * q + 2 * j + 1) % A]));
+            return make_uint4(w[0], w[1], w[2], w[3]);
+          }, (lane & 7) < 4 ? co0 : p.K, 8);
+        }
+      }
+    }
+    if (!ok && lane == 0) raise_status(p.status, 33);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) mbar_wait(smem_u32(&bars->drain), 0);   // (the last arrival here from the pair's MMAs)
+  __syncwarp();
+  if (CG == 2) pair_sync();
+  tc_fence_after();
+  if (warp == 2) {
+    if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kColumns) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kColumns) : "memory");
+  }
+}
+constexpr int ST_THREADS = 128 + 32 * ST_OUT_WARPS;
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ST_THREADS, 1)
+    scaled_pair_kernel(const TallScaledParams p, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map) {
+  scaled_tall_body<2, 256>(p, x_map, w_map);
+}
+template <int N>
+__global__ void __launch_bounds__(ST_THREADS, 1) scaled_single_kernel(const TallScaledParams p, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map) {
+  scaled_tall_body<1, N>(p, x_map, w_map);
+}
+
+bool rows_map(CUtensorMap* map, const void* base, long long columns, long long rows, long long ld, int box_rows, bool swizzled) {
+  const MapEncoder encode = map_encoder();
+  const cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int CG, int N, class Kernel>
+cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p, const ScaledCall& c, int* launched) {
+  using S = TallScaledShape<CG, N>;
+  cudaError_t e = allow_max_smem(kernel, done);
+  if (e != cudaSuccess) return e;
+  CUtensorMap x_map, w_map;
+  if (!rows_map(&x_map, c.act, p.C, c.rows, c.ld_act, ST_BOX, true) ||
+      !rows_map(&w_map, p.tiles, 128, (long long)p.E * p.n_kt * p.n_kb * 128, 128, S::kBRows, false))
+    return cudaErrorInvalidValue;
+  const int size = c.out_type == SNN_OUT_F32 ? 4 : 2, fixed = S::kFixed + p.E * 12;
+  const TallScaledParams q{p.scales, c.scales, c.offsets, c.out, c.ld_scales, c.ld_out, c.rows, p.E, p.C, p.K, p.n_kt, p.n_kb, c.out_type, (p.K + N - 1) / N,
+                           min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::kStage), p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
+                           c.ld_out * size % 16 == 0 && ((uintptr_t)c.out & 15) == 0, p.status_dev};
+  const long long tiles = ((long long)c.rows / (CG * ST_ROWS) + (c.offsets ? min(p.E, c.rows) : 1)) * q.n_ct;
+  *launched += 1;
+  return launch_dependent(kernel, (unsigned)(CG * min(tiles, (long long)max(1, sm_count() / CG))), ST_THREADS, (size_t)(fixed + q.stages * S::kStage), c.stream, q, x_map, w_map);
+}
+
+}  // namespace
+
+cudaError_t scaled_tall(const Scaled& p, const ScaledCall& c, int shape, int* launched) {
+  static unsigned long long done[3] = {0, 0, 0};
+  if (shape == 256) return tall_launch<2, 256>(scaled_pair_kernel, done, p, c, launched);
+  if (shape == 128) return tall_launch<1, 128>(scaled_single_kernel<128>, done + 1, p, c, launched);
+  return tall_launch<1, 64>(scaled_single_kernel<64>, done + 2, p, c, launched);
+}
+
+}  // namespace snn
