@@ -391,6 +391,7 @@ SNN_API snn_status_t snn_conv_adapters_destroy(snn_conv_adapters_t* h);
  * snn_conv_experts_activate: out[r][c] = fn(gate[r][c]) * up[r][c], or fn(up[r][c]) where gate_dev is NULL, in fp32, one
  * rounding to out_type.  gate and up are of one type (`type`; both and out_type SNN_OUT_F32, SNN_OUT_F16 or SNN_OUT_BF16); rows
  * lie ld elements apart, each aligned to its element.  out may be gate or up itself where type, pointer and ld are the same.
+ * UNSUPPORTED: 2^34 values or more.
  */
 enum { SNN_FN_NONE = 0, SNN_FN_RELU = 1, SNN_FN_SILU = 2, SNN_FN_GELU = 3 };
 SNN_API snn_status_t snn_conv_experts_activate(const void* gate_dev, int64_t ld_gate, const void* up_dev, int64_t ld_up,
@@ -441,7 +442,8 @@ SNN_API snn_status_t snn_conv_moe_destroy(snn_conv_moe_t* m);
  * rows ld_scales apart.  Row i belongs to projection e with offsets[e] <= i < offsets[e + 1] (DEVICE, count + 1 ints, as the router
  * writes them; what lies outside [0, act_rows] is taken for the nearest end); offsets_dev NULL: all rows are projection 0's.  Rows of the
  * output without a projection are left as they are.  Infinite or NaN values or scales of a row reach that row's outputs and no others.
- * Calls may overlap.  UNSUPPORTED: above 2^30 rows, or where (act_rows / 8 + count) * ceil(c_out / 16) reaches 2^31.
+ * Calls may overlap.  UNSUPPORTED: above 2^30 rows, or where (act_rows / 8 + 1) * count or
+ * (act_rows / 8 + count) * ceil(c_out / 16) reaches 2^31.
  */
 #define SNN_SCALED_BLOCK 128
 typedef struct snn_conv_scaled snn_conv_scaled_t; /* opaque; owned by the library */
@@ -458,7 +460,7 @@ SNN_API snn_status_t snn_conv_scaled_destroy(snn_conv_scaled_t* h);
  * v is up[r][c], or behind an activation fn(up[r][c]) or fn(gate[r][c]) * up[r][c], in fp32.  Output row i is of input row rows[i] (DEVICE, out_rows ints; an
  * index outside [0, in_rows) stands for a row of zeros), or without rows_dev of row i (out_rows = in_rows).
  * values_dev [out_rows] rows ld_values bytes apart, scales_dev [out_rows][ceil(columns / 128)] fp32, rows ld_scales apart; nothing is written
- * between the rows.
+ * between the rows.  UNSUPPORTED: 2^34 values or more.
  */
 SNN_API snn_status_t snn_conv_scaled_quantise(const void* gate_dev, int64_t ld_gate, const void* up_dev, int64_t ld_up, int32_t type,
                                               int32_t in_rows, const int32_t* rows_dev, int32_t out_rows, int32_t columns, int32_t fn,

@@ -161,6 +161,7 @@ class _PythonChecks:
 
     group_forward = stack_forward = static_forward = layer_forward
     experts_forward = adapters_forward = route = combine = layer_forward
+    moe_forward = scaled_forward = quantise = activate = layer_forward
 
 
 def _load_fast():
@@ -178,6 +179,9 @@ def _load_fast():
             module.bind_projections(*(ctypes.cast(f, ctypes.c_void_p).value
                                       for f in (lib.snn_conv_experts_forward, lib.snn_conv_adapters_forward, lib.snn_conv_experts_route,
                                                 lib.snn_conv_experts_combine, lib.snn_conv_experts_route_work)))
+            module.bind_mixture(*(ctypes.cast(f, ctypes.c_void_p).value
+                                  for f in (lib.snn_conv_moe_forward, lib.snn_conv_moe_work, lib.snn_conv_scaled_forward, lib.snn_conv_scaled_quantise,
+                                            lib.snn_conv_experts_activate)))
             module.bind_static(ctypes.cast(lib.snn_conv_forward_static, ctypes.c_void_p).value, np.ndarray)
         except (ImportError, AttributeError) as e:   # (AttributeError: a module built from older source)
             warnings.warn(f"the forward calls are checked in Python, which takes longer: {e} "

@@ -361,6 +361,139 @@ PyObject* combine(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the whole mixture, activations, and the form of 8 bits
+using MoeForward = snn_status_t (*)(snn_conv_moe_t*, const void*, int32_t, int32_t, int64_t, const void*, int32_t, int64_t, int32_t, int32_t, void*, void*, int32_t,
+                                    int64_t, void*);
+using MoeWork = int64_t (*)(const snn_conv_moe_t*, int32_t, int32_t);
+using ScaledForward = snn_status_t (*)(snn_conv_scaled_t*, const void*, int64_t, const float*, int64_t, const int32_t*, int32_t, void*, int32_t, int64_t, void*);
+using Quantise = snn_status_t (*)(const void*, int64_t, const void*, int64_t, int32_t, int32_t, const int32_t*, int32_t, int32_t, int32_t, void*, int64_t, float*, int64_t,
+                                  int32_t, void*);
+using Activate = snn_status_t (*)(const void*, int64_t, const void*, int64_t, int32_t, int32_t, int32_t, int32_t, void*, int32_t, int64_t, int32_t, void*);
+MoeForward g_moe = nullptr;
+MoeWork g_moe_work = nullptr;
+ScaledForward g_scaled = nullptr;
+Quantise g_quantise = nullptr;
+Activate g_activate = nullptr;
+
+// A matrix of e4m3 values.
+struct Values {
+  const at::Tensor* t = nullptr;
+  int64_t rows = 0, columns = 0, ld = 0;
+  bool take(PyObject* o, int device) {
+    t = on_device(o, device);
+    if (!t || t->dim() != 2 || t->scalar_type() != at::kFloat8_e4m3fn) return false;
+    rows = t->size(0);
+    columns = t->size(1);
+    ld = rows > 1 ? t->stride(0) : (columns + 15) / 16 * 16;
+    return (columns <= 1 || t->stride(1) == 1) && ld >= columns && rows <= INT32_MAX && columns <= INT32_MAX;
+  }
+};
+
+// moe_forward(description, x, logits, top_k, normalise, out)
+PyObject* moe_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    const Projection* d = n == 6 ? described<Projection>(a[0], sizeof(Projection)) : nullptr;
+    Matrix x, logits, y;
+    int32_t k = 0;
+    if (!d || !d->handle || !g_moe || !x.take(a[1], d->device) || !logits.take(a[2], d->device) || !int_between(a[3], 1, SNN_ROUTE_TOP_MAX, &k) || !PyBool_Check(a[4]) ||
+        !y.take(a[5], d->device) || x.act_type() < 0 || x.columns != d->c_in || y.columns != d->c_out || logits.columns != d->count || logits.rows != x.rows ||
+        y.rows != x.rows || c10::cuda::current_device() != d->device)
+      return kUnusual;
+    snn_conv_moe_t* const h = reinterpret_cast<snn_conv_moe_t*>(d->handle);
+    const int64_t bytes = x.rows <= SNN_MOE_TOKENS_MAX ? g_moe_work(h, (int32_t)x.rows, k) : -1;
+    if (bytes < 0) return kUnusual;
+    void* const stream = current_stream(d->device);
+    const c10::DataPtr work = c10::cuda::CUDACachingAllocator::get()->allocate((size_t)bytes);   // (of the current stream)
+    const void *act = x.t->data_ptr(), *from = logits.t->data_ptr();
+    void* const out = y.t->data_ptr();
+    return unlocked([&] {
+      return g_moe(h, act, x.act_type(), (int32_t)x.rows, x.ld, from, logits.type, logits.ld, k, a[4] == Py_True, work.get(), out, y.type, y.ld, stream);
+    });
+  });
+}
+
+// scaled_forward(description, x, scales, offsets or None, out)
+PyObject* scaled_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    const Projection* d = n == 5 ? described<Projection>(a[0], sizeof(Projection)) : nullptr;
+    Values x;
+    Matrix scales, y;
+    if (!d || !d->handle || !g_scaled || !x.take(a[1], d->device) || !scales.take(a[2], d->device) || !y.take(a[4], d->device) || x.columns != d->c_in ||
+        y.columns != d->c_out || y.rows != x.rows || scales.type != SNN_OUT_F32 || scales.rows != x.rows || scales.columns != ((int64_t)d->c_in + 127) / 128)
+      return kUnusual;
+    const at::Tensor* offsets = a[3] == Py_None ? nullptr : dense(a[3], d->device, at::kInt, {d->count + 1});
+    if (!offsets && a[3] != Py_None) return kUnusual;
+    const void* const act = x.t->data_ptr();
+    const float* const xs = scales.t->data_ptr<float>();
+    const int32_t* const off = offsets ? offsets->data_ptr<int32_t>() : nullptr;
+    void* const out = y.t->data_ptr();
+    void* const stream = current_stream(d->device);
+    return unlocked([&] { return g_scaled(reinterpret_cast<snn_conv_scaled_t*>(d->handle), act, x.ld, xs, scales.ld, off, (int32_t)x.rows, out, y.type, y.ld, stream); });
+  });
+}
+
+// quantise(up, gate or None, fn, rows or None, values, scales)
+PyObject* quantise(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Matrix up, gate, scales;
+    Values values;
+    int32_t fn = 0;
+    if (n != 6 || !g_quantise || !up.take(a[0], -1) || !int_between(a[2], SNN_FN_NONE, SNN_FN_GELU, &fn)) return kUnusual;
+    const int device = up.t->get_device();
+    if (a[1] != Py_None && (!gate.take(a[1], device) || gate.type != up.type || gate.rows != up.rows || gate.columns != up.columns)) return kUnusual;
+    if (!values.take(a[4], device) || !scales.take(a[5], device)) return kUnusual;
+    const at::Tensor* rows = a[3] == Py_None ? nullptr : dense(a[3], device, at::kInt, {values.rows});
+    if ((!rows && a[3] != Py_None) || (!rows && values.rows != up.rows) || values.columns != up.columns || scales.type != SNN_OUT_F32 || scales.rows != values.rows ||
+        scales.columns != (up.columns + 127) / 128)
+      return kUnusual;
+    const void *const from = up.t->data_ptr(), *const by = gate.t ? gate.t->data_ptr() : nullptr;
+    const int32_t* const index = rows ? rows->data_ptr<int32_t>() : nullptr;
+    void* const to = values.t->data_ptr();
+    float* const s = scales.t->data_ptr<float>();
+    void* const stream = current_stream(device);
+    return unlocked([&] {
+      return g_quantise(by, gate.ld, from, up.ld, up.type, (int32_t)up.rows, index, (int32_t)values.rows, (int32_t)up.columns, fn, to, values.ld, s, scales.ld, device, stream);
+    });
+  });
+}
+
+// activate(up, gate or None, fn, out)
+PyObject* activate(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Matrix up, gate, out;
+    int32_t fn = 0;
+    if (n != 4 || !g_activate || !up.take(a[0], -1) || !int_between(a[2], SNN_FN_NONE, SNN_FN_GELU, &fn)) return kUnusual;
+    const int device = up.t->get_device();
+    if (a[1] != Py_None && (!gate.take(a[1], device) || gate.type != up.type || gate.rows != up.rows || gate.columns != up.columns)) return kUnusual;
+    if (!out.take(a[3], device) || out.rows != up.rows || out.columns != up.columns) return kUnusual;
+    const void *const from = up.t->data_ptr(), *const by = gate.t ? gate.t->data_ptr() : nullptr;
+    void* const to = out.t->data_ptr();
+    void* const stream = current_stream(device);
+    return unlocked([&] {
+      return g_activate(by, gate.ld, from, up.ld, up.type, (int32_t)up.rows, (int32_t)up.columns, fn, to, out.type, out.ld, device, stream);
+    });
+  });
+}
+
+// bind_mixture(moe, moe_work, scaled, quantise, activate): addresses of the library's entry points
+PyObject* bind_mixture(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "bind_mixture takes five addresses");
+    return nullptr;
+  }
+  void* p[5];
+  for (int i = 0; i < 5; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i] && PyErr_Occurred()) return nullptr;
+  }
+  g_moe = reinterpret_cast<MoeForward>(p[0]);
+  g_moe_work = reinterpret_cast<MoeWork>(p[1]);
+  g_scaled = reinterpret_cast<ScaledForward>(p[2]);
+  g_quantise = reinterpret_cast<Quantise>(p[3]);
+  g_activate = reinterpret_cast<Activate>(p[4]);
+  Py_RETURN_NONE;
+}
+
 // bind_projections(experts, adapters, route, combine, route_work): addresses of the library's entry points
 PyObject* bind_projections(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 5) {
@@ -420,6 +553,11 @@ PyMethodDef methods[] = {
     {"adapters_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(adapters_forward)), METH_FASTCALL, nullptr},
     {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(route)), METH_FASTCALL, nullptr},
     {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(combine)), METH_FASTCALL, nullptr},
+    {"moe_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(moe_forward)), METH_FASTCALL, nullptr},
+    {"scaled_forward", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(scaled_forward)), METH_FASTCALL, nullptr},
+    {"quantise", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quantise)), METH_FASTCALL, nullptr},
+    {"activate", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(activate)), METH_FASTCALL, nullptr},
+    {"bind_mixture", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_mixture)), METH_FASTCALL, nullptr},
     {"bind_projections", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_projections)), METH_FASTCALL, nullptr},
     {"bind_static", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind_static)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind)), METH_FASTCALL, nullptr},

@@ -38,7 +38,7 @@ snn_status_t snn_conv_experts_activate(const void* gate_dev, int64_t ld_gate, co
   if (st != SNN_OK) return st;
   if (!out_ok(out_type)) return api_fail(SNN_ERR_INVALID_ARG, "outputs are SNN_OUT_F32, SNN_OUT_F16 or SNN_OUT_BF16, not %d", out_type);
   if (ld_out < columns) return api_fail(SNN_ERR_INVALID_ARG, "rows of %lld outputs for %d columns", (long long)ld_out, columns);
-  if ((long long)rows * columns >= (1ll << 38)) return api_fail(SNN_ERR_UNSUPPORTED, "%d rows of %d columns: split the call", rows, columns);
+  if ((long long)rows * columns >= (1ll << 34)) return api_fail(SNN_ERR_UNSUPPORTED, "%d rows of %d columns: split the call", rows, columns);
   if (rows == 0) return SNN_OK;
   if (!up_dev || !out_dev) return api_fail(SNN_ERR_INVALID_ARG, "null device pointer");
   if ((uintptr_t)out_dev & (out_size(out_type) - 1)) return api_fail(SNN_ERR_INVALID_ARG, "misaligned device pointer");
@@ -181,7 +181,7 @@ snn_status_t snn_conv_scaled_quantise(const void* gate_dev, int64_t ld_gate, con
   if (out_rows < 0 || (!rows_dev && out_rows != in_rows)) return api_fail(SNN_ERR_INVALID_ARG, "%d rows of outputs for %d rows without an index", out_rows, in_rows);
   if (ld_values < columns || ld_scales < ((long long)columns + 127) / 128)
     return api_fail(SNN_ERR_INVALID_ARG, "rows of %lld values and %lld scales for %d columns", (long long)ld_values, (long long)ld_scales, columns);
-  if ((long long)out_rows * columns >= (1ll << 38)) return api_fail(SNN_ERR_UNSUPPORTED, "%d rows of %d columns: split the call", out_rows, columns);
+  if ((long long)out_rows * columns >= (1ll << 34)) return api_fail(SNN_ERR_UNSUPPORTED, "%d rows of %d columns: split the call", out_rows, columns);
   if (out_rows == 0) return SNN_OK;
   if ((in_rows > 0 && !up_dev) || !values_dev || !scales_dev) return api_fail(SNN_ERR_INVALID_ARG, "null device pointer");
   if (((uintptr_t)rows_dev | (uintptr_t)scales_dev) & 3) return api_fail(SNN_ERR_INVALID_ARG, "misaligned device pointer");

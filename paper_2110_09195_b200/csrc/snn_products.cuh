@@ -227,12 +227,88 @@ __device__ __forceinline__ float value(const void* y, int type, long long i) {
   return __bfloat162float(static_cast<const __nv_bfloat16*>(y)[i]);
 }
 
+// Two fp32 operations an instruction, each rounded as by itself.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 floats_of(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float exp2_approx(float v) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float reciprocal_approx(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// v / (1 + exp(-v)), twice.  The exponential by powers of 2 with the product's rest (what the first number leaves of v / ln 2) in a second factor: within 2^-21.  (Of v
+// below -88 the result is 0: less than the smallest normal number.)
+__device__ __forceinline__ uint64_t silu2(uint64_t v) {
+  constexpr float L = -1.44269504088896340736f, L_rest = -1.44269504088896340736 - (double)L, ln2 = 0.69314718055994530942f;
+  const float2 f = floats_of(v);
+  const uint64_t c = pair_of(fminf(fmaxf(f.x, -126.f), 126.f), fminf(fmaxf(f.y, -126.f), 126.f));   // (infinities would leave a rest that is none)
+  const uint64_t h = mul2(c, pair_of(L, L));
+  const float2 hs = floats_of(h);
+  const uint64_t rest = fma2(c, pair_of(L, L), pair_of(-hs.x, -hs.y));
+  const uint64_t e = pair_of(exp2_approx(hs.x), exp2_approx(hs.y));
+  const uint64_t factor = fma2(fma2(c, pair_of(L_rest, L_rest), rest), pair_of(ln2, ln2), pair_of(1.f, 1.f));
+  const float2 d = floats_of(fma2(e, factor, pair_of(1.f, 1.f)));
+  return mul2(v, pair_of(reciprocal_approx(d.x), reciprocal_approx(d.y)));
+}
+
+// The normal distribution's function.  For z = |v|:  exp(-z^2 / 2) times a smooth factor, which is P(u) / (z + k), u = 1 - 2 k / (z + k) in [-1, 1), with P fitted for the
+// least relative error (2^-23 up to z = 13.3, from values of erfc in 64 bits); z^2 / 2 as a sum of two numbers.  Within 2^-20.4 of the value where that is a normal
+// number, on both sides.  (normcdff takes 60 instructions; with them the activation of 8191 x 4096 gated bf16 values took 78 us.)
+__device__ __forceinline__ float normal_cdf(float v) {
+  constexpr float k = 4.25f, L = -0.72134752044448170368f, L_rest = -0.72134752044448170368 - (double)L;   // 1 / (2 ln 2)
+  const float z = fminf(fabsf(v), 14.5f);   // (from there on 0; NaN is in the other factor)
+  const float r = __fdividef(1.f, z + k), u = fmaf(-2.f * k, r, 1.f);
+  float p = 0.0021056882105767727f;
+  p = fmaf(p, u, -0.0010409007081761956f);
+  p = fmaf(p, u, -0.01938452757894993f);
+  p = fmaf(p, u, 0.08534717559814453f);
+  p = fmaf(p, u, -0.22050929069519043f);
+  p = fmaf(p, u, 0.41822102665901184f);
+  p = fmaf(p, u, -0.6251299977302551f);
+  p = fmaf(p, u, 0.7595543265342712f);
+  const float square = z * z, h = square * L, rest = fmaf(square, L_rest, fmaf(fmaf(z, z, -square), L, fmaf(square, L, -h)));
+  const float e = exp2_approx(h), lower = p * r * fmaf(e, rest * 0.69314718056f, e);
+  return v < 0.f ? lower : 1.f - lower;
+}
+
 // What stands between two projections (SNN_FN_*): with a gate, fn(gate) * up.
 __device__ __forceinline__ float activated(int fn, float v) {
-  if (fn == SNN_FN_SILU) return v / (1.f + expf(-v));
-  if (fn == SNN_FN_GELU) return v * normcdff(v);   // (no 1 + erf(v): that loses the digits of a negative v)
+  if (fn == SNN_FN_SILU) return floats_of(silu2(pair_of(v, v))).x;
+  if (fn == SNN_FN_GELU) return v * normal_cdf(v);   // (no 1 + erf(v): that loses the digits of a negative v)
   if (fn == SNN_FN_RELU) return v < 0.f ? 0.f : v;   // (NaN stays)
   return v;
+}
+__device__ __forceinline__ uint64_t activated2(int fn, uint64_t v) {
+  if (fn == SNN_FN_SILU) return silu2(v);
+  const float2 f = floats_of(v);
+  return pair_of(activated(fn, f.x), activated(fn, f.y));
 }
 
 }  // namespace

@@ -1,5 +1,8 @@
 // Rows between two projections: activations, and the form of 8 bits with a scale for each 128 channels.
 #include <cuda_fp8.h>
+#include <math_constants.h>
+
+#include <type_traits>
 
 #include "snn_products.h"
 
@@ -9,21 +12,33 @@
 namespace snn {
 namespace {
 
+// q / d for q below 2^31, by a multiplication.  (A division of 64 bits by each thread took as long as the activation.)
+struct Divisor {
+  uint32_t d, m, s;
+  explicit Divisor(uint32_t by) : d(by), s(0) {
+    while ((1ull << s) < d) ++s;
+    m = (uint32_t)((1ull << (31 + s)) / d + 1);
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t q) const { return __umulhi(2u * q, m) >> s; }
+};
+
 struct ActivateParams {
   const void *gate, *up;
   void* out;
   long long ld_gate, ld_up, ld_out;
-  int rows, columns, groups, fn, type, out_type;
+  int rows, columns, fn, type, out_type;
+  Divisor each;   // eights of a row, or 256ths
 };
 
 // A thread has 8 neighbouring columns.  Bound by memory: each value is read and written once, and leaves the caches first.
 template <class Y, bool GATE>
 __global__ void __launch_bounds__(256) activate_kernel(const ActivateParams p) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, r = i / p.groups;
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+  const long long r = p.each(i);
   grid_dep_wait();
   grid_dep_launch();
   if (r >= p.rows) return;
-  const int c = (int)(i - r * p.groups) * 8;
+  const int c = (int)(i - (uint32_t)r * p.each.d) * 8;
   using E = typename Element<Y>::type;
   Eight<Y> u, g;
   u.load(static_cast<const E*>(p.up) + r * p.ld_up + c);
@@ -32,11 +47,12 @@ __global__ void __launch_bounds__(256) activate_kernel(const ActivateParams p) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const float2 a = u.pair(q);
+    const uint64_t w = pair_of(a.x, a.y);
     if (GATE) {
       const float2 b = g.pair(q);
-      v[q] = make_float2(activated(p.fn, b.x) * a.x, activated(p.fn, b.y) * a.y);
+      v[q] = floats_of(mul2(activated2(p.fn, pair_of(b.x, b.y)), w));
     } else {
-      v[q] = make_float2(activated(p.fn, a.x), activated(p.fn, a.y));
+      v[q] = floats_of(activated2(p.fn, w));
     }
   }
   const long long at = r * p.ld_out + c;
@@ -52,11 +68,11 @@ __global__ void __launch_bounds__(256) activate_kernel(const ActivateParams p) {
 
 // The same where columns, row lengths or pointers are not multiples of 8 values: one column a thread.
 __global__ void __launch_bounds__(256) activate_odd_kernel(const ActivateParams p) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, r = i / p.columns;
+  const long long r = p.each(blockIdx.x);
+  const int c = (int)(blockIdx.x - (uint32_t)r * p.each.d) * 256 + (int)threadIdx.x;
   grid_dep_wait();
   grid_dep_launch();
-  if (r >= p.rows) return;
-  const int c = (int)(i - r * p.columns);
+  if (c >= p.columns) return;
   const float u = value(p.up, p.type, r * p.ld_up + c);
   store_out(p.out, p.out_type, r * p.ld_out + c, p.gate ? activated(p.fn, value(p.gate, p.type, r * p.ld_gate + c)) * u : activated(p.fn, u));
 }
@@ -67,76 +83,111 @@ struct QuantiseParams {
   uint8_t* values;
   float* scales;
   long long ld_gate, ld_up, ld_values, ld_scales;
-  int in_rows, out_rows, columns, blocks, fn, type;
+  int in_rows, out_rows, columns, fn, type;
+  Divisor blocks;   // of a row
 };
 
 constexpr float kLargest = 448.f, kLeastScale = 0x1p-70f;
 
-// 16 lanes have a block of 128 channels of a row, 8 each: the largest magnitude by four shuffles, one division for the scale and one for each value
-// (by the scale, not times its reciprocal: 16-bit values often lie on a border between two of 8 bits, and go the way that the formula
-// says).  ODD: columns, row lengths or pointers that are not multiples of 8 values.  Bound by memory.
+// v / scale in fp32, by the scale's reciprocal (itself rounded once): the product is within 1.5 steps, and a correction of it within 2^-46 of the quotient before it is
+// rounded; a second one then gives the quotient's nearest number (Markstein, IBM Journal of Research and Development 34, 1990).  ONCE: values of 16 bits.  One correction is
+// then enough: what could go another way is a quotient that lies next to a number halfway between two fp32 numbers one of which is a border of the 8-bit values, and a value of
+// 11 bits over one of 24 comes no nearer to it than 2^-35.  (Behind an activation the value itself is rounded.)  scale is at least 2^-70 and at most 2^120, so that
+// nothing that reaches a step of the 8-bit value underflows; an infinity becomes NaN.  (Not v times the reciprocal: 16-bit values often lie on a border
+// between two of 8 bits, and go the way that the formula says.)
+template <bool ONCE>
+__device__ __forceinline__ uint64_t quotients(uint64_t v, uint64_t minus_scale, uint64_t inverse) {
+  uint64_t q = mul2(v, inverse);
+  q = fma2(fma2(q, minus_scale, v), inverse, q);
+  return ONCE ? q : fma2(fma2(q, minus_scale, v), inverse, q);
+}
+
+// 8 lanes have a block of 128 channels of a row, 8 neighbouring ones and the 8 that lie 64 behind them each: the largest magnitude by three shuffles, two divisions for the
+// scale, three or five multiplications and additions for each value.  ODD: columns, row lengths or pointers that are not multiples of 8 values.  Bound by
+// memory, nearly by the number of instructions (8191 x 4096 gated bf16 values behind SILU: 16 lanes a block, two corrections always and comparisons against infinity took 46 us).
 template <class Y, bool GATE, bool ODD>
 __global__ void __launch_bounds__(256) quantise_kernel(const QuantiseParams p) {
-  const long long i = (long long)blockIdx.x * 16 + (threadIdx.x >> 4), r = i / p.blocks;
+  const uint32_t i = blockIdx.x * 32 + (threadIdx.x >> 3);
+  const long long r = p.blocks(i);
   grid_dep_wait();
   grid_dep_launch();
-  // (whole half-warps; the shuffles name them alone)
+  // (whole groups of 8 lanes; the shuffles name them alone)
   if (r >= p.out_rows) return;
-  const int b = (int)(i - r * p.blocks), lane = threadIdx.x & 15, c = b * 128 + lane * 8;
+  const int b = (int)(i - (uint32_t)r * p.blocks.d), lane = threadIdx.x & 7, c0 = b * 128 + lane * 8;
   const long long from = p.rows ? p.rows[r] : r;
   const bool there = from >= 0 && from < p.in_rows;
   using E = typename Element<Y>::type;
-  float v[8];
+  float v[16];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] = 0.f;
+  for (int q = 0; q < 16; ++q) v[q] = 0.f;
   if (ODD) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
-      if (there && c + q < p.columns) {
-        const float u = value(p.up, p.type, from * p.ld_up + c + q);
-        v[q] = GATE ? activated(p.fn, value(p.gate, p.type, from * p.ld_gate + c + q)) * u : activated(p.fn, u);
-      }
-  } else if (there && c < p.columns) {
-    Eight<Y> u, g;
-    u.load(static_cast<const E*>(p.up) + from * p.ld_up + c);
-    if (GATE) g.load(static_cast<const E*>(p.gate) + from * p.ld_gate + c);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float2 a = u.pair(q);
-      if (GATE) {
-        const float2 h = g.pair(q);
-        v[2 * q] = activated(p.fn, h.x) * a.x;
-        v[2 * q + 1] = activated(p.fn, h.y) * a.y;
-      } else {
-        v[2 * q] = activated(p.fn, a.x);
-        v[2 * q + 1] = activated(p.fn, a.y);
+    for (int q = 0; q < 16; ++q) {
+      const int c = c0 + (q >> 3) * 64 + (q & 7);
+      if (there && c < p.columns) {
+        const float u = value(p.up, p.type, from * p.ld_up + c);
+        v[q] = GATE ? activated(p.fn, value(p.gate, p.type, from * p.ld_gate + c)) * u : activated(p.fn, u);
       }
     }
+  } else {
+    Eight<Y> u[2], g[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = c0 + 64 * h;
+      const bool have = there && c < p.columns;
+      if (have) u[h].load(static_cast<const E*>(p.up) + from * p.ld_up + c);
+      else u[h].zero();
+      if (GATE) {
+        if (have) g[h].load(static_cast<const E*>(p.gate) + from * p.ld_gate + c);
+        else g[h].zero();
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float2 a = u[q >> 2].pair(q & 3);
+      uint64_t w = pair_of(a.x, a.y);
+      if (GATE) {
+        const float2 h = g[q >> 2].pair(q & 3);
+        w = mul2(activated2(p.fn, pair_of(h.x, h.y)), w);
+      } else {
+        w = activated2(p.fn, w);
+      }
+      const float2 f = floats_of(w);
+      v[2 * q] = f.x;
+      v[2 * q + 1] = f.y;
+    }
   }
+  const uint32_t mine = 0xffu << (threadIdx.x & 24);
   float most = 0.f;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const float m = fabsf(v[q]);
-    most = m <= 3.402823466e38f ? fmaxf(most, m) : most;   // (infinities and NaN do not count)
+  for (int q = 0; q < 16; ++q) most = fmaxf(most, fabsf(v[q]));   // (NaN is nobody's larger)
+#pragma unroll
+  for (int d = 4; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(mine, most, d));
+  if (most == CUDART_INF_F) {   // (the same in the 8 lanes)
+    most = 0.f;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) most = fabsf(v[q]) < CUDART_INF_F ? fmaxf(most, fabsf(v[q])) : most;
+#pragma unroll
+    for (int d = 4; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(mine, most, d));
   }
-  const uint32_t mine = 0xffffu << (threadIdx.x & 16);
+  const float scale = fmaxf(most / kLargest, kLeastScale), inverse = 1.f / scale;
+  constexpr bool ONCE = !std::is_same<Y, float>::value;
+  const uint64_t minus2 = pair_of(-scale, -scale), inverse2 = pair_of(inverse, inverse);
 #pragma unroll
-  for (int d = 8; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(mine, most, d));
-  const float scale = fmaxf(most / kLargest, kLeastScale);
-  uint32_t out[2] = {};
+  for (int h = 0; h < 2; ++h) {
+    uint32_t out[2] = {};
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const bool finite = fabsf(v[q]) <= 3.402823466e38f;
-    const uint32_t bits = finite ? (uint32_t)__nv_cvt_float_to_fp8(v[q] / scale, __NV_SATFINITE, __NV_E4M3) : 0x7fu;
-    out[q >> 2] |= bits << (8 * (q & 3));
-  }
-  uint8_t* const to = p.values + r * p.ld_values + c;
-  if (ODD) {
+    for (int q = 0; q < 8; q += 2)
+      out[q >> 2] |= (uint32_t)__nv_cvt_float2_to_fp8x2(floats_of(quotients<ONCE>(pair_of(v[8 * h + q], v[8 * h + q + 1]), minus2, inverse2)), __NV_SATFINITE, __NV_E4M3) << (8 * (q & 3));
+    const int c = c0 + 64 * h;
+    uint8_t* const to = p.values + r * p.ld_values + c;
+    if (ODD) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q)
-      if (c + q < p.columns) to[q] = (uint8_t)(out[q >> 2] >> (8 * (q & 3)));
-  } else if (c < p.columns) {
-    *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
+      for (int q = 0; q < 8; ++q)
+        if (c + q < p.columns) to[q] = (uint8_t)(out[q >> 2] >> (8 * (q & 3)));
+    } else if (c < p.columns) {
+      *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
+    }
   }
   if (lane == 0) p.scales[r * p.ld_scales + b] = scale;
 }
@@ -154,11 +205,11 @@ cudaError_t activate_type(const ActivateParams& p, unsigned blocks, cudaStream_t
 }  // namespace
 
 cudaError_t activate_forward(const ActivateCall& c, int* launched) {
-  ActivateParams p{c.gate, c.up, c.out, c.ld_gate, c.ld_up, c.ld_out, c.rows, c.columns, c.columns / 8, c.fn, c.type, c.out_type};
   const bool eights = c.columns % 8 == 0 && c.ld_up % 8 == 0 && (!c.gate || c.ld_gate % 8 == 0) && c.ld_out % 8 == 0 &&
                       (((uintptr_t)c.up | (uintptr_t)c.gate | (uintptr_t)c.out) & 15) == 0;
-  const long long blocks = ((long long)c.rows * (eights ? p.groups : c.columns) + 255) / 256;
-  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  const ActivateParams p{c.gate, c.up, c.out, c.ld_gate, c.ld_up, c.ld_out, c.rows, c.columns, c.fn, c.type, c.out_type, Divisor(eights ? c.columns / 8 : (c.columns + 255) / 256)};
+  const long long units = (long long)c.rows * p.each.d, blocks = eights ? (units + 255) / 256 : units;
+  if (units >= (1ll << 31)) return cudaErrorInvalidValue;
   *launched += 1;
   if (!eights) return launch_dependent(activate_odd_kernel, (unsigned)blocks, 256, 0, c.stream, p);
   if (c.type == SNN_OUT_F32) return activate_type<float>(p, (unsigned)blocks, c.stream);
@@ -166,11 +217,11 @@ cudaError_t activate_forward(const ActivateCall& c, int* launched) {
 }
 
 cudaError_t quantise_forward(const QuantiseCall& c, int* launched) {
-  const QuantiseParams p{c.gate, c.up, c.rows, c.values, c.scales, c.ld_gate, c.ld_up, c.ld_values, c.ld_scales, c.in_rows, c.out_rows, c.columns, (c.columns + 127) / 128, c.fn, c.type};
+  const QuantiseParams p{c.gate, c.up, c.rows, c.values, c.scales, c.ld_gate, c.ld_up, c.ld_values, c.ld_scales, c.in_rows, c.out_rows, c.columns, c.fn, c.type, Divisor((c.columns + 127) / 128)};
   const bool odd = c.columns % 8 || c.ld_up % 8 || (c.gate && c.ld_gate % 8) || c.ld_values % 8 ||
                    (((uintptr_t)c.up | (uintptr_t)c.gate) & 15) || ((uintptr_t)c.values & 7);
-  const long long blocks = ((long long)c.out_rows * p.blocks + 15) / 16;
-  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  const long long units = (long long)c.out_rows * p.blocks.d, blocks = (units + 31) / 32;
+  if (units >= (1ll << 31)) return cudaErrorInvalidValue;
   *launched += 1;
   if (c.type == SNN_OUT_F32) return quantise_type<float>(p, odd, (unsigned)blocks, c.stream);
   return c.type == SNN_OUT_F16 ? quantise_type<F16>(p, odd, (unsigned)blocks, c.stream) : quantise_type<BF16>(p, odd, (unsigned)blocks, c.stream);

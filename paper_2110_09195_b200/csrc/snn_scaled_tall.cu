@@ -17,18 +17,17 @@ namespace {
 //   CG = 1, N = 128 or 64: fewer rows, more tiles, for problems that would leave SMs without any.
 constexpr int ST_ROWS = 128;          // of a CTA's tile
 constexpr int ST_A_BYTES = ST_ROWS * 128;
-constexpr int ST_BOX = 32;            // rows of one TMA box
 constexpr int ST_MAX_STAGES = 10;
 constexpr int ST_OUT_WARPS = 8;
 constexpr int ST_STAGING = 4096;      // of a warp: 32 rows of 128 bytes
-// warps: 0 copies, 1 MMA, 2 tensor memory, 4-11 sums and outputs
+// warps: 0 copies of the rows, 1 MMA, 2 tensor memory, 3 copies of the weights, 4-11 sums and outputs
 
 struct TallScaledParams {
   const float *w_scales, *x_scales;
   const int32_t* offsets;
   void* out;
   long long ld_scales, ld_out;
-  int rows, E, C, K, n_kt, n_kb, out_type, n_ct, stages, fours, eights;   // fours, eights: scales and outputs by 16 bytes
+  int rows, E, C, K, n_kt, n_kb, out_type, n_ct, stages, box, fours, eights;   // rows of a box of x; scales and outputs by 16 bytes
   int* status;
 };
 struct TallScaledBars {
@@ -37,34 +36,36 @@ struct TallScaledBars {
 };
 template <int CG, int N>
 struct TallScaledShape {
-  static constexpr int kBRows = N / CG;                            // of the weights, in each CTA
-  static constexpr int kStage = ST_A_BYTES + kBRows * 128;
-  static constexpr int kBuffers = N == 256 ? 2 : 4;
-  static constexpr int kColumns = N * kBuffers;                    // of tensor memory: 512, 512, 256
+  static constexpr int kParts = CG;                                // instructions of N / CG channels for a block, each with buffers of its own
+  static constexpr int kN = N / kParts, kBRows = kN / CG;          // channels of an instruction, and rows of the weights that each CTA has of them
+  static constexpr int kStage = ST_A_BYTES + kParts * kBRows * 128;
+  static constexpr int kBuffers = 4, kColumns = kN * kBuffers;     // of tensor memory: 512, 512, 256
+  static constexpr int kWarps = ST_OUT_WARPS / kParts;             // that read a buffer, in each CTA
   static constexpr int kFixed = 1024 + ST_OUT_WARPS * ST_STAGING + (int)sizeof(TallScaledBars);
 };
 
 // Issued by the lanes for which `on` is not 0: D = A * B^T over 128 input channels in four steps of 32, then the commits: the stage is free, the buffer is full.
+// (the stage only if `last`)
 template <int CG>
-__device__ __forceinline__ void block_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on);
+__device__ __forceinline__ void block_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t last);
 template <>
-__device__ __forceinline__ void block_e4m3<2>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on) {
+__device__ __forceinline__ void block_e4m3<2>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t last) {
   asm volatile(
-      "{\n\t.reg .pred q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
-      "setp.ne.b32 q, %6, 0;\n\t"
+      "{\n\t.reg .pred q, z;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "setp.ne.b32 q, %6, 0;\n\tsetp.ne.and.b32 z, %8, 0, q;\n\t"
       "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
       "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, 0;\n\t"
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a1, b1, %3, 1;\n\t"
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a2, b2, %3, 1;\n\t"
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a3, b3, %3, 1;\n\t"
-      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], %7;\n\t"
+      "@z tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], %7;\n\t"
       "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], %7;\n\t}" ::"r"(d),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on), "h"((uint16_t)3)
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on), "h"((uint16_t)3), "r"(last)
       : "memory");
 }
 template <>
-__device__ __forceinline__ void block_e4m3<1>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on) {
+__device__ __forceinline__ void block_e4m3<1>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t) {
   asm volatile(
       "{\n\t.reg .pred q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
       "setp.ne.b32 q, %6, 0;\n\t"
@@ -96,10 +97,55 @@ __device__ __forceinline__ uint4 lds16_at(uint32_t addr) {
   asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ float ld_plain(const float* p) {
-  float v;
-  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
-  return v;
+// Four neighbouring numbers, of which `n` are there, by one load if `whole`.  (One statement: where the two ways meet in code, the registers are moved, and
+// the warp waits for the load.)
+__device__ __forceinline__ void ld_four(const float* p, int n, int whole, float (&v)[4]) {
+  asm volatile(
+      "{\n\t.reg .pred a, b, c, d, e;\n\t"
+      "setp.ne.s32 a, %6, 0;\n\tsetp.eq.s32 b, %6, 0;\n\t"
+      "setp.gt.and.s32 c, %5, 1, b;\n\tsetp.gt.and.s32 d, %5, 2, b;\n\tsetp.gt.and.s32 e, %5, 3, b;\n\t"
+      "@a ld.global.v4.f32 {%0, %1, %2, %3}, [%4];\n\t"
+      "@b ld.global.f32 %0, [%4];\n\t"
+      "@c ld.global.f32 %1, [%4 + 4];\n\t"
+      "@d ld.global.f32 %2, [%4 + 8];\n\t"
+      "@e ld.global.f32 %3, [%4 + 12];\n\t}"
+      : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3])
+      : "l"(p), "r"(n), "r"(whole));
+}
+
+// W columns of the warp's 32 lanes; load and wait are one statement.
+template <int W>
+__device__ __forceinline__ void tmem_ld_some(uint32_t taddr, uint32_t (&v)[W]);
+template <>
+__device__ __forceinline__ void tmem_ld_some<32>(uint32_t taddr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr)
+      : "memory");
+}
+template <>
+__device__ __forceinline__ void tmem_ld_some<64>(uint32_t taddr, uint32_t (&v)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\ttcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+        "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+        "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]),
+        "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]),
+        "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]),
+        "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]),
+        "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+      : "r"(taddr)
+      : "memory");
+}
+template <int W>
+__device__ __forceinline__ void add_some(uint64_t* acc, const uint32_t (&v)[W], uint64_t f) {
+#pragma unroll
+  for (int i = 0; i < W / 2; ++i) asm("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tfma.rn.f32x2 %0, t, %3, %0;\n\t}" : "+l"(acc[i]) : "r"(v[2 * i]), "r"(v[2 * i + 1]), "l"(f));
 }
 
 struct ScaledTile {
@@ -126,7 +172,7 @@ __device__ __forceinline__ bool scaled_tile(const ScaledRanges& R, int E, int n_
 template <int CG, int N>
 __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, const CUtensorMap& x_map, const CUtensorMap& w_map) {
   using S = TallScaledShape<CG, N>;
-  constexpr int NB = S::kBuffers;
+  constexpr int NB = S::kBuffers, PARTS = S::kParts;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* const staging = smem + p.stages * S::kStage;
@@ -136,7 +182,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
   R.n = R.lo + p.E;
   R.end = R.n + p.E;
   const int warp = uni(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const uint32_t base = smem_u32(smem);
+  const uint32_t base = (uint32_t)uni((int)smem_u32(smem));
   const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, first_tile = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
   if (warp == 0) {
     grid_dep_wait();
@@ -160,12 +206,12 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
     for (int e = e0; e < e1; ++e) R.end[e] = end += (R.n[e] + CG * ST_ROWS - 1) / (CG * ST_ROWS);
   } else if (warp == 1 && lane == 0) {
     for (int i = 0; i < p.stages; ++i) {
-      mbar_init(smem_u32(&bars->full[i]), 1);
+      mbar_init(smem_u32(&bars->full[i]), 2);
       mbar_init(smem_u32(&bars->empty[i]), 1);
     }
     for (int i = 0; i < NB; ++i) {
       mbar_init(smem_u32(&bars->d_full[i]), 1);
-      mbar_init(smem_u32(&bars->d_empty[i]), CG * ST_OUT_WARPS);
+      mbar_init(smem_u32(&bars->d_empty[i]), CG * S::kWarps);
     }
     mbar_init(smem_u32(&bars->drain), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -194,24 +240,31 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
 
   if (warp < 4) {
     if (N == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0) {
+    if (warp == 0 || warp == 3) {
       // ------------------------------------------------------------ copies: a stage is 128 input channels of the rows and of the weights
       int s = 0, filled = 0;
       uint32_t phase = 0;
+      const bool leader = elect_one();
       for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
-        auto boxes = [&](int r) { return (min(max(t.n - r * ST_ROWS, 0), ST_ROWS) + ST_BOX - 1) / ST_BOX; };
+        auto boxes = [&](int r) { return (min(max(t.n - r * ST_ROWS, 0), ST_ROWS) + p.box - 1) / p.box; };
         const int mine = boxes(rank);
-        const uint32_t bytes = (uint32_t)(boxes(0) + (CG == 2 ? boxes(1) : 0)) * (ST_BOX * 128) + CG * S::kBRows * 128;   // of both CTAs
-        const int kt = N == 256 ? min(2 * t.ct + rank, p.n_kt - 1) : N == 128 ? t.ct : t.ct >> 1;
-        const int w_row0 = (t.e * p.n_kt + kt) * nk, w_half = N == 64 ? (t.ct & 1) * 64 : 0;
+        const uint32_t bytes = (uint32_t)(warp ? CG * PARTS * S::kBRows : (boxes(0) + (CG == 2 ? boxes(1) : 0)) * p.box) * 128u;   // of both CTAs
+        // the weights: 64 rows of each of two tiles, one, or half of one
+        const int kt = N == 256 ? 2 * t.ct : N == 128 ? t.ct : t.ct >> 1, w_half = CG == 2 ? rank * 64 : N == 64 ? (t.ct & 1) * 64 : 0;
         for (int kb = 0; kb < nk; ++kb) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->empty[s]), phase ^ 1u));
           if (!ok) break;
           const uint32_t full = smem_u32(&bars->full[s]), dst = base + s * S::kStage;
-          if (rank == 0 && lane == 0) mbar_expect_tx(full, bytes);
-          __syncwarp();
-          if (lane < mine) copy_box<CG>(dst + lane * ST_BOX * 128, &x_map, kb * 128, t.r0 + rank * ST_ROWS + lane * ST_BOX, full);
-          else if (lane == 4) copy_box<CG>(dst + ST_A_BYTES, &w_map, 0, (w_row0 + kb) * 128 + w_half, full);
+          if (leader) {   // (one lane: copies of several lanes are issued one after the other, 100 cycles each)
+            if (rank == 0) mbar_expect_tx(full, bytes);
+            if (warp == 0) {
+              for (int i = 0; i < mine; ++i) copy_box<CG>(dst + i * p.box * 128, &x_map, kb * 128, t.r0 + rank * ST_ROWS + i * p.box, full);
+            } else {
+#pragma unroll
+              for (int i = 0; i < PARTS; ++i)
+                copy_box<CG>(dst + ST_A_BYTES + i * S::kBRows * 128, &w_map, 0, ((t.e * p.n_kt + min(kt + i, p.n_kt - 1)) * nk + kb) * 128 + w_half, full);
+            }
+          }
           __syncwarp();
           filled = min(filled + 1, p.stages);
           if (++s == p.stages) {
@@ -234,22 +287,28 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
       int s = 0, d = 0;
       uint32_t phase = 0, d_phase = 0;
       const uint32_t leader = elect_one(), tmem_u = (uint32_t)uni((int)tmem);
-      const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(CG * ST_ROWS >> 4) << 24);   // fp32 sums of e4m3 values
+      const uint32_t idesc = (1u << 4) | ((uint32_t)(S::kN >> 3) << 17) | ((uint32_t)(CG * ST_ROWS >> 4) << 24);   // fp32 sums of e4m3 values
       for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
         for (int kb = 0; kb < nk; ++kb) {
-          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_empty[d]), d_phase ^ 1u) && mbar_wait(smem_u32(&bars->full[s]), phase));
-          if (!ok) break;
-          tc_fence_after();
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase));
           const uint32_t a = base + s * S::kStage;
-          block_e4m3<CG>(tmem_u + d * N, rows_desc(a), rows_desc(a + ST_A_BYTES), idesc, smem_u32(&bars->empty[s]), smem_u32(&bars->d_full[d]), leader);
-          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < PARTS; ++i) {
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(&bars->d_empty[d]), d_phase ^ 1u));
+            if (!ok) break;
+            tc_fence_after();
+            block_e4m3<CG>(tmem_u + d * S::kN, rows_desc(a), rows_desc(a + ST_A_BYTES + i * S::kBRows * 128), idesc, smem_u32(&bars->empty[s]), smem_u32(&bars->d_full[d]), leader,
+                           i + 1 == PARTS);
+            __syncwarp();
+            if (++d == NB) {
+              d = 0;
+              d_phase ^= 1u;
+            }
+          }
+          if (!ok) break;
           if (++s == p.stages) {
             s = 0;
             phase ^= 1u;
-          }
-          if (++d == NB) {
-            d = 0;
-            d_phase ^= 1u;
           }
         }
       }
@@ -263,36 +322,25 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
     if (N == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     constexpr int A = N / 2;
     const int quarter = warp & 3, half = (warp - 4) >> 2, row = quarter * 32 + lane;
-    const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + half * A, stage = smem_u32(staging) + (warp - 4) * ST_STAGING;
-    int d = 0;
+    const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + (PARTS == 1 ? half * A : 0), stage = smem_u32(staging) + (warp - 4) * ST_STAGING;
+    int d = PARTS == 2 ? half : 0;
     uint32_t d_phase = 0;
     for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
       const int n = t.n - rank * ST_ROWS, co0 = t.ct * N + half * A;   // rows of this CTA's (0 or less: none), first channel
       const float* const xs = p.x_scales + (size_t)(t.r0 + min(rank * ST_ROWS + row, t.n - 1)) * (size_t)p.ld_scales;
       const float* const ws = p.w_scales + ((size_t)t.e * p.n_kt + min(co0 >> 7, p.n_kt - 1)) * nk;
-      float next[4];
-      auto load = [&](int kb) {   // four blocks' factors
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p.fours) {
-          const uint4 u = ld16(xs + kb);
-          v = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
-        } else {
-          v.x = ld_plain(xs + kb);
-          if (kb + 1 < nk) v.y = ld_plain(xs + kb + 1);
-          if (kb + 2 < nk) v.z = ld_plain(xs + kb + 2);
-          if (kb + 3 < nk) v.w = ld_plain(xs + kb + 3);
-        }
-        next[0] = v.x * ld_plain(ws + kb);
-        next[1] = kb + 1 < nk ? v.y * ld_plain(ws + kb + 1) : 0.f;
-        next[2] = kb + 2 < nk ? v.z * ld_plain(ws + kb + 2) : 0.f;
-        next[3] = kb + 3 < nk ? v.w * ld_plain(ws + kb + 3) : 0.f;
+      // Four blocks' scales on their way while four blocks are added up.  (They are multiplied where they are used: at the loads the warp would wait for them.)
+      float next_x[4] = {}, next_w[4] = {};
+      auto load = [&](int kb) {
+        ld_four(xs + kb, nk - kb, p.fours, next_x);
+        ld_four(ws + kb, nk - kb, p.fours, next_w);
       };
       load(0);
-      float acc[A];
+      uint64_t acc[A / 2];
 #pragma unroll
-      for (int i = 0; i < A; ++i) acc[i] = 0.f;
+      for (int i = 0; i < A / 2; ++i) acc[i] = 0;
       for (int kb = 0; ok && kb < nk; kb += 4) {
-        const float f[4] = {next[0], next[1], next[2], next[3]};
+        const float f[4] = {next_x[0] * next_w[0], next_x[1] * next_w[1], next_x[2] * next_w[2], next_x[3] * next_w[3]};
         if (kb + 4 < nk) load(kb + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -300,11 +348,13 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), d_phase));
           if (!ok) break;
           tc_fence_after();
+          const uint64_t factor = pair_of(f[i], f[i]);
+          constexpr int W = A < 64 ? A : 64;
 #pragma unroll
-          for (int c = 0; c < A; c += 32) {
-            uint32_t v[32];
-            tmem_ld32(src + d * N + c, v);
-            if (c + 32 == A) {   // (all of the buffer has been read)
+          for (int c = 0; c < A; c += W) {
+            uint32_t v[W];
+            tmem_ld_some<W>(src + d * S::kN + c, v);
+            if (c + W == A) {   // (all of the buffer has been read)
               tc_fence_before();
               __syncwarp();
               if (lane == 0) {
@@ -312,11 +362,11 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
                 else mbar_arrive(smem_u32(&bars->d_empty[d]));
               }
             }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) acc[c + j] = fmaf(f[i], __uint_as_float(v[j]), acc[c + j]);
+            add_some<W>(acc + c / 2, v, factor);
           }
-          if (++d == NB) {
-            d = 0;
+          d += PARTS;
+          if (d >= NB) {
+            d -= NB;
             d_phase ^= 1u;
           }
         }
@@ -355,15 +405,17 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
         if (p.out_type == SNN_OUT_F32) {
 #pragma unroll
           for (int c = 0; c < A; c += 32)
-            pass([&](int q) { return make_uint4(__float_as_uint(acc[c + 4 * q]), __float_as_uint(acc[c + 4 * q + 1]), __float_as_uint(acc[c + 4 * q + 2]), __float_as_uint(acc[c + 4 * q + 3])); },
-                 co0 + c, 4);
+            pass([&](int q) {
+              const float2 a = floats_of(acc[c / 2 + 2 * q]), b = floats_of(acc[c / 2 + 2 * q + 1]);
+              return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+            }, co0 + c, 4);
         } else if (A >= 64) {
 #pragma unroll
           for (int c = 0; c < A; c += 64)
             pass([&](int q) {
               uint32_t w[4];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, make_float2(acc[c + 8 * q + 2 * j], acc[c + 8 * q + 2 * j + 1]));
+              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, floats_of(acc[c / 2 + 4 * q + j]));
               return make_uint4(w[0], w[1], w[2], w[3]);
             }, co0 + c, 8);
         } else {   // (32 channels: half of a pass, the other half is not there)
@@ -371,7 +423,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
             uint32_t w[4] = {};
             if (q < 4)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, make_float2(acc[(8 * q + 2 * j) % A], acc[(8 * q + 2 * j + 1) % A]));
+              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, floats_of(acc[(4 * q + j) % (A / 2)]));
             return make_uint4(w[0], w[1], w[2], w[3]);
           }, (lane & 7) < 4 ? co0 : p.K, 8);
         }
@@ -415,12 +467,15 @@ cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p
   cudaError_t e = allow_max_smem(kernel, done);
   if (e != cudaSuccess) return e;
   CUtensorMap x_map, w_map;
-  if (!rows_map(&x_map, c.act, p.C, c.rows, c.ld_act, ST_BOX, true) ||
+  // (few rows: no more than there are)
+  const long long each = c.offsets ? ((long long)c.rows + min(p.E, c.rows) - 1) / min(p.E, c.rows) : c.rows;
+  const int box = each <= 32 ? 32 : each <= 64 ? 64 : ST_ROWS;
+  if (!rows_map(&x_map, c.act, p.C, c.rows, c.ld_act, box, true) ||
       !rows_map(&w_map, p.tiles, 128, (long long)p.E * p.n_kt * p.n_kb * 128, 128, S::kBRows, false))
     return cudaErrorInvalidValue;
   const int size = c.out_type == SNN_OUT_F32 ? 4 : 2, fixed = S::kFixed + p.E * 12;
   const TallScaledParams q{p.scales, c.scales, c.offsets, c.out, c.ld_scales, c.ld_out, c.rows, p.E, p.C, p.K, p.n_kt, p.n_kb, c.out_type, (p.K + N - 1) / N,
-                           min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::kStage), p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
+                           min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::kStage), box, p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
                            c.ld_out * size % 16 == 0 && ((uintptr_t)c.out & 15) == 0, p.status_dev};
   const long long tiles = ((long long)c.rows / (CG * ST_ROWS) + (c.offsets ? min(p.E, c.rows) : 1)) * q.n_ct;
   *launched += 1;

@@ -9,9 +9,11 @@ long, calls are asynchronous on `stream` (default: torch's current stream), and 
 from __future__ import annotations
 
 import ctypes
+import struct
 from collections import namedtuple
 
-from .binding import SnnError, _check, _raw_stream, load_library
+from . import binding
+from .binding import SnnError, _check, _load_fast, _raw_stream, load_library
 from .projections import OUT_BF16, SnnConvExperts, _act_type, _dtype, _floats, _here, _ints, _matrix, _on, _output, _types
 
 FN_NONE, FN_RELU, FN_SILU, FN_GELU = 0, 1, 2, 3
@@ -44,6 +46,12 @@ def _pointer(t):
 def activate(up, gate=None, fn=FN_SILU, out=None, out_type=None, stream=None):
     """snn_conv_experts_activate: fn(gate) * up, or fn(up) without a gate, for matrices float32, float16 or bfloat16.
     Outputs are of the type of `out`, else out_type, else up's; `out` may be up or gate itself."""
+    if out is not None and out_type is None and stream is None:
+        st = (binding._fast or _load_fast()).activate(up, gate, fn, out)
+        if st == 0:
+            return out
+        if st > 0:
+            _check(st)
     device, kind, rows, columns, ld_up, ld_gate = _between(up, gate)
     with _on(stream):
         out, _, ld_out, ot = _output(out, out_type, up.dtype, rows, columns, device)
@@ -56,7 +64,7 @@ class SnnConvMoe:
     """A whole mixture of experts for at most MOE_TOKENS_MAX tokens (wraps snn_conv_moe_t).  `up`, `down` and `gate` are
     SnnConvExperts, kept (and kept alive) by reference; do not destroy them before the mixture."""
 
-    _h = None
+    _h = _desc = None
 
     def __init__(self, up, down, gate=None, fn=FN_SILU):
         lib = load_library()
@@ -67,6 +75,7 @@ class SnnConvMoe:
         _check(lib.snn_conv_moe_create(None if gate is None else gate._h, up._h, down._h, int(fn), ctypes.byref(h)))
         self._h, self._experts = h, (up, down, gate)
         self.device, self.count, self.c_in, self.hidden, self.c_out = up.device, up.count, up.c_in, up.c_out, down.c_out
+        self._desc = struct.pack("=Q4i", h.value, self.device, self.count, self.c_in, self.c_out)
 
     def forward(self, x, logits, top_k, normalise=True, out=None, out_type=None, stream=None):
         """snn_conv_moe_forward: out[t] = sum_j w_j down_e(fn(gate_e(x[t])) * up_e(x[t])) over the top_k experts e of
@@ -74,6 +83,12 @@ class SnnConvMoe:
         import torch
         if self._h is None or any(e is not None and e._h is None for e in self._experts):
             raise SnnError(1, "the mixture or its experts were destroyed")
+        if out is not None and out_type is None and stream is None:
+            st = (binding._fast or _load_fast()).moe_forward(self._desc, x, logits, top_k, normalise, out)
+            if st == 0:
+                return out
+            if st > 0:
+                _check(st)
         act_type = _act_type(x)
         ld_x = _matrix(x, "x", self.device, self.c_in, aligned=True)
         types = _types()[1]
@@ -92,6 +107,7 @@ class SnnConvMoe:
 
     def destroy(self):
         if getattr(self, "_h", None) is not None:
+            self._desc = None
             load_library().snn_conv_moe_destroy(self._h)
             self._h = self._experts = None
 
@@ -142,6 +158,13 @@ def quantise(up, gate=None, fn=FN_NONE, rows=None, out=None, stream=None):
     """snn_conv_scaled_quantise: rows of `up` (float32, float16 or bfloat16) as e4m3 values with a scale for each 128
     columns, behind an activation where fn says so; output row i is of row rows[i] (int32) where there is an index.
     Returns `out`, or a new Quantised(values, scales)."""
+    if out is not None and stream is None:
+        values, scales = out
+        st = (binding._fast or _load_fast()).quantise(up, gate, fn, rows, values, scales)
+        if st == 0:
+            return out
+        if st > 0:
+            _check(st)
     device, kind, n, columns, ld_up, ld_gate = _between(up, gate)
     row_ptr, m = None, n
     if rows is not None:
@@ -165,7 +188,7 @@ class SnnConvScaled:
     (c_out, c_in) or (projections, c_out, c_in) and `scales` float32 (..., ceil(c_out / 128), ceil(c_in / 128)) are
     contiguous CUDA tensors; they are copied."""
 
-    _h = None
+    _h = _desc = None
 
     def __init__(self, weights, scales, stream=None):
         import torch
@@ -182,12 +205,19 @@ class SnnConvScaled:
         h = ctypes.c_void_p()
         _check(lib.snn_conv_scaled_create(weights.data_ptr(), sp, e, c, k, device, _raw_stream(device, stream), ctypes.byref(h)))
         self._h, self.device, self.count, self.c_in, self.c_out = h, device, e, c, k
+        self._desc = struct.pack("=Q4i", h.value, device, e, c, k)
 
     def forward(self, x, scales, offsets=None, out=None, out_type=None, stream=None):
         """snn_conv_scaled_forward: x float8_e4m3fn (rows, c_in) with its scales (rows, ceil(c_in / 128)), as quantise()
         gives them; row i goes through projection e with offsets[e] <= i < offsets[e + 1] (int32, count + 1), without offsets all
         through the first.  Outputs are of the type of `out`, else out_type, else bfloat16; rows outside the
         projections' ranges are left as they are."""
+        if out is not None and out_type is None and stream is None:
+            st = (binding._fast or _load_fast()).scaled_forward(self._desc, x, scales, offsets, out)
+            if st == 0:
+                return out
+            if st > 0:
+                _check(st)
         if self._h is None:
             raise SnnError(1, "the projections were destroyed")
         ld_x = _values(x, "x", self.device, self.c_in, align=16)
@@ -202,6 +232,7 @@ class SnnConvScaled:
 
     def destroy(self):
         if getattr(self, "_h", None) is not None:
+            self._desc = None
             load_library().snn_conv_scaled_destroy(self._h)
             self._h = None
 
