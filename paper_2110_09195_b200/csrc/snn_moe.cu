@@ -10,12 +10,15 @@ namespace {
 
 constexpr int MO_N = 8;    // rows of a piece
 constexpr int MO_M = 32;   // output channels of a warp
+constexpr int MO_FEW = SNN_MOE_FUSED_TOKENS * SNN_ROUTE_TOP_MAX;
 
 // What lies in the workspace.
 struct MoeWork {
-  int32_t *offsets, *rows;   // [E + 1], [slots]
+  int32_t* total;            // pieces that there are
+  int4* pieces;              // [slots]: expert, first row, rows
+  int32_t* rows;             // [slots]: the token of each row
   float* shares;             // [slots]: the weight of each row in its token's sum
-  int32_t *ids, *slots;      // [tokens][top_k], of a router in a launch of its own
+  int32_t *offsets, *ids, *slots;   // of a router in a launch of its own
   float* weights;
   uint16_t* h;               // [parts][slots][hidden], bf16
 };
@@ -27,9 +30,11 @@ long long carve(void* base, int E, int slots, int hidden, MoeWork* w) {
     return p;
   };
   MoeWork m;
-  m.offsets = static_cast<int32_t*>(take((E + 1) * 4ll));
+  m.total = static_cast<int32_t*>(take(4));
+  m.pieces = static_cast<int4*>(take(slots * 16ll));
   m.rows = static_cast<int32_t*>(take(slots * 4ll));
   m.shares = static_cast<float*>(take(slots * 4ll));
+  m.offsets = static_cast<int32_t*>(take((E + 1) * 4ll));
   m.ids = static_cast<int32_t*>(take(slots * 4ll));
   m.slots = static_cast<int32_t*>(take(slots * 4ll));
   m.weights = static_cast<float*>(take(slots * 4ll));
@@ -38,8 +43,8 @@ long long carve(void* base, int E, int slots, int hidden, MoeWork* w) {
   return at;
 }
 
-// Products of 256 input channels: 32 output channels (two tiles) times 8 rows; bits and rows as in the kernel for few rows.
-struct Bits32 {
+// Bits of two tiles of 16 output channels times 256 input channels (layout: snn_products.h).
+struct TileBits {
   uint2 w[2][2];   // [tile][odd blocks of 64]
   __device__ __forceinline__ void load(const uint2* bits, int mt, int n_kb, int kb) {
 #pragma unroll
@@ -47,22 +52,25 @@ struct Bits32 {
 #pragma unroll
       for (int o = 0; o < 2; ++o) w[m][o] = ld8(bits + ((size_t)(mt + m) * n_kb + kb) * 64 + 4 * o);
   }
-  // word j: the 64 input channels from 64 j on
+  // the word of the 64 input channels from 64 j on
   __device__ __forceinline__ uint32_t word(int m, int j) const { return j < 2 ? w[m][j & 1].x : w[m][j & 1].y; }
 };
-template <class T>
-__device__ __forceinline__ void multiply64(float (&acc)[2][4], const Bits32& bits, int j, const uint4 (&b)[2], const Powers& pow) {
+// 64 input channels' products with P parts of 8 rows: the weights, expanded once, are the M operand.
+template <class T, int P>
+__device__ __forceinline__ void multiply64(float (&acc)[2][4], const TileBits& bits, int j, const uint4 (&b)[P][2], const Powers& pow) {
 #pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    const uint4& v = b[s >> 1];
+  for (int s = 0; s < 4; ++s)
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       const uint32_t u = bits.word(m, j);
       const uint32_t a0 = plus_minus<T>(u, 15 - 2 * s, pow), a1 = plus_minus<T>(u, 7 - 2 * s, pow);
       const uint32_t a2 = plus_minus<T>(u, 14 - 2 * s, pow), a3 = plus_minus<T>(u, 6 - 2 * s, pow);
-      mma_16x8<T>(acc[m], a0, a1, a2, a3, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const uint4& v = b[k][s >> 1];
+        mma_16x8<T>(acc[m], a0, a1, a2, a3, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
+      }
     }
-  }
 }
 
 struct UpParams {
@@ -76,140 +84,208 @@ struct UpParams {
   Powers pow;
 };
 
-// First launch.  Up to SNN_MOE_FUSED_TOKENS tokens, every CTA routes for itself (a token a warp): less than a launch in front.  Then as in the kernel for few rows: 8 rows
-// of an expert times 32 output channels a warp, of both the gate and the other projection, input channels split over the warps; the sums meet in shared memory,
-// and what comes of them behind the activation goes out as the sum of `parts` bf16 numbers.
+// A team of warps and nobody else (one warp: the barrier is its own).
+__device__ __forceinline__ void team_sync(int team, int warps) {
+  __syncwarp();
+  if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(warps * 32) : "memory");
+}
+
+// First launch.  Up to SNN_MOE_FUSED_TOKENS tokens, every CTA routes for itself (a token a warp, then each choice finds its place among at most 128): less than a launch in
+// front.  Then 8 rows of an expert times 32 output channels, of both the gate and the other projection, are an item of a team of warps, which share the input channels;
+// a team has a run of items.  A team of one warp holds whole sums and needs nobody; larger ones, where there are few items, meet in shared memory.  What comes out
+// behind the activation goes to memory as the sum of `parts` bf16 numbers.
 template <class T, bool GATE>
 __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
-  constexpr int WIDE = (GATE ? 2 : 1) * MO_M;
+  constexpr int G = GATE ? 2 : 1, M = MO_M, WIDE = G * M;
   __shared__ float red_both[2][8][MO_N][WIDE + 1];
-  __shared__ int s_ids[SNN_MOE_FUSED_TOKENS * SNN_ROUTE_TOP_MAX], s_rows[SNN_MOE_FUSED_TOKENS * SNN_ROUTE_TOP_MAX], s_slots[SNN_MOE_FUSED_TOKENS * SNN_ROUTE_TOP_MAX];
-  __shared__ float s_weights[SNN_MOE_FUSED_TOKENS * SNN_ROUTE_TOP_MAX];
-  __shared__ int part[8];
-  extern __shared__ int s_experts[];   // offsets [E + 1], mask [E][2]
+  __shared__ int s_ids[MO_FEW], s_rows[MO_FEW], s_first[MO_FEW], s_total;
+  __shared__ float s_weights[MO_FEW];
+  __shared__ int4 s_pieces[MO_FEW];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int kw = warp % p.k_warps, mw = warp / p.k_warps, m_warps = 8 / p.k_warps, n_groups = (p.H + MO_M * m_warps - 1) / (MO_M * m_warps);
-  const int *offsets = p.work.offsets, *rows = p.work.rows;
   const int choices = p.tokens * p.route.k;
+  Pieces counted{0, 0, 0};
   if (p.fused) {
-    uint32_t* const mask = reinterpret_cast<uint32_t*>(s_experts + p.E + 1);
-    for (int i = threadIdx.x; i < 2 * p.E; i += 256) mask[i] = 0;
-    RouteParams r = p.route;
-    r.ids = s_ids;
-    r.weights = s_weights;
-    r.rows = s_rows;
-    r.slots = s_slots;
-    __syncthreads();
+    if (threadIdx.x == 0) s_total = 0;
     grid_dep_wait();
     if (warp < p.tokens) {
+      RouteParams r = p.route;
+      r.ids = s_ids;
+      r.weights = s_weights;
       if (p.E <= 64) {
         float v[2];
         load_logits(r, warp, v);
-        choose<2>(r, warp, v, mask, warp);
+        choose<2>(r, warp, v, nullptr, warp);
       } else if (p.E <= 256) {
         float v[8];
         load_logits(r, warp, v);
-        choose<8>(r, warp, v, mask, warp);
+        choose<8>(r, warp, v, nullptr, warp);
       } else {
         float v[32];
         load_logits(r, warp, v);
-        choose<32>(r, warp, v, mask, warp);
+        choose<32>(r, warp, v, nullptr, warp);
       }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < p.E; e += 256) s_experts[e] = __popc(mask[2 * e]);
-    __syncthreads();
-    const int total = scan_counts(s_experts, p.E, part);
-    if (threadIdx.x == 0) s_experts[p.E] = total;
-    place(r, mask, s_experts, 0, p.tokens);
-    __syncthreads();
-    if (blockIdx.x == 0) {
-      for (int e = threadIdx.x; e <= p.E; e += 256) p.work.offsets[e] = s_experts[e];
-      for (int i = threadIdx.x; i < choices; i += 256)
-        if (s_slots[i] >= 0) {
-          p.work.rows[s_slots[i]] = i / p.route.k;
-          p.work.shares[s_slots[i]] = s_weights[i];
+    // An expert's choices are one piece (it has no more than 8); pieces in the order of their first choices, rows in that of the choices.
+    auto place_choice = [&](int i, int id, int piece, int before, int same, int lower) {
+      s_rows[lower + before] = i / p.route.k;
+      if (before == 0) s_pieces[piece] = make_int4(id, lower, same, 0);
+      if (blockIdx.x == 0) {
+        p.work.rows[lower + before] = i / p.route.k;
+        p.work.shares[lower + before] = s_weights[i];
+        if (before == 0) p.work.pieces[piece] = make_int4(id, lower, same, 0);
+      }
+    };
+    if (choices <= 32) {   // a lane has a choice
+      if (warp == 0) {
+        const int id = lane < choices ? s_ids[lane] : -1;
+        const unsigned like = __match_any_sync(0xffffffffu, id), firsts = __ballot_sync(0xffffffffu, id >= 0 && __ffs(like) - 1 == lane);
+        const int first = __ffs(like) - 1, before = __popc(like & ((1u << lane) - 1u)), same = __popc(like);
+        int lower = 0;   // rows of the pieces before
+        for (unsigned left = firsts; left; left &= left - 1) {
+          const int q = __ffs(left) - 1, n = __shfl_sync(0xffffffffu, same, q);
+          if (q < first) lower += n;
         }
+        if (id >= 0) place_choice(lane, id, __popc(firsts & ((1u << first) - 1u)), before, same, lower);
+        if (lane == 0) s_total = __popc(firsts);
+      }
+    } else {
+      for (int i = threadIdx.x; i < choices; i += 256) {
+        int first = 0;
+        while (s_ids[first] != s_ids[i]) ++first;
+        s_first[i] = first;
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < choices; i += 256) {
+        const int first = s_first[i];
+        int before = 0, same = 0, lower = 0, piece = 0;
+        for (int q = 0; q < choices; ++q) {
+          const int f = s_first[q];
+          same += f == first;
+          before += f == first && q < i;
+          lower += f < first && s_ids[f] >= 0;
+          piece += f == q && q < first && s_ids[f] >= 0;
+        }
+        if (s_ids[i] >= 0) {
+          place_choice(i, s_ids[i], piece, before, same, lower);
+          if (before == 0) atomicAdd(&s_total, 1);   // (a count)
+        }
+      }
     }
-    offsets = s_experts;
-    rows = s_rows;
+    __syncthreads();
+    counted.total = s_total;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.work.total = s_total;
   } else {
     grid_dep_wait();
-    if (blockIdx.x == 0)
+    counted = count_pieces(p.work.offsets, p.E, choices, MO_N);
+    if (blockIdx.x == 0) {
       for (int i = threadIdx.x; i < choices; i += 256) {
         const int slot = p.work.slots[i];
         if (slot >= 0) p.work.shares[slot] = p.work.weights[i];
       }
+      for (int i = warp; i < counted.total; i += 8) {
+        int e, r0, n;
+        find_piece(counted, p.work.offsets, p.E, choices, MO_N, i, &e, &r0, &n);
+        if (lane == 0) p.work.pieces[i] = make_int4(e, r0, n, 0);
+      }
+      if (threadIdx.x == 0) *p.work.total = counted.total;
+    }
   }
   grid_dep_launch();
   const Powers pow = in_registers(p.pow);
-  const Pieces pieces = count_pieces(offsets, p.E, choices, MO_N);
-  const long long items = (long long)pieces.total * n_groups;
-  long long item = items * blockIdx.x / gridDim.x;
-  const long long last = items * (blockIdx.x + 1) / gridDim.x;
-  int turn = 0;
-  while (item < last) {
-    const int piece = (int)(item / n_groups), group0 = (int)(item - (long long)piece * n_groups);
-    const int group1 = (int)min((long long)n_groups, group0 + (last - item));
-    item += group1 - group0;
-    int e, r0, n;
-    find_piece(pieces, offsets, p.E, choices, MO_N, piece, &e, &r0, &n);
-    const uint16_t* x = nullptr;
-    if (g < n) x = static_cast<const uint16_t*>(p.act) + (size_t)rows[r0 + g] * (size_t)p.ld_act + 8 * t;
+  const int team = warp / p.k_warps, kw = warp - team * p.k_warps, teams = 8 / p.k_warps, strips = (p.H + M - 1) / M;
+  const long long items = (long long)counted.total * strips, all = (long long)gridDim.x * teams, me = (long long)blockIdx.x * teams + team;
+  const int* const rows = p.fused ? s_rows : p.work.rows;
+  long long item = items * me / all;
+  const long long last = items * (me + 1) / all;
+  const size_t step = (size_t)choices * p.H;
+  int turn = 0, piece = -1, e = 0, r0 = 0, n = 0;
+  const uint16_t* x = nullptr;
+  for (; item < last; ++item) {
+    const int now = (int)(item / strips), strip = (int)(item - (long long)now * strips);
+    if (now != piece) {
+      piece = now;
+      if (p.fused) {
+        const int4 v = s_pieces[piece];
+        e = v.x, r0 = v.y, n = v.z;
+      } else {
+        find_piece(counted, p.work.offsets, p.E, choices, MO_N, piece, &e, &r0, &n);
+      }
+      x = g < n ? static_cast<const uint16_t*>(p.act) + (size_t)rows[r0 + g] * (size_t)p.ld_act + 8 * t : nullptr;
+    }
     const size_t expert = (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
-    for (int group = group0; group < group1; ++group) {
-      float acc[GATE ? 2 : 1][2][4] = {};
-      const int mt = min(2 * (group * m_warps + mw), p.n_mt - 2);
-      for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
-        Bits32 bits[GATE ? 2 : 1];
+    float acc[G][2][4] = {};
+    TileBits bits[G], more[G];
+    uint4 b[4][1][2];   // the rows of four blocks of 64: each is asked for again, 256 channels on, as soon as it has been used
+    auto load_bits = [&](int kb) {
 #pragma unroll
-        for (int i = 0; i < (GATE ? 2 : 1); ++i) bits[i].load(reinterpret_cast<const uint2*>(p.bits[GATE ? i : 1]) + expert, mt, p.n_kb, kb);
-        uint4 b[4][2];
+      for (int i = 0; i < G; ++i) more[i].load(reinterpret_cast<const uint2*>(p.bits[GATE ? i : 1]) + expert, 2 * strip, p.n_kb, kb);
+    };
+    auto load_rows = [&](int kb, int j) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int c = kb * 256 + j * 64 + 32 * h;
-            b[j][h] = x && c + 8 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
-          }
-#pragma unroll
-        for (int i = 0; i < (GATE ? 2 : 1); ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) multiply64<T>(acc[i], bits[i], j, b[j], pow);
+      for (int h = 0; h < 2; ++h) {
+        const int c = kb * 256 + j * 64 + 32 * h;
+        b[j][0][h] = x && c + 8 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
       }
-      float (*const red)[MO_N][WIDE + 1] = red_both[turn];
-      turn ^= 1;
+    };
+    if (kw < p.n_kb) {
+      load_bits(kw);
 #pragma unroll
-      for (int i = 0; i < (GATE ? 2 : 1); ++i)
+      for (int j = 0; j < 4; ++j) load_rows(kw, j);
+    }
+    for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+      for (int i = 0; i < G; ++i) bits[i] = more[i];
+      const bool another = kb + p.k_warps < p.n_kb;
+      if (another) load_bits(kb + p.k_warps);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) red[warp][2 * t + (q & 1)][MO_M * i + 16 * m + g + 8 * (q >> 1)] = acc[i][m][q];
-      __syncthreads();   // (the other half of the buffer is for the next strip)
-      const int width = MO_M * m_warps;
-      for (int i = threadIdx.x; i < width * n; i += 256) {
-        const int m = i & (width - 1), c = i / width, co = group * width + m;
-        if (co >= p.H) continue;
-        float s[2] = {};
-        for (int k = 0; k < p.k_warps; ++k) {
-          const float* const from = red[(m / MO_M) * p.k_warps + k][c] + m % MO_M;
-          s[0] += from[0];
-          if (GATE) s[1] += from[MO_M];
-        }
-        const size_t of = (size_t)e * p.n_mt * 16 + co;
-        const float v = GATE ? activated(p.fn, p.alpha[0][of] * s[0]) * (p.alpha[1][of] * s[1]) : activated(p.fn, p.alpha[1][of] * s[0]);
-        // 8 bits at a time, cut (the rests are exact), the last part rounded; an infinity or NaN in the first
-        uint16_t* const to = p.work.h + (size_t)(r0 + c) * p.H + co;
-        const size_t step = (size_t)choices * p.H;
-        float rest = v;
-        const bool finite = fabsf(v) <= 3.402823466e38f;
-        for (int k = 0; k < p.parts; ++k) {
-          const bool whole = k + 1 == p.parts || !finite;
-          const __nv_bfloat16 b = whole ? __float2bfloat16_rn(rest) : __ushort_as_bfloat16((unsigned short)(__float_as_uint(rest) >> 16));
-          to[k * step] = __bfloat16_as_ushort(b);
-          rest = finite ? rest - __bfloat162float(b) : 0.f;
-        }
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) multiply64<T, 1>(acc[i], bits[i], j, b[j], pow);
+        if (another) load_rows(kb + p.k_warps, j);
       }
+    }
+    // 8 bits at a time, cut (the rests are exact), the last part rounded; an infinity or NaN in the first
+    auto write = [&](int c, int co, float first, float second) {
+      const size_t of = (size_t)e * p.n_mt * 16 + co;
+      const float v = GATE ? activated(p.fn, p.alpha[0][of] * first) * (p.alpha[1][of] * second) : activated(p.fn, p.alpha[1][of] * first);
+      uint16_t* const to = p.work.h + (size_t)(r0 + c) * p.H + co;
+      float rest = v;
+      const bool finite = fabsf(v) <= 3.402823466e38f;
+      for (int k = 0; k < p.parts; ++k) {
+        const bool whole = k + 1 == p.parts || !finite;
+        const __nv_bfloat16 part = whole ? __float2bfloat16_rn(rest) : __ushort_as_bfloat16((unsigned short)(__float_as_uint(rest) >> 16));
+        to[k * step] = __bfloat16_as_ushort(part);
+        rest = finite ? rest - __bfloat162float(part) : 0.f;
+      }
+    };
+    if (p.k_warps == 1) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = 2 * t + (q & 1), co = strip * M + 16 * m + g + 8 * (q >> 1);
+          if (c < n && co < p.H) write(c, co, acc[0][m][q], acc[G - 1][m][q]);
+        }
+      continue;
+    }
+    float (*const red)[MO_N][WIDE + 1] = red_both[turn] + team * p.k_warps;
+    turn ^= 1;
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) red[kw][2 * t + (q & 1)][M * i + 16 * m + g + 8 * (q >> 1)] = acc[i][m][q];
+    team_sync(team, p.k_warps);   // (the other half of the buffer is for the next strip)
+    for (int i = kw * 32 + lane; i < n * M; i += p.k_warps * 32) {
+      const int c = i / M, m = i % M, co = strip * M + m;
+      float s[2] = {};
+      for (int k = 0; k < p.k_warps; ++k) {
+        s[0] += red[k][c][m];
+        if (GATE) s[1] += red[k][c][M + m];
+      }
+      if (co < p.H) write(c, co, s[0], s[1]);
     }
   }
 }
@@ -218,11 +294,12 @@ struct DownParams {
   const uint32_t* bits;
   const float* alpha;
   const uint16_t* h;
-  const int32_t *offsets, *rows;
+  const int32_t *total, *rows;
+  const int4* pieces;
   const float* shares;
   void* out;
   long long ld_out;
-  int tokens, choices, E, C, K, n_mt, n_kb, out_type, cluster;
+  int tokens, choices, C, K, n_mt, n_kb, out_type, cluster;
   Powers pow;
 };
 
@@ -234,25 +311,31 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
   return v;
 }
 __device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ int4 ld_piece(const int4* p) {
+  const uint4 v = ld16(p);
+  return make_int4((int)v.x, (int)v.y, (int)v.z, (int)v.w);
+}
 
 // Second launch.  A cluster has 32 output channels; its warps share out all pieces of all experts, 256 input channels at a time, evenly: a run of them
-// each.  The outputs are linear in what the pieces give, so a warp adds its run's products, times the scale and the row's share, to a table of its own [tokens][32],
+// each.  The outputs are linear in what the pieces give, so a warp adds its run's products, times the scale and the row's share, to a table of its own [tokens][channels],
 // and the tables are added up at the end, warp by warp, CTA by CTA (through distributed shared memory).  No atomics, no partial sums in memory, and
-// no waiting until then.
+// no waiting until then.  Sums of three parts (fp32 outputs) begin anew every 256 channels: the matrix instructions cut what they add.
 constexpr int MO_LD = MO_M + 1;
 template <int PARTS>
 __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
-  extern __shared__ float sums[];   // [8][tokens][MO_LD]
+  constexpr int M = MO_M, LD = MO_LD, RING = PARTS == 3 ? 2 : 4;
+  extern __shared__ float sums[];   // [8][tokens][LD]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int strip = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x % p.cluster, table = p.tokens * MO_LD;
+  const int strip = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x % p.cluster, table = p.tokens * LD;
   float* const mine = sums + warp * table;
   for (int i = lane; i < table; i += 32) mine[i] = 0.f;
   __syncwarp();
   const Powers pow = in_registers(p.pow);
   grid_dep_wait();
   grid_dep_launch();
-  const Pieces pieces = count_pieces(p.offsets, p.E, p.choices, MO_N);
-  const long long units = (long long)pieces.total * p.n_kb;
+  int total;
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(total) : "l"(p.total));
+  const long long units = (long long)total * p.n_kb;
   const int w = rank * 8 + warp, warps = p.cluster * 8;
   long long unit = units * w / warps;
   const long long last = units * (w + 1) / warps;
@@ -261,36 +344,49 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
     const int piece = (int)(unit / p.n_kb), kb0 = (int)(unit - (long long)piece * p.n_kb);
     const int kb1 = (int)min((long long)p.n_kb, kb0 + (last - unit));
     unit += kb1 - kb0;
-    int e, r0, n;
-    find_piece(pieces, p.offsets, p.E, p.choices, MO_N, piece, &e, &r0, &n);
-    const uint2* const bits = reinterpret_cast<const uint2*>(p.bits) + (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
+    const int4 of = ld_piece(p.pieces + piece);
+    const int e = of.x, r0 = of.y, n = of.z;
+    const uint2* const from = reinterpret_cast<const uint2*>(p.bits) + (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
     const uint16_t* const x = p.h + (size_t)(r0 + g) * p.C + 8 * t;
     float acc[2][4] = {};
+    TileBits bits, more;
+    uint4 b[RING][PARTS][2];   // the rows of the next blocks of 64
+    auto load_rows = [&](int kb, int j) {
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = kb * 256 + j * 64 + 32 * h;
+          b[j % RING][k][h] = g < n && c + 8 * t < p.C ? ld16(x + k * step + c) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    more.load(from, 2 * strip, p.n_kb, kb0);
+#pragma unroll
+    for (int j = 0; j < RING; ++j) load_rows(kb0, j);
     for (int kb = kb0; kb < kb1; ++kb) {
-      Bits32 b32;
-      b32.load(bits, 2 * strip, p.n_kb, kb);
+      bits = more;
+      if (kb + 1 < kb1) more.load(from, 2 * strip, p.n_kb, kb + 1);
+      float part[2][4] = {};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        uint4 b[PARTS][2];
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int c = kb * 256 + j * 64 + 32 * h;
-            b[k][h] = g < n && c + 8 * t < p.C ? ld16(x + k * step + c) : make_uint4(0, 0, 0, 0);
-          }
-#pragma unroll
-        for (int k = 0; k < PARTS; ++k) multiply64<BF16>(acc, b32, j, b[k], pow);
+        multiply64<BF16, PARTS>(PARTS == 3 ? part : acc, bits, j, b[j % RING], pow);
+        if (j + RING < 4) load_rows(kb, j + RING);
+        else if (kb + 1 < kb1) load_rows(kb + 1, j + RING - 4);
       }
+      if (PARTS == 3)
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) acc[m][q] += part[m][q];
     }
     // (a piece's rows are of different tokens)
-    const float* const alpha = p.alpha + (size_t)e * p.n_mt * 16 + strip * MO_M;
+    const float* const alpha = p.alpha + (size_t)e * p.n_mt * 16 + strip * M;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const int c = 2 * t + q;
       if (c < n) {
         const float share = p.shares[r0 + c];
-        float* const to = mine + p.rows[r0 + c] * MO_LD;
+        float* const to = mine + p.rows[r0 + c] * LD;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -311,10 +407,10 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   }
   if (p.cluster > 1) cluster_sync();
   else __syncthreads();
-  for (int i = rank * 256 + (int)threadIdx.x; i < p.tokens * MO_M; i += p.cluster * 256) {
-    const int token = i / MO_M, ch = i % MO_M, co = strip * MO_M + ch;
+  for (int i = rank * 256 + (int)threadIdx.x; i < p.tokens * M; i += p.cluster * 256) {
+    const int token = i / M, ch = i % M, co = strip * M + ch;
     float s = 0.f;
-    for (int k = 0; k < p.cluster; ++k) s += p.cluster > 1 ? ld_cluster(smem_u32(sums + token * MO_LD + ch), k) : sums[token * MO_LD + ch];
+    for (int k = 0; k < p.cluster; ++k) s += p.cluster > 1 ? ld_cluster(smem_u32(sums + token * LD + ch), k) : sums[token * LD + ch];
     if (co < p.K) store_out(p.out, p.out_type, token * p.ld_out + co, s);
   }
   if (p.cluster > 1) cluster_sync();   // (nobody ends while its table is read)
@@ -343,8 +439,7 @@ cudaError_t down_launch(const DownParams& p, unsigned strips, cudaStream_t s) {
 
 template <class T>
 cudaError_t up_launch(const UpParams& p, bool gate, unsigned ctas, cudaStream_t s) {
-  const size_t smem = p.fused ? (size_t)(3 * p.E + 1) * 4 : 0;
-  return gate ? launch_dependent(moe_up_kernel<T, true>, ctas, 256, smem, s, p) : launch_dependent(moe_up_kernel<T, false>, ctas, 256, smem, s, p);
+  return gate ? launch_dependent(moe_up_kernel<T, true>, ctas, 256, 0, s, p) : launch_dependent(moe_up_kernel<T, false>, ctas, 256, 0, s, p);
 }
 
 }  // namespace
@@ -379,16 +474,24 @@ cudaError_t moe_forward(const MoeCall& c, int* launched) {
   u.fn = c.fn;
   u.parts = c.out_type == SNN_OUT_F32 ? 3 : 2;
   u.pow = powers();
-  // (as in the kernel for few rows: all warps on one strip, unless there are not so many blocks of input channels, and more strips than CTAs)
-  const long long ctas = 2ll * sm_count(), pieces = ((long long)choices + (long long)min(E, choices) * (MO_N - 1)) / MO_N;
-  auto items = [&](int k) { return pieces * ((up.K + 8 / k * MO_M - 1) / (8 / k * MO_M)); };
-  u.k_warps = 8;
-  while (u.k_warps > up.n_kb && items(u.k_warps) > ctas) u.k_warps /= 2;
-  const unsigned grid = (unsigned)min(ctas, items(u.k_warps));
+  // Pieces that the choices make at most: each expert of theirs has one that is not full.
+  const long long ctas = 2ll * sm_count(), pieces = ((long long)choices + (long long)min(E, choices) * (MO_N - 1)) / MO_N, items = pieces * ((up.K + MO_M - 1) / MO_M);
+  // Warps of a team, by what its longest run takes: blocks of input channels, and for each item about half of one around them.
+  double best = 0;
+  for (int k = 1; k <= 8; k *= 2) {
+    const long long teams = min(ctas * (8 / k), (items + 8 / k - 1) / (8 / k) * (8 / k)), runs = (items + teams - 1) / teams;
+    const double time = runs * ((up.n_kb + k - 1) / k + (k == 1 ? 0.5 : 0.8));
+    if (k == 1 || time < best) {
+      best = time;
+      u.k_warps = k;
+    }
+  }
+  const unsigned grid = (unsigned)min(ctas, (items + 8 / u.k_warps - 1) / (8 / u.k_warps));
   e = c.act_type == SNN_ACT_F16 ? up_launch<F16>(u, c.gate != nullptr, grid, c.stream) : up_launch<BF16>(u, c.gate != nullptr, grid, c.stream);
   *launched += 1;
   if (e != cudaSuccess) return e;
-  DownParams d{down.bits, down.alpha, u.work.h, u.work.offsets, u.work.rows, u.work.shares, c.out, c.ld_out, c.tokens, choices, E, down.C, down.K, down.n_mt, down.n_kb, c.out_type, 1, powers()};
+  DownParams d{down.bits, down.alpha, u.work.h, u.work.total, u.work.rows, u.work.pieces, u.work.shares, c.out, c.ld_out, c.tokens, choices, down.C, down.K, down.n_mt, down.n_kb,
+               c.out_type, 1, powers()};
   const int strips = (down.K + MO_M - 1) / MO_M;
   while (d.cluster < 8 && strips * d.cluster * 2 <= ctas && d.cluster * 8 < pieces * down.n_kb) d.cluster *= 2;
   *launched += 1;

@@ -127,7 +127,7 @@ __device__ __forceinline__ void choose(const RouteParams& p, int t, const float 
   if (lane < p.k) {
     p.ids[(size_t)t * p.k + lane] = id;
     p.weights[(size_t)t * p.k + lane] = id < 0 ? 0.f : w / all;
-    if (id >= 0) atomicOr(mask + 2 * id + (local >> 5), 1u << (local & 31));   // (bits: any order gives the same word)
+    if (mask && id >= 0) atomicOr(mask + 2 * id + (local >> 5), 1u << (local & 31));   // (bits: any order gives the same word)
   }
 }
 

@@ -1,4 +1,5 @@
 // Projections in 8-bit floating point with a scale for each block of 128: layout of the weights, and the kernel for few rows.
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 
@@ -223,6 +224,55 @@ cudaError_t few_launch(const Scaled& p, const ScaledCall& c, int* launched) {
   return launch_dependent(scaled_few_kernel<NT>, (unsigned)min(items, 2ll * sm_count()), 256, FewShape<NT>::kBytes, c.stream, q);
 }
 
+// Which kernel, by the time that each would take (us), where the experts have equal numbers of rows.  Few rows: the weights' bytes, once for each 8, 16 or 32 rows, or what a
+// CTA's turns take; many rows: each block of 128 input channels takes a tile's CTA 0.22 us (a pair's 0.5: 256 rows and channels), a launch 3.5, a join of two or four CTAs 1.6
+// to 2.2; or the weights' bytes.  On 212 calls (dense 256 x 256 to 4096 x 8192 and 8192 x 1024 with 1 to 2048 rows, 8 to 64 experts with 1 to 512 rows each) the
+// kernel taken was 2.9 % slower than the best (geometric mean), 1.4 times at worst (1024 rows of 2048 x 512: 9.9 us by four CTAs a tile, 7.2 by one).  Both sides: one row of
+// 4096 x 4096 5.1 (few rows) and 8.9 us, 16 rows 7.2 and 9.0, 24 rows 11.5 and 9.0; 64 experts of 2048 x 2048, 4 rows each 67 and 48; 48 rows of 8192 x 1024
+// 8.6 by four CTAs a tile and 17 by one; 2048 rows of 4096 x 4096 38.4 by pairs and 39.7 by tiles of 128 channels.
+// SNN_FORCE_ROWS=few, many, or 64, 128 or 256 (with /2 or /4 behind the first two: CTAs that share a tile) in the environment takes that wherever it can run.
+struct Way {
+  int tile, split;   // output channels of a tile, 0: few rows, and CTAs that share it, or eights of rows of a piece
+};
+Way choose_way(const Scaled& p, const ScaledCall& c) {
+  const auto up = [](double a, double b) { return ceil(a / b); };
+  const double used = c.offsets ? min(p.E, c.rows) : 1, each = up(c.rows, used), sms = sm_count(), nk = p.n_kb, mb = used * p.n_kt * nk * 16384e-6;
+  const long long row_tiles = c.offsets ? c.rows / 128 + (long long)min(p.E, c.rows) : (c.rows + 127ll) / 128;   // at most
+  const int nt = each <= 8 ? 1 : each <= 16 ? 2 : 4;
+  const char* const force = getenv("SNN_FORCE_ROWS");
+  const auto can_share = [&](int tile, int split) { return row_tiles * ((p.K + tile - 1) / tile) * split <= (long long)sms && p.n_kb >= 2 * split; };
+  if (force) {
+    if (!strcmp(force, "few")) return {0, nt};
+    for (int tile = 64; tile <= 256; tile *= 2) {
+      char* end;
+      if (strtol(force, &end, 10) != tile) continue;
+      int split = *end == '/' && tile < 256 ? atoi(end + 1) : 1;
+      while (split > 1 && (split > 4 || !can_share(tile, split))) split /= 2;
+      return {tile, max(split, 1)};
+    }
+  }
+  const double turns = up(up(each, 8 * nt) * used * up(p.K, 16), 2 * sms);
+  Way best{0, nt};
+  double least = 1.5 + (nt == 4 ? 1.0 : 0.0) + 0.5 * turns +
+                 fmax(mb * (nt == 1 ? 0.2 : nt == 2 ? 0.29 : 0.55) * up(nk, 8) * 8 / fmax(nk, 8) * up(each, 8 * nt), turns * up(nk, 8) * (nt == 1 ? 0.5 : nt == 2 ? 0.8 : 1.5));
+  if (force && !strcmp(force, "many")) least = 1e30;
+  const auto offer = [&](int tile, int split, double time) {
+    if (time < least) {
+      least = time;
+      best = Way{tile, split};
+    }
+  };
+  for (int tile = 64; tile <= 128; tile *= 2)
+    for (int split = 1; split <= 4; split *= 2) {
+      if (split > 1 && !can_share(tile, split)) break;
+      const double n = used * up(each, 128) * up(p.K, tile) * split, around = up(n, sms), block = tile == 64 ? (around > 1 ? 0.235 : 0.215) : around > 1 ? 0.29 : 0.225;
+      offer(tile, split, fmax(3.5 + (up(nk, split) * block + 0.15) * around + (split == 1 ? 0.0 : tile == 64 ? 1.6 : 2.2), 2.5 + mb / (tile == 64 ? 4.5 : 6.0)));
+    }
+  const double around = up(used * up(each, 256) * up(p.K, 256), fmax(1.0, floor(sms / 2)));
+  offer(256, 1, fmax(3.5 + around * (nk * (around > 1 ? 0.53 : 0.47) + 0.3), 3.5 + mb / 4));
+  return best;
+}
+
 }  // namespace
 
 cudaError_t scaled_create(const uint8_t* weights, const float* scales, int E, int C, int K, cudaStream_t s, Scaled* p, int* launched) {
@@ -257,19 +307,9 @@ void scaled_destroy(Scaled* p) {
 }
 
 cudaError_t scaled_forward(const Scaled& p, const ScaledCall& c, int* launched) {
-  const long long each = c.offsets ? ((long long)c.rows + min(p.E, c.rows) - 1) / min(p.E, c.rows) : c.rows;
-  bool many = each > 16;
-  int shape = each > 256 ? 256 : each > 64 ? 128 : 64;
-  if (const char* f = getenv("SNN_FORCE_ROWS")) {
-    many = strcmp(f, "few") && (!strcmp(f, "many") || many);
-    if (!strcmp(f, "256") || !strcmp(f, "128") || !strcmp(f, "64")) {
-      many = true;
-      shape = atoi(f);
-    }
-  }
-  if (many) return scaled_tall(p, c, shape, launched);
-  if (each <= 8) return few_launch<1>(p, c, launched);
-  return each <= 16 ? few_launch<2>(p, c, launched) : few_launch<4>(p, c, launched);
+  const Way way = choose_way(p, c);
+  if (way.tile) return scaled_tall(p, c, way.tile, way.split, launched);
+  return way.split == 1 ? few_launch<1>(p, c, launched) : way.split == 2 ? few_launch<2>(p, c, launched) : few_launch<4>(p, c, launched);
 }
 
 }  // namespace snn

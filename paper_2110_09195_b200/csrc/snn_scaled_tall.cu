@@ -20,14 +20,14 @@ constexpr int ST_A_BYTES = ST_ROWS * 128;
 constexpr int ST_MAX_STAGES = 10;
 constexpr int ST_OUT_WARPS = 8;
 constexpr int ST_STAGING = 4096;      // of a warp: 32 rows of 128 bytes
-// warps: 0 copies of the rows, 1 MMA, 2 tensor memory, 3 copies of the weights, 4-11 sums and outputs
+// warps: 0 copies, 1 MMA, 2 tensor memory, 4-11 sums and outputs
 
 struct TallScaledParams {
   const float *w_scales, *x_scales;
   const int32_t* offsets;
   void* out;
   long long ld_scales, ld_out;
-  int rows, E, C, K, n_kt, n_kb, out_type, n_ct, stages, box, fours, eights;   // rows of a box of x; scales and outputs by 16 bytes
+  int rows, E, C, K, n_kt, n_kb, out_type, n_ct, stages, staging, box, split, fours, eights;   // rows of a box of x; CTAs that share a tile; scales and outputs by 16 bytes
   int* status;
 };
 struct TallScaledBars {
@@ -41,7 +41,7 @@ struct TallScaledShape {
   static constexpr int kStage = ST_A_BYTES + kParts * kBRows * 128;
   static constexpr int kBuffers = 4, kColumns = kN * kBuffers;     // of tensor memory: 512, 512, 256
   static constexpr int kWarps = ST_OUT_WARPS / kParts;             // that read a buffer, in each CTA
-  static constexpr int kFixed = 1024 + ST_OUT_WARPS * ST_STAGING + (int)sizeof(TallScaledBars);
+  static constexpr int kFixed = 1024 + (int)sizeof(TallScaledBars);
 };
 
 // Issued by the lanes for which `on` is not 0: D = A * B^T over 128 input channels in four steps of 32, then the commits: the stage is free, the buffer is full.
@@ -148,6 +148,12 @@ __device__ __forceinline__ void add_some(uint64_t* acc, const uint32_t (&v)[W], 
   for (int i = 0; i < W / 2; ++i) asm("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tfma.rn.f32x2 %0, t, %3, %0;\n\t}" : "+l"(acc[i]) : "r"(v[2 * i]), "r"(v[2 * i + 1]), "l"(f));
 }
 
+// 16 bytes to the shared memory of a CTA of the cluster.
+__device__ __forceinline__ void st_shared_of(uint32_t addr, int rank, float4 v) {
+  uint32_t there;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
 struct ScaledTile {
   int e, r0, n, ct;   // expert, first row, rows, channel tile
 };
@@ -175,15 +181,15 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
   constexpr int NB = S::kBuffers, PARTS = S::kParts;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint8_t* const staging = smem + p.stages * S::kStage;
-  TallScaledBars* const bars = reinterpret_cast<TallScaledBars*>(staging + ST_OUT_WARPS * ST_STAGING);
+  uint8_t* const staging = smem + p.stages * S::kStage;   // of the outputs, or what is received of the sums
+  TallScaledBars* const bars = reinterpret_cast<TallScaledBars*>(staging + p.staging);
   ScaledRanges R;
   R.lo = reinterpret_cast<int*>(bars + 1);
   R.n = R.lo + p.E;
   R.end = R.n + p.E;
   const int warp = uni(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const uint32_t base = (uint32_t)uni((int)smem_u32(smem));
-  const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, first_tile = (int)blockIdx.x / CG, step = (int)gridDim.x / CG;
+  const uint32_t base = (uint32_t)uni((int)smem_u32(smem)), received = smem_u32(staging);
+  const int rank = CG == 2 ? (int)(blockIdx.x & 1) : 0, shared_by = CG * p.split, first_tile = (int)blockIdx.x / shared_by, step = (int)gridDim.x / shared_by;
   if (warp == 0) {
     grid_dep_wait();
     // tiles of each expert, summed up: every lane a run of experts
@@ -206,7 +212,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
     for (int e = e0; e < e1; ++e) R.end[e] = end += (R.n[e] + CG * ST_ROWS - 1) / (CG * ST_ROWS);
   } else if (warp == 1 && lane == 0) {
     for (int i = 0; i < p.stages; ++i) {
-      mbar_init(smem_u32(&bars->full[i]), 2);
+      mbar_init(smem_u32(&bars->full[i]), 1);
       mbar_init(smem_u32(&bars->empty[i]), 1);
     }
     for (int i = 0; i < NB; ++i) {
@@ -230,17 +236,18 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
   if (warp > 2 || warp == 1) grid_dep_wait();
   tc_fence_before();
   __syncthreads();
-  if (CG == 2) pair_sync();
+  if (CG == 2 || p.split > 1) pair_sync();
   tc_fence_after();
   grid_dep_launch();   // (only now: a dependent that has tensor memory before this CTA does would wait for it for good)
   const uint32_t tmem = bars->tmem;
-  const int nk = p.n_kb;
+  // blocks of input channels: all, or this CTA's share of them
+  const int nk = p.n_kb, part = CG == 1 ? (int)blockIdx.x % p.split : 0, kb_first = nk * part / p.split, kb_last = nk * (part + 1) / p.split;
   bool ok = true;
   ScaledTile t{};
 
   if (warp < 4) {
     if (N == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0 || warp == 3) {
+    if (warp == 0) {
       // ------------------------------------------------------------ copies: a stage is 128 input channels of the rows and of the weights
       int s = 0, filled = 0;
       uint32_t phase = 0;
@@ -248,22 +255,19 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
       for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
         auto boxes = [&](int r) { return (min(max(t.n - r * ST_ROWS, 0), ST_ROWS) + p.box - 1) / p.box; };
         const int mine = boxes(rank);
-        const uint32_t bytes = (uint32_t)(warp ? CG * PARTS * S::kBRows : (boxes(0) + (CG == 2 ? boxes(1) : 0)) * p.box) * 128u;   // of both CTAs
+        const uint32_t bytes = (uint32_t)(CG * PARTS * S::kBRows + (boxes(0) + (CG == 2 ? boxes(1) : 0)) * p.box) * 128u;   // of both CTAs
         // the weights: 64 rows of each of two tiles, one, or half of one
         const int kt = N == 256 ? 2 * t.ct : N == 128 ? t.ct : t.ct >> 1, w_half = CG == 2 ? rank * 64 : N == 64 ? (t.ct & 1) * 64 : 0;
-        for (int kb = 0; kb < nk; ++kb) {
+        for (int kb = kb_first; kb < kb_last; ++kb) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->empty[s]), phase ^ 1u));
           if (!ok) break;
           const uint32_t full = smem_u32(&bars->full[s]), dst = base + s * S::kStage;
           if (leader) {   // (one lane: copies of several lanes are issued one after the other, 100 cycles each)
             if (rank == 0) mbar_expect_tx(full, bytes);
-            if (warp == 0) {
-              for (int i = 0; i < mine; ++i) copy_box<CG>(dst + i * p.box * 128, &x_map, kb * 128, t.r0 + rank * ST_ROWS + i * p.box, full);
-            } else {
+            for (int i = 0; i < mine; ++i) copy_box<CG>(dst + i * p.box * 128, &x_map, kb * 128, t.r0 + rank * ST_ROWS + i * p.box, full);
 #pragma unroll
-              for (int i = 0; i < PARTS; ++i)
-                copy_box<CG>(dst + ST_A_BYTES + i * S::kBRows * 128, &w_map, 0, ((t.e * p.n_kt + min(kt + i, p.n_kt - 1)) * nk + kb) * 128 + w_half, full);
-            }
+            for (int i = 0; i < PARTS; ++i)
+              copy_box<CG>(dst + ST_A_BYTES + i * S::kBRows * 128, &w_map, 0, ((t.e * p.n_kt + min(kt + i, p.n_kt - 1)) * nk + kb) * 128 + w_half, full);
           }
           __syncwarp();
           filled = min(filled + 1, p.stages);
@@ -289,7 +293,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
       const uint32_t leader = elect_one(), tmem_u = (uint32_t)uni((int)tmem);
       const uint32_t idesc = (1u << 4) | ((uint32_t)(S::kN >> 3) << 17) | ((uint32_t)(CG * ST_ROWS >> 4) << 24);   // fp32 sums of e4m3 values
       for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
-        for (int kb = 0; kb < nk; ++kb) {
+        for (int kb = kb_first; kb < kb_last; ++kb) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase));
           const uint32_t a = base + s * S::kStage;
 #pragma unroll
@@ -332,19 +336,19 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
       // Four blocks' scales on their way while four blocks are added up.  (They are multiplied where they are used: at the loads the warp would wait for them.)
       float next_x[4] = {}, next_w[4] = {};
       auto load = [&](int kb) {
-        ld_four(xs + kb, nk - kb, p.fours, next_x);
-        ld_four(ws + kb, nk - kb, p.fours, next_w);
+        ld_four(xs + kb, kb_last - kb, p.fours && kb + 4 <= kb_last, next_x);
+        ld_four(ws + kb, kb_last - kb, p.fours && kb + 4 <= kb_last, next_w);
       };
-      load(0);
+      load(kb_first);
       uint64_t acc[A / 2];
 #pragma unroll
       for (int i = 0; i < A / 2; ++i) acc[i] = 0;
-      for (int kb = 0; ok && kb < nk; kb += 4) {
+      for (int kb = kb_first; ok && kb < kb_last; kb += 4) {
         const float f[4] = {next_x[0] * next_w[0], next_x[1] * next_w[1], next_x[2] * next_w[2], next_x[3] * next_w[3]};
-        if (kb + 4 < nk) load(kb + 4);
+        if (kb + 4 < kb_last) load(kb + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (kb + i >= nk) break;
+          if (kb + i >= kb_last) break;
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), d_phase));
           if (!ok) break;
           tc_fence_after();
@@ -372,33 +376,50 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
         }
       }
       if (!ok) break;
+      if (CG == 1 && p.split > 1) {
+        // This CTA's share of the sums goes to the CTAs that have the channels: [CTA from][fours of channels][row], 16 bytes each.
+        const int fours = N / 4 / p.split;
+#pragma unroll
+        for (int i = 0; i < A / 4; ++i) {
+          const float2 u = floats_of(acc[2 * i]), v = floats_of(acc[2 * i + 1]);
+          const int four = half * (A / 4) + i, to = four / fours;
+          st_shared_of(received + (uint32_t)((part * fours + four - to * fours) * ST_ROWS + row) * 16u, to, make_float4(u.x, u.y, v.x, v.y));
+        }
+        continue;
+      }
       // Outputs through shared memory, 128 bytes of each row at a time (16-byte pieces, their order by the row: no bank twice), so that whole lines go out.
       const long long to = (long long)(t.r0 + rank * ST_ROWS + quarter * 32) * p.ld_out;
       const int rows = min(n - quarter * 32, 32);
-      auto pass = [&](auto words, int co, int each) {   // `each` values in 16 bytes
+      constexpr int PIECES = A < 64 ? 4 : 8;   // of 16-bit outputs
+      auto pass = [&](auto words, int co, int each, int pieces) {   // `each` values in 16 bytes
         __syncwarp();
 #pragma unroll
         for (int q = 0; q < 8; ++q) sts16(stage + lane * 128 + ((q ^ (lane & 7)) << 4), words(q));
         __syncwarp();
-        const int piece = lane & 7, c = co + piece * each, size = 16 / each;
+        const int size = 16 / each;
+        uint8_t* const first = static_cast<uint8_t*>(p.out) + (to + co) * size;
+        if (p.eights && co + pieces * each <= p.K) {
+          const int piece = lane & 7;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = 4 * i + (lane >> 3);
-          const uint4 v = lds16_at(stage + r * 128 + ((piece ^ (r & 7)) << 4));
-          if (r >= rows) continue;
-          uint8_t* const at = static_cast<uint8_t*>(p.out) + (to + (long long)r * p.ld_out + c) * size;
-          if (p.eights && c + each <= p.K) *reinterpret_cast<uint4*>(at) = v;
-          else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (size == 4) {
-                if (c + j < p.K) reinterpret_cast<uint32_t*>(at)[j] = w[j];
-              } else {
-                if (c + 2 * j < p.K) reinterpret_cast<uint16_t*>(at)[2 * j] = (uint16_t)w[j];
-                if (c + 2 * j + 1 < p.K) reinterpret_cast<uint16_t*>(at)[2 * j + 1] = (uint16_t)(w[j] >> 16);
-              }
+          for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 3);
+            const uint4 v = lds16_at(stage + r * 128 + ((piece ^ (r & 7)) << 4));
+            if (r < rows && piece < pieces) *reinterpret_cast<uint4*>(first + (long long)r * p.ld_out * size + piece * 16) = v;
           }
+        } else {   // (neighbouring lanes, neighbouring values)
+          for (int r = 0; r < rows; ++r)
+            for (int e = lane; e < pieces * each && co + e < p.K; e += 32) {
+              const uint32_t at = stage + r * 128 + ((e / each ^ (r & 7)) << 4) + e % each * size;
+              if (size == 4) {
+                uint32_t v;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+                reinterpret_cast<uint32_t*>(first + (long long)r * p.ld_out * 4)[e] = v;
+              } else {
+                uint16_t v;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
+                reinterpret_cast<uint16_t*>(first + (long long)r * p.ld_out * 2)[e] = v;
+              }
+            }
         }
       };
       if (rows > 0 && co0 < p.K) {   // (the same for all lanes)
@@ -408,7 +429,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
             pass([&](int q) {
               const float2 a = floats_of(acc[c / 2 + 2 * q]), b = floats_of(acc[c / 2 + 2 * q + 1]);
               return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
-            }, co0 + c, 4);
+            }, co0 + c, 4, 8);
         } else if (A >= 64) {
 #pragma unroll
           for (int c = 0; c < A; c += 64)
@@ -417,7 +438,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
 #pragma unroll
               for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, floats_of(acc[c / 2 + 4 * q + j]));
               return make_uint4(w[0], w[1], w[2], w[3]);
-            }, co0 + c, 8);
+            }, co0 + c, 8, PIECES);
         } else {   // (32 channels: half of a pass, the other half is not there)
           pass([&](int q) {
             uint32_t w[4] = {};
@@ -425,7 +446,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
 #pragma unroll
               for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, floats_of(acc[(4 * q + j) % (A / 2)]));
             return make_uint4(w[0], w[1], w[2], w[3]);
-          }, (lane & 7) < 4 ? co0 : p.K, 8);
+          }, co0, 8, PIECES);
         }
       }
     }
@@ -437,6 +458,34 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
   if (warp == 2) mbar_wait(smem_u32(&bars->drain), 0);   // (the last arrival here from the pair's MMAs)
   __syncwarp();
   if (CG == 2) pair_sync();
+  if (CG == 1 && p.split > 1) {
+    pair_sync();
+    // the sums over the CTAs in their order; a thread has a row and every second four of this CTA's channels
+    t = ScaledTile{};
+    if (warp >= 4 && scaled_tile<CG>(R, p.E, p.n_ct, first_tile, t)) {
+      const int row = ((int)threadIdx.x - 128) & 127, fours = N / 4 / p.split;
+      for (int four = ((int)threadIdx.x - 128) >> 7; four < fours; four += 2) {
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < p.split; ++k) {
+          const uint4 v = lds16_at(received + (uint32_t)((k * fours + four) * ST_ROWS + row) * 16u);
+          sum.x += __uint_as_float(v.x), sum.y += __uint_as_float(v.y), sum.z += __uint_as_float(v.z), sum.w += __uint_as_float(v.w);
+        }
+        const int co = t.ct * N + (part * fours + four) * 4;
+        const long long to = (long long)(t.r0 + row) * p.ld_out + co;
+        if (row >= t.n) continue;
+        if (p.eights && co + 4 <= p.K) {
+          if (p.out_type == SNN_OUT_F32) *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to) = sum;
+          else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + to) = make_uint2(pack_pair(p.out_type, make_float2(sum.x, sum.y)), pack_pair(p.out_type, make_float2(sum.z, sum.w)));
+        } else {
+          const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (co + j < p.K) store_out(p.out, p.out_type, to + j, v[j]);
+        }
+      }
+    }
+  }
   tc_fence_after();
   if (warp == 2) {
     if (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kColumns) : "memory");
@@ -444,7 +493,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
   }
 }
 constexpr int ST_THREADS = 128 + 32 * ST_OUT_WARPS;
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ST_THREADS, 1)
+__global__ void __launch_bounds__(ST_THREADS, 1)
     scaled_pair_kernel(const TallScaledParams p, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map) {
   scaled_tall_body<2, 256>(p, x_map, w_map);
 }
@@ -462,7 +511,7 @@ bool rows_map(CUtensorMap* map, const void* base, long long columns, long long r
 }
 
 template <int CG, int N, class Kernel>
-cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p, const ScaledCall& c, int* launched) {
+cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p, const ScaledCall& c, int split, int* launched) {
   using S = TallScaledShape<CG, N>;
   cudaError_t e = allow_max_smem(kernel, done);
   if (e != cudaSuccess) return e;
@@ -473,22 +522,36 @@ cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p
   if (!rows_map(&x_map, c.act, p.C, c.rows, c.ld_act, box, true) ||
       !rows_map(&w_map, p.tiles, 128, (long long)p.E * p.n_kt * p.n_kb * 128, 128, S::kBRows, false))
     return cudaErrorInvalidValue;
-  const int size = c.out_type == SNN_OUT_F32 ? 4 : 2, fixed = S::kFixed + p.E * 12;
+  const int size = c.out_type == SNN_OUT_F32 ? 4 : 2, staging = split > 1 && ST_ROWS * N * 4 > ST_OUT_WARPS * ST_STAGING ? ST_ROWS * N * 4 : ST_OUT_WARPS * ST_STAGING,
+            fixed = S::kFixed + staging + p.E * 12;
   const TallScaledParams q{p.scales, c.scales, c.offsets, c.out, c.ld_scales, c.ld_out, c.rows, p.E, p.C, p.K, p.n_kt, p.n_kb, c.out_type, (p.K + N - 1) / N,
-                           min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::kStage), box, p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
+                           min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::kStage), staging, box, split, p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
                            c.ld_out * size % 16 == 0 && ((uintptr_t)c.out & 15) == 0, p.status_dev};
   const long long tiles = ((long long)c.rows / (CG * ST_ROWS) + (c.offsets ? min(p.E, c.rows) : 1)) * q.n_ct;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)(CG * split);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.stream = c.stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cfg.gridDim = dim3((unsigned)(CG * split * min(tiles, (long long)max(1, sm_count() / (CG * split)))));
+  cfg.blockDim = dim3(ST_THREADS);
+  cfg.dynamicSmemBytes = (size_t)(fixed + q.stages * S::kStage);
   *launched += 1;
-  return launch_dependent(kernel, (unsigned)(CG * min(tiles, (long long)max(1, sm_count() / CG))), ST_THREADS, (size_t)(fixed + q.stages * S::kStage), c.stream, q, x_map, w_map);
+  return cudaLaunchKernelEx(&cfg, kernel, q, x_map, w_map);
 }
 
 }  // namespace
 
-cudaError_t scaled_tall(const Scaled& p, const ScaledCall& c, int shape, int* launched) {
+cudaError_t scaled_tall(const Scaled& p, const ScaledCall& c, int shape, int split, int* launched) {
   static unsigned long long done[3] = {0, 0, 0};
-  if (shape == 256) return tall_launch<2, 256>(scaled_pair_kernel, done, p, c, launched);
-  if (shape == 128) return tall_launch<1, 128>(scaled_single_kernel<128>, done + 1, p, c, launched);
-  return tall_launch<1, 64>(scaled_single_kernel<64>, done + 2, p, c, launched);
+  if (shape == 256) return tall_launch<2, 256>(scaled_pair_kernel, done, p, c, 1, launched);
+  if (shape == 128) return tall_launch<1, 128>(scaled_single_kernel<128>, done + 1, p, c, split, launched);
+  return tall_launch<1, 64>(scaled_single_kernel<64>, done + 2, p, c, split, launched);
 }
 
 }  // namespace snn
