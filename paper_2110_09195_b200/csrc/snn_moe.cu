@@ -84,6 +84,16 @@ struct UpParams {
   Powers pow;
 };
 
+__device__ __forceinline__ int ld_int(const int32_t* p) {
+  int v;
+  asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ float ld_number(const float* p) {
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
 // A team of warps and nobody else (one warp: the barrier is its own).
 __device__ __forceinline__ void team_sync(int team, int warps) {
   __syncwarp();
@@ -96,11 +106,12 @@ __device__ __forceinline__ void team_sync(int team, int warps) {
 // behind the activation goes to memory as the sum of `parts` bf16 numbers.
 template <class T, bool GATE>
 __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
-  constexpr int G = GATE ? 2 : 1, M = MO_M, WIDE = G * M;
+  constexpr int G = GATE ? 2 : 1, WIDE = G * MO_M;
   __shared__ float red_both[2][8][MO_N][WIDE + 1];
   __shared__ int s_ids[MO_FEW], s_rows[MO_FEW], s_first[MO_FEW], s_total;
   __shared__ float s_weights[MO_FEW];
   __shared__ int4 s_pieces[MO_FEW];
+  __shared__ int s_offsets[SNN_EXPERTS_MAX + 1];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int choices = p.tokens * p.route.k;
   Pieces counted{0, 0, 0};
@@ -177,7 +188,9 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.work.total = s_total;
   } else {
     grid_dep_wait();
-    counted = count_pieces(p.work.offsets, p.E, choices, MO_N);
+    for (int i = threadIdx.x; i <= p.E; i += 256) s_offsets[i] = ld_int(p.work.offsets + i);
+    __syncthreads();
+    counted = count_pieces(s_offsets, p.E, choices, MO_N);
     if (blockIdx.x == 0) {
       for (int i = threadIdx.x; i < choices; i += 256) {
         const int slot = p.work.slots[i];
@@ -185,7 +198,7 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
       }
       for (int i = warp; i < counted.total; i += 8) {
         int e, r0, n;
-        find_piece(counted, p.work.offsets, p.E, choices, MO_N, i, &e, &r0, &n);
+        find_piece(counted, s_offsets, p.E, choices, MO_N, i, &e, &r0, &n);
         if (lane == 0) p.work.pieces[i] = make_int4(e, r0, n, 0);
       }
       if (threadIdx.x == 0) *p.work.total = counted.total;
@@ -193,63 +206,82 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
   }
   grid_dep_launch();
   const Powers pow = in_registers(p.pow);
-  const int team = warp / p.k_warps, kw = warp - team * p.k_warps, teams = 8 / p.k_warps, strips = (p.H + M - 1) / M;
+  const int team = warp / p.k_warps, kw = warp - team * p.k_warps, teams = 8 / p.k_warps, strips = (p.H + MO_M - 1) / MO_M;
   const long long items = (long long)counted.total * strips, all = (long long)gridDim.x * teams, me = (long long)blockIdx.x * teams + team;
   const int* const rows = p.fused ? s_rows : p.work.rows;
-  long long item = items * me / all;
-  const long long last = items * (me + 1) / all;
   const size_t step = (size_t)choices * p.H;
-  int turn = 0, piece = -1, e = 0, r0 = 0, n = 0;
-  const uint16_t* x = nullptr;
-  for (; item < last; ++item) {
-    const int now = (int)(item / strips), strip = (int)(item - (long long)now * strips);
-    if (now != piece) {
-      piece = now;
-      if (p.fused) {
-        const int4 v = s_pieces[piece];
-        e = v.x, r0 = v.y, n = v.z;
-      } else {
-        find_piece(counted, p.work.offsets, p.E, choices, MO_N, piece, &e, &r0, &n);
-      }
-      x = g < n ? static_cast<const uint16_t*>(p.act) + (size_t)rows[r0 + g] * (size_t)p.ld_act + 8 * t : nullptr;
+  // An item's rows and weights, as they are asked for: a block of input channels ahead, across the ends of items.
+  struct Place {
+    int piece, strip, e, r0, n;
+    const uint16_t* x;
+  };
+  auto find = [&](Place& at) {
+    if (p.fused) {
+      const int4 v = s_pieces[at.piece];
+      at.e = v.x, at.r0 = v.y, at.n = v.z;
+    } else {
+      find_piece(counted, s_offsets, p.E, choices, MO_N, at.piece, &at.e, &at.r0, &at.n);
     }
-    const size_t expert = (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
+    at.x = g < at.n ? static_cast<const uint16_t*>(p.act) + (size_t)rows[at.r0 + g] * (size_t)p.ld_act + 8 * t : nullptr;
+  };
+  const long long first = items * me / all, last = items * (me + 1) / all;
+  if (first >= last) return;
+  TileBits bits[G], more[G];
+  uint4 b[4][1][2];   // the rows of four blocks of 64: each is asked for again as soon as it has been used
+  auto load_bits = [&](const Place& at, int kb) {
+    const size_t expert = (size_t)at.e * p.n_mt * p.n_kb * 64 + 8 * g + t;
+#pragma unroll
+    for (int i = 0; i < G; ++i) more[i].load(reinterpret_cast<const uint2*>(p.bits[GATE ? i : 1]) + expert, 2 * at.strip, p.n_kb, kb);
+  };
+  auto load_rows = [&](const Place& at, int kb, int j) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = kb * 256 + j * 64 + 32 * h;
+      b[j][0][h] = at.x && c + 8 * t < p.C ? ld16(at.x + c) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  Place now{(int)(first / strips), (int)(first % strips), 0, 0, 0, nullptr};
+  find(now);
+  load_bits(now, kw);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) load_rows(now, kw, j);
+  int turn = 0;
+  for (long long item = first; item < last; ++item) {
+    // the scales of the channels whose outputs this lane writes
+    const size_t of = (size_t)now.e * p.n_mt * 16 + now.strip * MO_M;
+    float alpha[G][4];
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q == 0 || p.k_warps == 1) alpha[i][q] = ld_number(p.alpha[GATE ? i : 1] + of + (p.k_warps == 1 ? g + 8 * q : lane));
     float acc[G][2][4] = {};
-    TileBits bits[G], more[G];
-    uint4 b[4][1][2];   // the rows of four blocks of 64: each is asked for again, 256 channels on, as soon as it has been used
-    auto load_bits = [&](int kb) {
-#pragma unroll
-      for (int i = 0; i < G; ++i) more[i].load(reinterpret_cast<const uint2*>(p.bits[GATE ? i : 1]) + expert, 2 * strip, p.n_kb, kb);
-    };
-    auto load_rows = [&](int kb, int j) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = kb * 256 + j * 64 + 32 * h;
-        b[j][0][h] = x && c + 8 * t < p.C ? ld16(x + c) : make_uint4(0, 0, 0, 0);
-      }
-    };
-    if (kw < p.n_kb) {
-      load_bits(kw);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) load_rows(kw, j);
-    }
+    Place then = now;
     for (int kb = kw; kb < p.n_kb; kb += p.k_warps) {
 #pragma unroll
       for (int i = 0; i < G; ++i) bits[i] = more[i];
-      const bool another = kb + p.k_warps < p.n_kb;
-      if (another) load_bits(kb + p.k_warps);
+      int next = kb + p.k_warps;
+      bool another = true;
+      if (next >= p.n_kb) {   // the next item's
+        next = kw;
+        another = item + 1 < last;
+        if (another && ++then.strip == strips) {
+          then.strip = 0;
+          ++then.piece;
+          find(then);
+        }
+      }
+      if (another) load_bits(then, next);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
 #pragma unroll
         for (int i = 0; i < G; ++i) multiply64<T, 1>(acc[i], bits[i], j, b[j], pow);
-        if (another) load_rows(kb + p.k_warps, j);
+        if (another) load_rows(then, next, j);
       }
     }
     // 8 bits at a time, cut (the rests are exact), the last part rounded; an infinity or NaN in the first
-    auto write = [&](int c, int co, float first, float second) {
-      const size_t of = (size_t)e * p.n_mt * 16 + co;
-      const float v = GATE ? activated(p.fn, p.alpha[0][of] * first) * (p.alpha[1][of] * second) : activated(p.fn, p.alpha[1][of] * first);
-      uint16_t* const to = p.work.h + (size_t)(r0 + c) * p.H + co;
+    auto write = [&](int c, int co, float v) {
+      uint16_t* const to = p.work.h + (size_t)(now.r0 + c) * p.H + co;
       float rest = v;
       const bool finite = fabsf(v) <= 3.402823466e38f;
       for (int k = 0; k < p.parts; ++k) {
@@ -264,29 +296,32 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int c = 2 * t + (q & 1), co = strip * M + 16 * m + g + 8 * (q >> 1);
-          if (c < n && co < p.H) write(c, co, acc[0][m][q], acc[G - 1][m][q]);
+          const int c = 2 * t + (q & 1), ch = 2 * m + (q >> 1), co = now.strip * MO_M + g + 8 * ch;
+          const float v = activated(p.fn, alpha[0][ch] * acc[0][m][q]);
+          if (c < now.n && co < p.H) write(c, co, GATE ? v * (alpha[G - 1][ch] * acc[G - 1][m][q]) : v);
         }
-      continue;
-    }
-    float (*const red)[MO_N][WIDE + 1] = red_both[turn] + team * p.k_warps;
-    turn ^= 1;
+    } else {
+      float (*const red)[MO_N][WIDE + 1] = red_both[turn] + team * p.k_warps;
+      turn ^= 1;
 #pragma unroll
-    for (int i = 0; i < G; ++i)
+      for (int i = 0; i < G; ++i)
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) red[kw][2 * t + (q & 1)][M * i + 16 * m + g + 8 * (q >> 1)] = acc[i][m][q];
-    team_sync(team, p.k_warps);   // (the other half of the buffer is for the next strip)
-    for (int i = kw * 32 + lane; i < n * M; i += p.k_warps * 32) {
-      const int c = i / M, m = i % M, co = strip * M + m;
-      float s[2] = {};
-      for (int k = 0; k < p.k_warps; ++k) {
-        s[0] += red[k][c][m];
-        if (GATE) s[1] += red[k][c][M + m];
+          for (int q = 0; q < 4; ++q) red[kw][2 * t + (q & 1)][MO_M * i + 16 * m + g + 8 * (q >> 1)] = acc[i][m][q];
+      team_sync(team, p.k_warps);   // (the other half of the buffer is for the next strip)
+      const int co = now.strip * MO_M + lane;
+      for (int c = kw; c < now.n; c += p.k_warps) {
+        float sum[2] = {};
+        for (int k = 0; k < p.k_warps; ++k) {
+          sum[0] += red[k][c][lane];
+          if (GATE) sum[1] += red[k][c][MO_M + lane];
+        }
+        const float v = activated(p.fn, alpha[0][0] * sum[0]);
+        if (co < p.H) write(c, co, GATE ? v * (alpha[G - 1][0] * sum[1]) : v);
       }
-      if (co < p.H) write(c, co, s[0], s[1]);
     }
+    now = then;
   }
 }
 
@@ -323,8 +358,8 @@ __device__ __forceinline__ int4 ld_piece(const int4* p) {
 constexpr int MO_LD = MO_M + 1;
 template <int PARTS>
 __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
-  constexpr int M = MO_M, LD = MO_LD, RING = PARTS == 3 ? 2 : 4;
-  extern __shared__ float sums[];   // [8][tokens][LD]
+  constexpr int LD = MO_LD, RING = PARTS == 3 ? 2 : 4;
+  extern __shared__ float sums[];   // [8][tokens][LD], then the pieces
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int strip = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x % p.cluster, table = p.tokens * LD;
   float* const mine = sums + warp * table;
@@ -333,70 +368,101 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   const Powers pow = in_registers(p.pow);
   grid_dep_wait();
   grid_dep_launch();
-  int total;
-  asm volatile("ld.global.s32 %0, [%1];" : "=r"(total) : "l"(p.total));
+  const int total = ld_int(p.total);
+  int4* const pieces = reinterpret_cast<int4*>(sums + 8 * table);
+  for (int i = threadIdx.x; i < total; i += 256) pieces[i] = ld_piece(p.pieces + i);
+  __syncthreads();
   const long long units = (long long)total * p.n_kb;
   const int w = rank * 8 + warp, warps = p.cluster * 8;
-  long long unit = units * w / warps;
-  const long long last = units * (w + 1) / warps;
+  const long long first = units * w / warps, last = units * (w + 1) / warps;
   const size_t step = (size_t)p.choices * p.C;
-  while (unit < last) {
-    const int piece = (int)(unit / p.n_kb), kb0 = (int)(unit - (long long)piece * p.n_kb);
-    const int kb1 = (int)min((long long)p.n_kb, kb0 + (last - unit));
-    unit += kb1 - kb0;
-    const int4 of = ld_piece(p.pieces + piece);
-    const int e = of.x, r0 = of.y, n = of.z;
-    const uint2* const from = reinterpret_cast<const uint2*>(p.bits) + (size_t)e * p.n_mt * p.n_kb * 64 + 8 * g + t;
-    const uint16_t* const x = p.h + (size_t)(r0 + g) * p.C + 8 * t;
-    float acc[2][4] = {};
-    TileBits bits, more;
-    uint4 b[RING][PARTS][2];   // the rows of the next blocks of 64
-    auto load_rows = [&](int kb, int j) {
+  TileBits bits, more;
+  uint4 b[RING][PARTS][2];   // the rows of the next blocks of 64, as in the first launch
+  struct Place {
+    int piece, kb, e, r0, n;
+    const uint16_t* x;
+  };
+  auto find = [&](Place& at) {
+    const int4 v = pieces[at.piece];
+    at.e = v.x, at.r0 = v.y, at.n = v.z;
+    at.x = p.h + (size_t)(at.r0 + g) * p.C + 8 * t;
+  };
+  auto load_bits = [&](const Place& at) {
+    more.load(reinterpret_cast<const uint2*>(p.bits) + (size_t)at.e * p.n_mt * p.n_kb * 64 + 8 * g + t, 2 * strip, p.n_kb, at.kb);
+  };
+  auto load_rows = [&](const Place& at, int j) {
 #pragma unroll
-      for (int k = 0; k < PARTS; ++k)
+    for (int k = 0; k < PARTS; ++k)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int c = kb * 256 + j * 64 + 32 * h;
-          b[j % RING][k][h] = g < n && c + 8 * t < p.C ? ld16(x + k * step + c) : make_uint4(0, 0, 0, 0);
+      for (int h = 0; h < 2; ++h) {
+        const int c = at.kb * 256 + j * 64 + 32 * h;
+        b[j % RING][k][h] = g < at.n && c + 8 * t < p.C ? ld16(at.x + k * step + c) : make_uint4(0, 0, 0, 0);
+      }
+  };
+  Place now{};
+  if (first < last) {
+    now.piece = (int)(first / p.n_kb);
+    now.kb = (int)(first % p.n_kb);
+    find(now);
+    load_bits(now);
+#pragma unroll
+    for (int j = 0; j < RING; ++j) load_rows(now, j);
+  }
+  float acc[2][4] = {}, alpha[4], share[2];
+  int token[2];
+  bool begins = true;
+  for (long long unit = first; unit < last; ++unit) {
+    if (begins) {   // what its outputs need
+#pragma unroll
+      for (int q = 0; q < 4; ++q) alpha[q] = ld_number(p.alpha + (size_t)now.e * p.n_mt * 16 + strip * MO_M + g + 8 * q);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        share[q] = 2 * t + q < now.n ? ld_number(p.shares + now.r0 + 2 * t + q) : 0.f;
+        token[q] = 2 * t + q < now.n ? ld_int(p.rows + now.r0 + 2 * t + q) : 0;
+      }
+    }
+    bits = more;
+    Place then = now;
+    const bool another = unit + 1 < last;
+    if (++then.kb == p.n_kb) {
+      then.kb = 0;
+      ++then.piece;
+      if (another) find(then);
+    }
+    if (another) load_bits(then);
+    float part[2][4] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      multiply64<BF16, PARTS>(PARTS == 3 ? part : acc, bits, j, b[j % RING], pow);
+      if (j + RING < 4) load_rows(now, j + RING);
+      else if (another) load_rows(then, j + RING - 4);
+    }
+    if (PARTS == 3)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[m][q] += part[m][q];
+    begins = then.kb == 0 || !another;
+    if (begins) {   // (a piece's rows are of different tokens)
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        if (2 * t + q < now.n) {
+          float* const to = mine + token[q] * LD + g;
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              float* const at = to + 16 * m + 8 * u;
+              *at = fmaf(share[q], alpha[2 * m + u] * acc[m][2 * u + q], *at);
+              acc[m][2 * u + q] = 0.f;
+            }
+        } else {
+#pragma unroll
+          for (int m = 0; m < 2; ++m) acc[m][q] = acc[m][2 + q] = 0.f;
         }
-    };
-    more.load(from, 2 * strip, p.n_kb, kb0);
-#pragma unroll
-    for (int j = 0; j < RING; ++j) load_rows(kb0, j);
-    for (int kb = kb0; kb < kb1; ++kb) {
-      bits = more;
-      if (kb + 1 < kb1) more.load(from, 2 * strip, p.n_kb, kb + 1);
-      float part[2][4] = {};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        multiply64<BF16, PARTS>(PARTS == 3 ? part : acc, bits, j, b[j % RING], pow);
-        if (j + RING < 4) load_rows(kb, j + RING);
-        else if (kb + 1 < kb1) load_rows(kb + 1, j + RING - 4);
-      }
-      if (PARTS == 3)
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) acc[m][q] += part[m][q];
+      __syncwarp();
     }
-    // (a piece's rows are of different tokens)
-    const float* const alpha = p.alpha + (size_t)e * p.n_mt * 16 + strip * M;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int c = 2 * t + q;
-      if (c < n) {
-        const float share = p.shares[r0 + c];
-        float* const to = mine + p.rows[r0 + c] * LD;
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int ch = 16 * m + 8 * u + g;
-            to[ch] = fmaf(share, alpha[ch] * acc[m][2 * u + q], to[ch]);
-          }
-      }
-    }
-    __syncwarp();
+    now = then;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < table; i += 256) {
@@ -407,8 +473,8 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   }
   if (p.cluster > 1) cluster_sync();
   else __syncthreads();
-  for (int i = rank * 256 + (int)threadIdx.x; i < p.tokens * M; i += p.cluster * 256) {
-    const int token = i / M, ch = i % M, co = strip * M + ch;
+  for (int i = rank * 256 + (int)threadIdx.x; i < p.tokens * MO_M; i += p.cluster * 256) {
+    const int token = i / MO_M, ch = i % MO_M, co = strip * MO_M + ch;
     float s = 0.f;
     for (int k = 0; k < p.cluster; ++k) s += p.cluster > 1 ? ld_cluster(smem_u32(sums + token * LD + ch), k) : sums[token * LD + ch];
     if (co < p.K) store_out(p.out, p.out_type, token * p.ld_out + co, s);
@@ -433,7 +499,7 @@ cudaError_t down_launch(const DownParams& p, unsigned strips, cudaStream_t s) {
   cfg.numAttrs = 2;
   cfg.gridDim = dim3(strips * (unsigned)p.cluster);
   cfg.blockDim = dim3(256);
-  cfg.dynamicSmemBytes = (size_t)8 * p.tokens * MO_LD * 4;
+  cfg.dynamicSmemBytes = (size_t)8 * p.tokens * MO_LD * 4 + (size_t)p.choices * 16;
   return cudaLaunchKernelEx(&cfg, moe_down_kernel<PARTS>, p);
 }
 
@@ -478,7 +544,7 @@ cudaError_t moe_forward(const MoeCall& c, int* launched) {
   const long long ctas = 2ll * sm_count(), pieces = ((long long)choices + (long long)min(E, choices) * (MO_N - 1)) / MO_N, items = pieces * ((up.K + MO_M - 1) / MO_M);
   // Warps of a team, by what its longest run takes: blocks of input channels, and for each item about half of one around them.
   double best = 0;
-  for (int k = 1; k <= 8; k *= 2) {
+  for (int k = 1; k <= min(8, up.n_kb); k *= 2) {   // (every warp has input channels)
     const long long teams = min(ctas * (8 / k), (items + 8 / k - 1) / (8 / k) * (8 / k)), runs = (items + teams - 1) / teams;
     const double time = runs * ((up.n_kb + k - 1) / k + (k == 1 ? 0.5 : 0.8));
     if (k == 1 || time < best) {
