@@ -16,8 +16,7 @@ namespace {
 //   operands, and as many arrive; alone with 128 x 256 it would be 96 and 96, more than shared memory gives.
 //   CG = 1, N = 128 or 64: fewer rows, more tiles, for problems that would leave SMs without any.
 constexpr int ST_ROWS = 128;          // of a CTA's tile
-constexpr int ST_A_BYTES = ST_ROWS * 128;
-constexpr int ST_MAX_STAGES = 10;
+constexpr int ST_MAX_STAGES = 16;
 constexpr int ST_OUT_WARPS = 8;
 constexpr int ST_STAGING = 4096;      // of a warp: 32 rows of 128 bytes
 // warps: 0 copies, 1 MMA, 2 tensor memory, 4-11 sums and outputs
@@ -27,7 +26,7 @@ struct TallScaledParams {
   const int32_t* offsets;
   void* out;
   long long ld_scales, ld_out;
-  int rows, E, C, K, n_kt, n_kb, out_type, n_ct, stages, staging, box, split, fours, eights;   // rows of a box of x; CTAs that share a tile; scales and outputs by 16 bytes
+  int rows, E, C, K, n_kt, n_kb, out_type, n_ct, stages, stage, staging, region, box, split, fours, eights;   // rows of x in a stage and of a box; CTAs that share a tile; scales and outputs by 16 bytes
   int* status;
 };
 struct TallScaledBars {
@@ -37,22 +36,25 @@ struct TallScaledBars {
 template <int CG, int N>
 struct TallScaledShape {
   static constexpr int kParts = CG;                                // instructions of N / CG channels for a block, each with buffers of its own
+  static constexpr int kBlocks = 3 - CG;                           // blocks that go through the stages and buffers together
   static constexpr int kN = N / kParts, kBRows = kN / CG;          // channels of an instruction, and rows of the weights that each CTA has of them
-  static constexpr int kStage = ST_A_BYTES + kParts * kBRows * 128;
-  static constexpr int kBuffers = 4, kColumns = kN * kBuffers;     // of tensor memory: 512, 512, 256
+  // A block's rows (a region of as many as a tile can have: the instruction reads 128, and what it makes of those behind them, other operands or outputs of before, is nobody's),
+  // and its weights
+  static int stage(int region) { return kBlocks * (region * 128 + kParts * kBRows * 128); }
+  static constexpr int kBuffers = N == 128 ? 2 : 4, kColumns = 512;   // of tensor memory
   static constexpr int kWarps = ST_OUT_WARPS / kParts;             // that read a buffer, in each CTA
   static constexpr int kFixed = 1024 + (int)sizeof(TallScaledBars);
 };
 
 // Issued by the lanes for which `on` is not 0: D = A * B^T over 128 input channels in four steps of 32, then the commits: the stage is free, the buffer is full.
-// (the stage only if `last`)
+// (the former if `frees`, the latter if `fills`)
 template <int CG>
-__device__ __forceinline__ void block_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t last);
+__device__ __forceinline__ void block_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t frees, uint32_t fills);
 template <>
-__device__ __forceinline__ void block_e4m3<2>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t last) {
+__device__ __forceinline__ void block_e4m3<2>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t frees, uint32_t fills) {
   asm volatile(
-      "{\n\t.reg .pred q, z;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
-      "setp.ne.b32 q, %6, 0;\n\tsetp.ne.and.b32 z, %8, 0, q;\n\t"
+      "{\n\t.reg .pred q, y, z;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "setp.ne.b32 q, %6, 0;\n\tsetp.ne.and.b32 z, %8, 0, q;\n\tsetp.ne.and.b32 y, %9, 0, q;\n\t"
       "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
       "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, 0;\n\t"
@@ -60,24 +62,24 @@ __device__ __forceinline__ void block_e4m3<2>(uint32_t d, uint64_t adesc, uint64
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a2, b2, %3, 1;\n\t"
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a3, b3, %3, 1;\n\t"
       "@z tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%4], %7;\n\t"
-      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], %7;\n\t}" ::"r"(d),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on), "h"((uint16_t)3), "r"(last)
+      "@y tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], %7;\n\t}" ::"r"(d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on), "h"((uint16_t)3), "r"(frees), "r"(fills)
       : "memory");
 }
 template <>
-__device__ __forceinline__ void block_e4m3<1>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t) {
+__device__ __forceinline__ void block_e4m3<1>(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t frees, uint32_t fills) {
   asm volatile(
-      "{\n\t.reg .pred q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
-      "setp.ne.b32 q, %6, 0;\n\t"
+      "{\n\t.reg .pred q, y, z;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "setp.ne.b32 q, %6, 0;\n\tsetp.ne.and.b32 z, %7, 0, q;\n\tsetp.ne.and.b32 y, %8, 0, q;\n\t"
       "add.u64 a1, %1, 2;\n\tadd.u64 a2, %1, 4;\n\tadd.u64 a3, %1, 6;\n\t"
       "add.u64 b1, %2, 2;\n\tadd.u64 b2, %2, 4;\n\tadd.u64 b3, %2, 6;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, 0;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a1, b1, %3, 1;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a2, b2, %3, 1;\n\t"
       "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a3, b3, %3, 1;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on)
+      "@z tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t"
+      "@y tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t}" ::"r"(d),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(bar0), "r"(bar1), "r"(on), "r"(frees), "r"(fills)
       : "memory");
 }
 template <int CG>
@@ -178,10 +180,10 @@ __device__ __forceinline__ bool scaled_tile(const ScaledRanges& R, int E, int n_
 template <int CG, int N>
 __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, const CUtensorMap& x_map, const CUtensorMap& w_map) {
   using S = TallScaledShape<CG, N>;
-  constexpr int NB = S::kBuffers, PARTS = S::kParts;
+  constexpr int NB = S::kBuffers, PARTS = S::kParts, BLOCKS = S::kBlocks;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  uint8_t* const staging = smem + p.stages * S::kStage;   // of the outputs, or what is received of the sums
+  uint8_t* const staging = smem + p.stages * p.stage;   // of the outputs, or what is received of the sums
   TallScaledBars* const bars = reinterpret_cast<TallScaledBars*>(staging + p.staging);
   ScaledRanges R;
   R.lo = reinterpret_cast<int*>(bars + 1);
@@ -255,19 +257,25 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
       for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
         auto boxes = [&](int r) { return (min(max(t.n - r * ST_ROWS, 0), ST_ROWS) + p.box - 1) / p.box; };
         const int mine = boxes(rank);
-        const uint32_t bytes = (uint32_t)(CG * PARTS * S::kBRows + (boxes(0) + (CG == 2 ? boxes(1) : 0)) * p.box) * 128u;   // of both CTAs
+        const uint32_t bytes = (uint32_t)(CG * PARTS * S::kBRows + (boxes(0) + (CG == 2 ? boxes(1) : 0)) * p.box) * 128u;   // of a block, of both CTAs
         // the weights: 64 rows of each of two tiles, one, or half of one
         const int kt = N == 256 ? 2 * t.ct : N == 128 ? t.ct : t.ct >> 1, w_half = CG == 2 ? rank * 64 : N == 64 ? (t.ct & 1) * 64 : 0;
-        for (int kb = kb_first; kb < kb_last; ++kb) {
+        for (int kb = kb_first; kb < kb_last; kb += BLOCKS) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->empty[s]), phase ^ 1u));
           if (!ok) break;
-          const uint32_t full = smem_u32(&bars->full[s]), dst = base + s * S::kStage;
+          const uint32_t full = smem_u32(&bars->full[s]), dst = base + s * p.stage;
+          const int blocks = min(BLOCKS, kb_last - kb);
           if (leader) {   // (one lane: copies of several lanes are issued one after the other, 100 cycles each)
-            if (rank == 0) mbar_expect_tx(full, bytes);
-            for (int i = 0; i < mine; ++i) copy_box<CG>(dst + i * p.box * 128, &x_map, kb * 128, t.r0 + rank * ST_ROWS + i * p.box, full);
+            if (rank == 0) mbar_expect_tx(full, blocks * bytes);
 #pragma unroll
-            for (int i = 0; i < PARTS; ++i)
-              copy_box<CG>(dst + ST_A_BYTES + i * S::kBRows * 128, &w_map, 0, ((t.e * p.n_kt + min(kt + i, p.n_kt - 1)) * nk + kb) * 128 + w_half, full);
+            for (int u = 0; u < BLOCKS; ++u) {
+              if (u >= blocks) break;
+              for (int i = 0; i < mine; ++i)
+                copy_box<CG>(dst + (u * p.region + i * p.box) * 128, &x_map, (kb + u) * 128, t.r0 + rank * ST_ROWS + i * p.box, full);
+#pragma unroll
+              for (int i = 0; i < PARTS; ++i)
+                copy_box<CG>(dst + (BLOCKS * p.region + (u * PARTS + i) * S::kBRows) * 128, &w_map, 0, ((t.e * p.n_kt + min(kt + i, p.n_kt - 1)) * nk + kb + u) * 128 + w_half, full);
+            }
           }
           __syncwarp();
           filled = min(filled + 1, p.stages);
@@ -293,17 +301,22 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
       const uint32_t leader = elect_one(), tmem_u = (uint32_t)uni((int)tmem);
       const uint32_t idesc = (1u << 4) | ((uint32_t)(S::kN >> 3) << 17) | ((uint32_t)(CG * ST_ROWS >> 4) << 24);   // fp32 sums of e4m3 values
       for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
-        for (int kb = kb_first; kb < kb_last; ++kb) {
+        for (int kb = kb_first; kb < kb_last; kb += BLOCKS) {
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase));
-          const uint32_t a = base + s * S::kStage;
+          const uint32_t a = base + s * p.stage;
 #pragma unroll
           for (int i = 0; i < PARTS; ++i) {
             ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(&bars->d_empty[d]), d_phase ^ 1u));
             if (!ok) break;
             tc_fence_after();
-            block_e4m3<CG>(tmem_u + d * S::kN, rows_desc(a), rows_desc(a + ST_A_BYTES + i * S::kBRows * 128), idesc, smem_u32(&bars->empty[s]), smem_u32(&bars->d_full[d]), leader,
-                           i + 1 == PARTS);
-            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < BLOCKS; ++u) {
+              if (kb + u >= kb_last) break;
+              const uint32_t last = u + 1 == BLOCKS || kb + u + 1 == kb_last;
+              block_e4m3<CG>(tmem_u + (d * BLOCKS + u) * S::kN, rows_desc(a + u * p.region * 128), rows_desc(a + (BLOCKS * p.region + (u * PARTS + i) * S::kBRows) * 128), idesc,
+                             smem_u32(&bars->empty[s]), smem_u32(&bars->d_full[d]), leader, last && i + 1 == PARTS, last);
+              __syncwarp();
+            }
             if (++d == NB) {
               d = 0;
               d_phase ^= 1u;
@@ -347,26 +360,31 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
         const float f[4] = {next_x[0] * next_w[0], next_x[1] * next_w[1], next_x[2] * next_w[2], next_x[3] * next_w[3]};
         if (kb + 4 < kb_last) load(kb + 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; i += BLOCKS) {
           if (kb + i >= kb_last) break;
           ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->d_full[d]), d_phase));
           if (!ok) break;
           tc_fence_after();
-          const uint64_t factor = pair_of(f[i], f[i]);
           constexpr int W = A < 64 ? A : 64;
 #pragma unroll
-          for (int c = 0; c < A; c += W) {
-            uint32_t v[W];
-            tmem_ld_some<W>(src + d * S::kN + c, v);
-            if (c + W == A) {   // (all of the buffer has been read)
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) {
-                if (CG == 2) arrive_at_first(smem_u32(&bars->d_empty[d]));
-                else mbar_arrive(smem_u32(&bars->d_empty[d]));
+          for (int u = 0; u < BLOCKS; ++u) {
+            const bool last = u + 1 == BLOCKS || kb + i + u + 1 == kb_last;
+            const uint64_t factor = pair_of(f[i + u], f[i + u]);
+#pragma unroll
+            for (int c = 0; c < A; c += W) {
+              uint32_t v[W];
+              tmem_ld_some<W>(src + (d * BLOCKS + u) * S::kN + c, v);
+              if (last && c + W == A) {   // (all of the buffer has been read)
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                  if (CG == 2) arrive_at_first(smem_u32(&bars->d_empty[d]));
+                  else mbar_arrive(smem_u32(&bars->d_empty[d]));
+                }
               }
+              add_some<W>(acc + c / 2, v, factor);
             }
-            add_some<W>(acc + c / 2, v, factor);
+            if (last) break;
           }
           d += PARTS;
           if (d >= NB) {
@@ -518,14 +536,15 @@ cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p
   CUtensorMap x_map, w_map;
   // (few rows: no more than there are)
   const long long each = c.offsets ? ((long long)c.rows + min(p.E, c.rows) - 1) / min(p.E, c.rows) : c.rows;
-  const int box = each <= 32 ? 32 : each <= 64 ? 64 : ST_ROWS;
+  const auto pieces = [](long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : ST_ROWS; };
+  const int region = pieces(c.rows), box = pieces(each);
   if (!rows_map(&x_map, c.act, p.C, c.rows, c.ld_act, box, true) ||
       !rows_map(&w_map, p.tiles, 128, (long long)p.E * p.n_kt * p.n_kb * 128, 128, S::kBRows, false))
     return cudaErrorInvalidValue;
   const int size = c.out_type == SNN_OUT_F32 ? 4 : 2, staging = split > 1 && ST_ROWS * N * 4 > ST_OUT_WARPS * ST_STAGING ? ST_ROWS * N * 4 : ST_OUT_WARPS * ST_STAGING,
             fixed = S::kFixed + staging + p.E * 12;
   const TallScaledParams q{p.scales, c.scales, c.offsets, c.out, c.ld_scales, c.ld_out, c.rows, p.E, p.C, p.K, p.n_kt, p.n_kb, c.out_type, (p.K + N - 1) / N,
-                           min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::kStage), staging, box, split, p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
+                           min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::stage(region)), S::stage(region), staging, region, box, split, p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
                            c.ld_out * size % 16 == 0 && ((uintptr_t)c.out & 15) == 0, p.status_dev};
   const long long tiles = ((long long)c.rows / (CG * ST_ROWS) + (c.offsets ? min(p.E, c.rows) : 1)) * q.n_ct;
   cudaLaunchAttribute attr[2];
@@ -540,7 +559,7 @@ cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p
   cfg.numAttrs = 2;
   cfg.gridDim = dim3((unsigned)(CG * split * min(tiles, (long long)max(1, sm_count() / (CG * split)))));
   cfg.blockDim = dim3(ST_THREADS);
-  cfg.dynamicSmemBytes = (size_t)(fixed + q.stages * S::kStage);
+  cfg.dynamicSmemBytes = (size_t)(fixed + q.stages * q.stage);
   *launched += 1;
   return cudaLaunchKernelEx(&cfg, kernel, q, x_map, w_map);
 }
