@@ -164,7 +164,7 @@ struct ScaledCall {
   cudaStream_t stream;
 };
 cudaError_t scaled_forward(const Scaled& p, const ScaledCall& c, int* launched);
-// (snn_scaled_tall.cu: many rows; output channels of a tile, 64, 128 or 256, and CTAs that share its input channels, 1 to 8, where each has one tile at most)
+// (snn_scaled_tall.cu: many rows; output channels of a tile, 64, 128 or 256, and CTAs that share a tile of 64: 1, 2 or 4, where each has one tile at most)
 cudaError_t scaled_tall(const Scaled& p, const ScaledCall& c, int shape, int split, int* launched);
 
 }  // namespace snn

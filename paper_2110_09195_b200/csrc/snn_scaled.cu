@@ -225,14 +225,15 @@ cudaError_t few_launch(const Scaled& p, const ScaledCall& c, int* launched) {
 }
 
 // Which kernel, by the time that each would take (us), where the experts have equal numbers of rows.  Few rows: the weights' bytes, once for each 8, 16 or 32 rows, or what a
-// CTA's turns take; many rows: each block of 128 input channels takes a tile's CTA 0.22 us (a pair's 0.5: 256 rows and channels), a launch 3.5, a join of two or four CTAs 1.6
-// to 2.2; or the weights' bytes.  On 212 calls (dense 256 x 256 to 4096 x 8192 and 8192 x 1024 with 1 to 2048 rows, 8 to 64 experts with 1 to 512 rows each) the
-// kernel taken was 2.9 % slower than the best (geometric mean), 1.4 times at worst (1024 rows of 2048 x 512: 9.9 us by four CTAs a tile, 7.2 by one).  Both sides: one row of
-// 4096 x 4096 5.1 (few rows) and 8.9 us, 16 rows 7.2 and 9.0, 24 rows 11.5 and 9.0; 64 experts of 2048 x 2048, 4 rows each 67 and 48; 48 rows of 8192 x 1024
-// 8.6 by four CTAs a tile and 17 by one; 2048 rows of 4096 x 4096 38.4 by pairs and 39.7 by tiles of 128 channels.
-// SNN_FORCE_ROWS=few, many, or 64, 128 or 256 (with /2 or /4 behind the first two: CTAs that share a tile) in the environment takes that wherever it can run.
+// CTA's turns take; many rows: each block of 128 input channels takes a tile's CTA 0.15 to 0.28 us (a pair's 0.42 to 0.55: 256 rows and channels), a launch 4, a join of two
+// or four CTAs 1.8; or the weights' bytes.  On 214 calls (dense 256 x 256 to 4096 x 8192 and 8192 x 1024 with 1 to 8192 rows, 8 to 64 experts with 1 to 512 rows each) the
+// kernel taken was 1.0 % slower than the best (geometric mean), 1.26 times at worst (16 experts of 1104 x 1003, 512 rows each: 29.9 us by tiles of 128 channels, 23.8 by
+// 64).  Both sides: one row of 4096 x 4096 5.1 (few rows) and 8.7 us, 16 rows 7.2 and 8.7, 24 rows 11.5 and 8.7; 64 experts of 2048 x 2048, 4 rows each 104 and 50;
+// 24 rows of 8192 x 1024 8.0 by four CTAs a tile and 13.3 by one; 192 rows of 4096 x 8192 15.6 by tiles of 64 channels and 12.1 by 128; 4096 rows 137 by tiles of 128
+// channels and 126 by pairs.
+// SNN_FORCE_ROWS=few, many, 64 (with /2 or /4 behind it: CTAs that share a tile), 128 or 256 in the environment takes that wherever it can run.
 struct Way {
-  int tile, split;   // output channels of a tile, 0: few rows, and CTAs that share it, or eights of rows of a piece
+  int tile, split;   // output channels of a tile, and CTAs that share one of 64; or 0: few rows, and eights of rows of a piece
 };
 Way choose_way(const Scaled& p, const ScaledCall& c) {
   const auto up = [](double a, double b) { return ceil(a / b); };
@@ -240,21 +241,21 @@ Way choose_way(const Scaled& p, const ScaledCall& c) {
   const long long row_tiles = c.offsets ? c.rows / 128 + (long long)min(p.E, c.rows) : (c.rows + 127ll) / 128;   // at most
   const int nt = each <= 8 ? 1 : each <= 16 ? 2 : 4;
   const char* const force = getenv("SNN_FORCE_ROWS");
-  const auto can_share = [&](int tile, int split) { return row_tiles * ((p.K + tile - 1) / tile) * split <= (long long)sms && p.n_kb >= 2 * split; };
+  const auto can_share = [&](int split) { return row_tiles * ((p.K + 63) / 64) * split <= (long long)sms && p.n_kb >= 2 * split; };
   if (force) {
     if (!strcmp(force, "few")) return {0, nt};
     for (int tile = 64; tile <= 256; tile *= 2) {
       char* end;
       if (strtol(force, &end, 10) != tile) continue;
-      int split = *end == '/' && tile < 256 ? atoi(end + 1) : 1;
-      while (split > 1 && (split > 4 || !can_share(tile, split))) split /= 2;
+      int split = *end == '/' && tile == 64 ? atoi(end + 1) : 1;
+      while (split > 1 && (split != 2 && split != 4 || !can_share(split))) split /= 2;
       return {tile, max(split, 1)};
     }
   }
   const double turns = up(up(each, 8 * nt) * used * up(p.K, 16), 2 * sms);
   Way best{0, nt};
-  double least = 1.5 + (nt == 4 ? 1.0 : 0.0) + 0.5 * turns +
-                 fmax(mb * (nt == 1 ? 0.2 : nt == 2 ? 0.29 : 0.55) * up(nk, 8) * 8 / fmax(nk, 8) * up(each, 8 * nt), turns * up(nk, 8) * (nt == 1 ? 0.5 : nt == 2 ? 0.8 : 1.5));
+  double least = 1.6 + (nt == 4 ? 1.45 : 0.0) + 0.34 * turns +
+                 fmax(mb * (nt == 1 ? 0.245 : nt == 2 ? 0.37 : 0.67) * up(nk, 8) * 8 / fmax(nk, 8) * up(each, 8 * nt), turns * up(nk, 8) * (nt == 1 ? 0.46 : nt == 2 ? 0.81 : 1.24));
   if (force && !strcmp(force, "many")) least = 1e30;
   const auto offer = [&](int tile, int split, double time) {
     if (time < least) {
@@ -262,14 +263,14 @@ Way choose_way(const Scaled& p, const ScaledCall& c) {
       best = Way{tile, split};
     }
   };
-  for (int tile = 64; tile <= 128; tile *= 2)
-    for (int split = 1; split <= 4; split *= 2) {
-      if (split > 1 && !can_share(tile, split)) break;
-      const double n = used * up(each, 128) * up(p.K, tile) * split, around = up(n, sms), block = tile == 64 ? (around > 1 ? 0.235 : 0.215) : around > 1 ? 0.29 : 0.225;
-      offer(tile, split, fmax(3.5 + (up(nk, split) * block + 0.15) * around + (split == 1 ? 0.0 : tile == 64 ? 1.6 : 2.2), 2.5 + mb / (tile == 64 ? 4.5 : 6.0)));
-    }
-  const double around = up(used * up(each, 256) * up(p.K, 256), fmax(1.0, floor(sms / 2)));
-  offer(256, 1, fmax(3.5 + around * (nk * (around > 1 ? 0.53 : 0.47) + 0.3), 3.5 + mb / 4));
+  for (int split = 1; split <= 4 && (split == 1 || can_share(split)); split *= 2) {
+    const double around = up(used * up(each, 128) * up(p.K, 64) * split, sms);
+    offer(64, split, fmax(3.75 + around * (up(nk, split) * (around > 1 ? 0.21 : 0.147) + 0.39) + (split > 1 ? 1.85 : 0.0), 3.6 + mb / 4.8));
+  }
+  double around = up(used * up(each, 128) * up(p.K, 128), sms);
+  offer(128, 1, fmax(3.75 + around * (nk * (around > 1 ? 0.28 : c.rows <= 64 ? 0.21 : 0.25) + 0.27), 3.6 + mb / 5.3));
+  around = up(used * up(each, 256) * up(p.K, 256), fmax(1.0, floor(sms / 2)));
+  offer(256, 1, fmax(4.2 + around * (nk * (around > 1 ? 0.545 : 0.42) + 0.74), 4.2 + mb / 2.9));
   return best;
 }
 

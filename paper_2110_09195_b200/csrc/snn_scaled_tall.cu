@@ -11,15 +11,21 @@ namespace {
 // out[row, co] = sum over blocks of 128 input channels of  xs[row, b] ws[co / 128, b] (x w)[row, co, b]:  D[128 or 256 rows x N channels] = x (M operand) * w^T (N
 // operand) for one block at a time, each into a buffer of its own in tensor memory, from where eight warps add it, times its scales, to sums in
 // registers (fp32).  Rows are the M operand so that a thread has one row: one factor for all of its channels of a block.  While they add one block up,
-// the next ones are multiplied: two buffers of 256 columns, or four.  Both operands come by TMA, the weights in the layout that they are kept in.
+// the next ones are multiplied: two to four buffers.  Both operands come by TMA, the weights in the layout that they are kept in.
 //   CG = 2, N = 256: a pair of CTAs (one instruction for both), 128 rows and half of the channels' weights in each.  An SM then reads 64 bytes a cycle of
 //   operands, and as many arrive; alone with 128 x 256 it would be 96 and 96, more than shared memory gives.
-//   CG = 1, N = 128 or 64: fewer rows, more tiles, for problems that would leave SMs without any.
+//   CG = 1, N = 128 or 64: fewer rows, more tiles, for problems that would leave SMs without any; of 64 a tile may be shared by two or four CTAs of a cluster, each a
+//   run of the input channels.  What bounds these is a block's waits, issues and commits: 300 to 400 cycles of one warp, so two warps do that in turns (one row of 4096 x
+//   4096 11.0 and 10.7 us), and of narrow stages two blocks go together (8.7).
+// 4096 rows of 4096 x 8192 take 126 us (2.19 PFLOP/s) in a short run, 155 at the power limit in a long one.
 constexpr int ST_ROWS = 128;          // of a CTA's tile
 constexpr int ST_MAX_STAGES = 16;
 constexpr int ST_OUT_WARPS = 8;
 constexpr int ST_STAGING = 4096;      // of a warp: 32 rows of 128 bytes
-// warps: 0 copies, 1 MMA, 2 tensor memory, 4-11 sums and outputs
+// Scales: of four blocks at a time, of a tile's rows and of its two halves' channels; a warp brings them.  (Each four cost an L2 latency; where the warps of the sums
+// waited for it themselves, that was 22 of 131 us on 4096 rows of 4096 x 8192.)
+constexpr int ST_SCALES = 4, ST_SCALE_BYTES = ST_ROWS * 16 + 32;
+// warps: 0 copies, 1 and 2 MMA (in turns: one takes 350 cycles for a block's waits, instructions and commits), 2 tensor memory, 3 scales, 4-11 sums and outputs
 
 struct TallScaledParams {
   const float *w_scales, *x_scales;
@@ -30,24 +36,23 @@ struct TallScaledParams {
   int* status;
 };
 struct TallScaledBars {
-  uint64_t full[ST_MAX_STAGES], empty[ST_MAX_STAGES], d_full[4], d_empty[4], drain;
+  uint64_t full[ST_MAX_STAGES], empty[ST_MAX_STAGES], d_full[4], d_empty[4], scales_full[ST_SCALES], scales_empty[ST_SCALES], drain[2];
   uint32_t tmem;
 };
-template <int CG, int N>
+template <int CG, int N, int BLOCKS>   // BLOCKS go through the stages and buffers together
 struct TallScaledShape {
   static constexpr int kParts = CG;                                // instructions of N / CG channels for a block, each with buffers of its own
-  static constexpr int kBlocks = 3 - CG;                           // blocks that go through the stages and buffers together
   static constexpr int kN = N / kParts, kBRows = kN / CG;          // channels of an instruction, and rows of the weights that each CTA has of them
   // A block's rows (a region of as many as a tile can have: the instruction reads 128, and what it makes of those behind them, other operands or outputs of before, is nobody's),
   // and its weights
-  static int stage(int region) { return kBlocks * (region * 128 + kParts * kBRows * 128); }
-  static constexpr int kBuffers = N == 128 ? 2 : 4, kColumns = 512;   // of tensor memory
+  static int stage(int region) { return BLOCKS * (region * 128 + kParts * kBRows * 128); }
+  static constexpr int kBuffers = BLOCKS == 2 ? 2 : 4, kColumns = kN * BLOCKS * kBuffers;   // of tensor memory
   static constexpr int kWarps = ST_OUT_WARPS / kParts;             // that read a buffer, in each CTA
-  static constexpr int kFixed = 1024 + (int)sizeof(TallScaledBars);
+  static constexpr int kFixed = 1024 + ST_SCALES * ST_SCALE_BYTES + (int)sizeof(TallScaledBars);
 };
 
-// Issued by the lanes for which `on` is not 0: D = A * B^T over 128 input channels in four steps of 32, then the commits: the stage is free, the buffer is full.
-// (the former if `frees`, the latter if `fills`)
+// Issued by the lanes for which `on` is not 0: D = A * B^T over 128 input channels in four steps of 32, then the commits: the stage is free (if `frees`), the buffer is
+// full (if `fills`).
 template <int CG>
 __device__ __forceinline__ void block_e4m3(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t bar0, uint32_t bar1, uint32_t on, uint32_t frees, uint32_t fills);
 template <>
@@ -177,14 +182,15 @@ __device__ __forceinline__ bool scaled_tile(const ScaledRanges& R, int E, int n_
   return true;
 }
 
-template <int CG, int N>
+template <int CG, int N, int BLOCKS>
 __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, const CUtensorMap& x_map, const CUtensorMap& w_map) {
-  using S = TallScaledShape<CG, N>;
-  constexpr int NB = S::kBuffers, PARTS = S::kParts, BLOCKS = S::kBlocks;
+  using S = TallScaledShape<CG, N, BLOCKS>;
+  constexpr int NB = S::kBuffers, PARTS = S::kParts;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* const staging = smem + p.stages * p.stage;   // of the outputs, or what is received of the sums
-  TallScaledBars* const bars = reinterpret_cast<TallScaledBars*>(staging + p.staging);
+  const uint32_t scales = smem_u32(staging) + p.staging;
+  TallScaledBars* const bars = reinterpret_cast<TallScaledBars*>(staging + p.staging + ST_SCALES * ST_SCALE_BYTES);
   ScaledRanges R;
   R.lo = reinterpret_cast<int*>(bars + 1);
   R.n = R.lo + p.E;
@@ -221,7 +227,12 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
       mbar_init(smem_u32(&bars->d_full[i]), 1);
       mbar_init(smem_u32(&bars->d_empty[i]), CG * S::kWarps);
     }
-    mbar_init(smem_u32(&bars->drain), 1);
+    for (int i = 0; i < ST_SCALES; ++i) {
+      mbar_init(smem_u32(&bars->scales_full[i]), 1);
+      mbar_init(smem_u32(&bars->scales_empty[i]), ST_OUT_WARPS);
+    }
+    mbar_init(smem_u32(&bars->drain[0]), 1);
+    mbar_init(smem_u32(&bars->drain[1]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_proxy_async();
   } else if (warp == 2) {
@@ -238,19 +249,19 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
   if (warp > 2 || warp == 1) grid_dep_wait();
   tc_fence_before();
   __syncthreads();
-  if (CG == 2 || p.split > 1) pair_sync();
+  if (CG == 2 || (N == 64 && p.split > 1)) pair_sync();
   tc_fence_after();
   grid_dep_launch();   // (only now: a dependent that has tensor memory before this CTA does would wait for it for good)
   const uint32_t tmem = bars->tmem;
   // blocks of input channels: all, or this CTA's share of them
-  const int nk = p.n_kb, part = CG == 1 ? (int)blockIdx.x % p.split : 0, kb_first = nk * part / p.split, kb_last = nk * (part + 1) / p.split;
+  const int nk = p.n_kb, part = N == 64 ? (int)blockIdx.x % p.split : 0, kb_first = nk * part / p.split, kb_last = nk * (part + 1) / p.split;
   bool ok = true;
   ScaledTile t{};
 
   if (warp < 4) {
     if (N == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0) {
-      // ------------------------------------------------------------ copies: a stage is 128 input channels of the rows and of the weights
+      // ------------------------------------------------------------ copies: a stage is BLOCKS times 128 input channels of the rows and of the weights
       int s = 0, filled = 0;
       uint32_t phase = 0;
       const bool leader = elect_one();
@@ -294,44 +305,83 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
         ok = mbar_wait(smem_u32(&bars->full[s]), phase) && ok;
       }
       if (!ok && lane == 0) raise_status(p.status, 31);
-    } else if (warp == 1 && rank == 0) {
-      // ------------------------------------------------------------ MMA, for both CTAs
-      int s = 0, d = 0;
+    } else if (warp == 3) {
+      // ------------------------------------------------------------ scales
+      int s = 0;
+      uint32_t phase = 0;
+      for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
+        const float* const ws = p.w_scales + (size_t)t.e * p.n_kt * nk;
+        for (int kb = kb_first; kb < kb_last; kb += 4) {
+          const int whole = p.fours && kb % 4 == 0 && kb + 4 <= kb_last;
+          float v[4][4] = {}, w[4] = {};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int row = min(rank * ST_ROWS + 32 * i + lane, t.n - 1);
+            ld_four(p.x_scales + (size_t)(t.r0 + row) * (size_t)p.ld_scales + kb, kb_last - kb, whole, v[i]);
+          }
+          if (lane < 2) ld_four(ws + (size_t)min((t.ct * N + lane * (N / 2)) >> 7, p.n_kt - 1) * nk + kb, kb_last - kb, whole, w);
+          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->scales_empty[s]), phase ^ 1u));
+          if (!ok) break;
+          const uint32_t to = scales + s * ST_SCALE_BYTES;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sts16(to + (32 * i + lane) * 16, make_uint4(__float_as_uint(v[i][0]), __float_as_uint(v[i][1]), __float_as_uint(v[i][2]), __float_as_uint(v[i][3])));
+          if (lane < 2) sts16(to + ST_ROWS * 16 + lane * 16, make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3])));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&bars->scales_full[s]));
+          if (++s == ST_SCALES) {
+            s = 0;
+            phase ^= 1u;
+          }
+        }
+      }
+      if (!ok && lane == 0) raise_status(p.status, 34);
+    } else if (rank == 0) {
+      // ------------------------------------------------------------ MMA, for both CTAs: every second stage
+      const int turn = warp - 1;
+      int s = turn, d = turn * PARTS, mine = turn;   // (the next of this warp's in the tile)
       uint32_t phase = 0, d_phase = 0;
       const uint32_t leader = elect_one(), tmem_u = (uint32_t)uni((int)tmem);
       const uint32_t idesc = (1u << 4) | ((uint32_t)(S::kN >> 3) << 17) | ((uint32_t)(CG * ST_ROWS >> 4) << 24);   // fp32 sums of e4m3 values
+      const int units = (kb_last - kb_first + BLOCKS - 1) / BLOCKS;
       for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
-        for (int kb = kb_first; kb < kb_last; kb += BLOCKS) {
-          ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->full[s]), phase));
+        int unit = mine;
+        for (; unit < units; unit += 2) {
+          const int kb = kb_first + unit * BLOCKS;
           const uint32_t a = base + s * p.stage;
 #pragma unroll
           for (int i = 0; i < PARTS; ++i) {
-            ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(&bars->d_empty[d]), d_phase ^ 1u));
+            // First the buffer: what was in it has been added up, and all before it, the stage's last contents among them (there are no fewer stages than buffers).  The
+            // stage's barrier is then in the phase before or past it, whichever warp has waited for it in between; parities tell no more apart.
+            ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(&bars->d_empty[d + i]), d_phase ^ 1u));
+            if (i == 0) ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(&bars->full[s]), phase));
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
             for (int u = 0; u < BLOCKS; ++u) {
               if (kb + u >= kb_last) break;
               const uint32_t last = u + 1 == BLOCKS || kb + u + 1 == kb_last;
-              block_e4m3<CG>(tmem_u + (d * BLOCKS + u) * S::kN, rows_desc(a + u * p.region * 128), rows_desc(a + (BLOCKS * p.region + (u * PARTS + i) * S::kBRows) * 128), idesc,
-                             smem_u32(&bars->empty[s]), smem_u32(&bars->d_full[d]), leader, last && i + 1 == PARTS, last);
+              block_e4m3<CG>(tmem_u + ((d + i) * BLOCKS + u) * S::kN, rows_desc(a + u * p.region * 128), rows_desc(a + (BLOCKS * p.region + (u * PARTS + i) * S::kBRows) * 128), idesc,
+                             smem_u32(&bars->empty[s]), smem_u32(&bars->d_full[d + i]), leader, last && i + 1 == PARTS, last);
               __syncwarp();
-            }
-            if (++d == NB) {
-              d = 0;
-              d_phase ^= 1u;
             }
           }
           if (!ok) break;
-          if (++s == p.stages) {
-            s = 0;
+          s += 2;
+          if (s >= p.stages) {
+            s -= p.stages;
             phase ^= 1u;
           }
+          d += 2 * PARTS;
+          if (d >= NB) {
+            d -= NB;
+            d_phase ^= 1u;
+          }
         }
+        mine = unit - units;
       }
-      commit_drain<CG>(smem_u32(&bars->drain), leader);
+      commit_drain<CG>(smem_u32(&bars->drain[turn]), leader);
       __syncwarp();
-      ok = mbar_wait(smem_u32(&bars->drain), 0) && ok;
+      ok = mbar_wait(smem_u32(&bars->drain[turn]), 0) && ok;
       if (!ok && lane == 0) raise_status(p.status, 32);
     }
   } else {
@@ -340,25 +390,26 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
     constexpr int A = N / 2;
     const int quarter = warp & 3, half = (warp - 4) >> 2, row = quarter * 32 + lane;
     const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + (PARTS == 1 ? half * A : 0), stage = smem_u32(staging) + (warp - 4) * ST_STAGING;
-    int d = PARTS == 2 ? half : 0;
-    uint32_t d_phase = 0;
+    int d = PARTS == 2 ? half : 0, g = 0;
+    uint32_t d_phase = 0, g_phase = 0;
     for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
       const int n = t.n - rank * ST_ROWS, co0 = t.ct * N + half * A;   // rows of this CTA's (0 or less: none), first channel
-      const float* const xs = p.x_scales + (size_t)(t.r0 + min(rank * ST_ROWS + row, t.n - 1)) * (size_t)p.ld_scales;
-      const float* const ws = p.w_scales + ((size_t)t.e * p.n_kt + min(co0 >> 7, p.n_kt - 1)) * nk;
-      // Four blocks' scales on their way while four blocks are added up.  (They are multiplied where they are used: at the loads the warp would wait for them.)
-      float next_x[4] = {}, next_w[4] = {};
-      auto load = [&](int kb) {
-        ld_four(xs + kb, kb_last - kb, p.fours && kb + 4 <= kb_last, next_x);
-        ld_four(ws + kb, kb_last - kb, p.fours && kb + 4 <= kb_last, next_w);
-      };
-      load(kb_first);
       uint64_t acc[A / 2];
 #pragma unroll
       for (int i = 0; i < A / 2; ++i) acc[i] = 0;
       for (int kb = kb_first; ok && kb < kb_last; kb += 4) {
-        const float f[4] = {next_x[0] * next_w[0], next_x[1] * next_w[1], next_x[2] * next_w[2], next_x[3] * next_w[3]};
-        if (kb + 4 < kb_last) load(kb + 4);
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->scales_full[g]), g_phase));
+        if (!ok) break;
+        const uint32_t from = scales + g * ST_SCALE_BYTES;
+        const uint4 xs = lds16_at(from + row * 16), ws = lds16_at(from + ST_ROWS * 16 + half * 16);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&bars->scales_empty[g]));
+        if (++g == ST_SCALES) {
+          g = 0;
+          g_phase ^= 1u;
+        }
+        const float f[4] = {__uint_as_float(xs.x) * __uint_as_float(ws.x), __uint_as_float(xs.y) * __uint_as_float(ws.y), __uint_as_float(xs.z) * __uint_as_float(ws.z),
+                            __uint_as_float(xs.w) * __uint_as_float(ws.w)};
 #pragma unroll
         for (int i = 0; i < 4; i += BLOCKS) {
           if (kb + i >= kb_last) break;
@@ -394,7 +445,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
         }
       }
       if (!ok) break;
-      if (CG == 1 && p.split > 1) {
+      if (N == 64 && p.split > 1) {
         // This CTA's share of the sums goes to the CTAs that have the channels: [CTA from][fours of channels][row], 16 bytes each.
         const int fours = N / 4 / p.split;
 #pragma unroll
@@ -473,10 +524,13 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 2) mbar_wait(smem_u32(&bars->drain), 0);   // (the last arrival here from the pair's MMAs)
+  if (warp == 2) {   // (the last arrivals here from the pair's MMAs)
+    mbar_wait(smem_u32(&bars->drain[0]), 0);
+    mbar_wait(smem_u32(&bars->drain[1]), 0);
+  }
   __syncwarp();
   if (CG == 2) pair_sync();
-  if (CG == 1 && p.split > 1) {
+  if (N == 64 && p.split > 1) {
     pair_sync();
     // the sums over the CTAs in their order; a thread has a row and every second four of this CTA's channels
     t = ScaledTile{};
@@ -513,11 +567,11 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
 constexpr int ST_THREADS = 128 + 32 * ST_OUT_WARPS;
 __global__ void __launch_bounds__(ST_THREADS, 1)
     scaled_pair_kernel(const TallScaledParams p, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map) {
-  scaled_tall_body<2, 256>(p, x_map, w_map);
+  scaled_tall_body<2, 256, 1>(p, x_map, w_map);
 }
-template <int N>
+template <int N, int BLOCKS>
 __global__ void __launch_bounds__(ST_THREADS, 1) scaled_single_kernel(const TallScaledParams p, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap w_map) {
-  scaled_tall_body<1, N>(p, x_map, w_map);
+  scaled_tall_body<1, N, BLOCKS>(p, x_map, w_map);
 }
 
 bool rows_map(CUtensorMap* map, const void* base, long long columns, long long rows, long long ld, int box_rows, bool swizzled) {
@@ -528,9 +582,9 @@ bool rows_map(CUtensorMap* map, const void* base, long long columns, long long r
                           swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int CG, int N, class Kernel>
+template <int CG, int N, int BLOCKS, class Kernel>
 cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p, const ScaledCall& c, int split, int* launched) {
-  using S = TallScaledShape<CG, N>;
+  using S = TallScaledShape<CG, N, BLOCKS>;
   cudaError_t e = allow_max_smem(kernel, done);
   if (e != cudaSuccess) return e;
   CUtensorMap x_map, w_map;
@@ -541,11 +595,13 @@ cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p
   if (!rows_map(&x_map, c.act, p.C, c.rows, c.ld_act, box, true) ||
       !rows_map(&w_map, p.tiles, 128, (long long)p.E * p.n_kt * p.n_kb * 128, 128, S::kBRows, false))
     return cudaErrorInvalidValue;
-  const int size = c.out_type == SNN_OUT_F32 ? 4 : 2, staging = split > 1 && ST_ROWS * N * 4 > ST_OUT_WARPS * ST_STAGING ? ST_ROWS * N * 4 : ST_OUT_WARPS * ST_STAGING,
+  static_assert(N != 64 || ST_ROWS * N * 4 <= ST_OUT_WARPS * ST_STAGING, "what is received of the sums fits the staging");
+  const int size = c.out_type == SNN_OUT_F32 ? 4 : 2, staging = ST_OUT_WARPS * ST_STAGING,
             fixed = S::kFixed + staging + p.E * 12;
   const TallScaledParams q{p.scales, c.scales, c.offsets, c.out, c.ld_scales, c.ld_out, c.rows, p.E, p.C, p.K, p.n_kt, p.n_kb, c.out_type, (p.K + N - 1) / N,
                            min(ST_MAX_STAGES, (kMaxDynSmem - fixed) / S::stage(region)), S::stage(region), staging, region, box, split, p.n_kb % 4 == 0 && c.ld_scales % 4 == 0 && ((uintptr_t)c.scales & 15) == 0,
                            c.ld_out * size % 16 == 0 && ((uintptr_t)c.out & 15) == 0, p.status_dev};
+  if (q.stages < S::kBuffers / S::kParts || (split > 1 && N != 64)) return cudaErrorInvalidConfiguration;   // (the warps of the MMAs count on it; the first never happens up to 1024 experts)
   const long long tiles = ((long long)c.rows / (CG * ST_ROWS) + (c.offsets ? min(p.E, c.rows) : 1)) * q.n_ct;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -567,10 +623,12 @@ cudaError_t tall_launch(Kernel kernel, unsigned long long* done, const Scaled& p
 }  // namespace
 
 cudaError_t scaled_tall(const Scaled& p, const ScaledCall& c, int shape, int split, int* launched) {
-  static unsigned long long done[3] = {0, 0, 0};
-  if (shape == 256) return tall_launch<2, 256>(scaled_pair_kernel, done, p, c, 1, launched);
-  if (shape == 128) return tall_launch<1, 128>(scaled_single_kernel<128>, done + 1, p, c, split, launched);
-  return tall_launch<1, 64>(scaled_single_kernel<64>, done + 2, p, c, split, launched);
+  static unsigned long long done[4] = {0, 0, 0, 0};
+  if (shape == 256) return tall_launch<2, 256, 1>(scaled_pair_kernel, done, p, c, 1, launched);
+  if (shape == 64) return tall_launch<1, 64, 2>(scaled_single_kernel<64, 2>, done + 1, p, c, split, launched);
+  // Two blocks at a time save waits, but of more than 64 rows they leave two stages only (a row of 4096 x 4096 9.6 and 11.0 us, 4096 rows of 4096 x 8192 149 and 139).
+  if (c.rows <= 64) return tall_launch<1, 128, 2>(scaled_single_kernel<128, 2>, done + 2, p, c, split, launched);
+  return tall_launch<1, 128, 1>(scaled_single_kernel<128, 1>, done + 3, p, c, split, launched);
 }
 
 }  // namespace snn
