@@ -338,14 +338,13 @@ struct DownParams {
   Powers pow;
 };
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {
+__device__ __forceinline__ void st_cluster(uint32_t addr, int rank, float v) {
   uint32_t there;
-  float v;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
-  return v;
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
 }
-__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ int4 ld_piece(const int4* p) {
   const uint4 v = ld16(p);
   return make_int4((int)v.x, (int)v.y, (int)v.z, (int)v.w);
@@ -353,24 +352,36 @@ __device__ __forceinline__ int4 ld_piece(const int4* p) {
 
 // Second launch.  A cluster has 32 output channels; its warps share out all pieces of all experts, 256 input channels at a time, evenly: a run of them
 // each.  The outputs are linear in what the pieces give, so a warp adds its run's products, times the scale and the row's share, to a table of its own [tokens][channels],
-// and the tables are added up at the end, warp by warp, CTA by CTA (through distributed shared memory).  No atomics, no partial sums in memory, and
+// and the tables are added up at the end, warp by warp, then CTA by CTA: each CTA sends every other one the outputs that that one writes (one barrier; read from there they took
+// two, and 5 tokens with 3 of 60 experts of 1000 -> 1003 17.4 us instead of 16.3).  No atomics, no partial sums in memory, and
 // no waiting until then.  Sums of three parts (fp32 outputs) begin anew every 256 channels: the matrix instructions cut what they add.
-constexpr int MO_LD = MO_M + 1;
+// What bounds it, and the first launch, is the expansion and the warp's matrix instruction behind it, which share their issue port: 17.5 cycles for 256 weights and 8 rows in one
+// part, 26 in two; 64 tokens with 4 of 64 experts (2048 -> 1024 -> 2048) 20 us each.  The same on the 5th-generation tensor cores (weights expanded into tensor memory, 128 channels a
+// CTA, clusters of four to eight) took 0.5 us for 128 x 256 weights and came out even: 60.3 and 59.3 us for those 64 tokens, 18.5 and 18.3 for one (2 of 8, 4096): not kept.
+constexpr int MO_LD = MO_M + 1, MO_TABLES = 9;
 template <int PARTS>
 __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   constexpr int LD = MO_LD, RING = PARTS == 3 ? 2 : 4;
-  extern __shared__ float sums[];   // [8][tokens][LD], then the pieces
+  extern __shared__ int4 pieces[];
+  int* const tokens = reinterpret_cast<int*>(pieces + p.choices);   // of the rows
+  float* const shares = reinterpret_cast<float*>(tokens + p.choices);
+  float* const sums = shares + p.choices;   // [8 warps][tokens][LD], then what the cluster's CTAs send (no more than one table: its sizes divide 32)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int strip = (int)blockIdx.x / p.cluster, rank = (int)blockIdx.x % p.cluster, table = p.tokens * LD;
   float* const mine = sums + warp * table;
   for (int i = lane; i < table; i += 32) mine[i] = 0.f;
   __syncwarp();
+  if (p.cluster > 1) cluster_arrive();
   const Powers pow = in_registers(p.pow);
   grid_dep_wait();
   grid_dep_launch();
+  // All at once, and more than there may be: one latency.
   const int total = ld_int(p.total);
-  int4* const pieces = reinterpret_cast<int4*>(sums + 8 * table);
-  for (int i = threadIdx.x; i < total; i += 256) pieces[i] = ld_piece(p.pieces + i);
+  for (int i = threadIdx.x; i < p.choices; i += 256) {
+    pieces[i] = ld_piece(p.pieces + i);
+    tokens[i] = ld_int(p.rows + i);
+    shares[i] = ld_number(p.shares + i);
+  }
   __syncthreads();
   const long long units = (long long)total * p.n_kb;
   const int w = rank * 8 + warp, warps = p.cluster * 8;
@@ -417,8 +428,8 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
       for (int q = 0; q < 4; ++q) alpha[q] = ld_number(p.alpha + (size_t)now.e * p.n_mt * 16 + strip * MO_M + g + 8 * q);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        share[q] = 2 * t + q < now.n ? ld_number(p.shares + now.r0 + 2 * t + q) : 0.f;
-        token[q] = 2 * t + q < now.n ? ld_int(p.rows + now.r0 + 2 * t + q) : 0;
+        share[q] = 2 * t + q < now.n ? shares[now.r0 + 2 * t + q] : 0.f;
+        token[q] = 2 * t + q < now.n ? tokens[now.r0 + 2 * t + q] : 0;
       }
     }
     bits = more;
@@ -465,21 +476,29 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
     now = then;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < table; i += 256) {
+  // A CTA adds its warps' tables up and sends every CTA of the cluster its share of the outputs, [CTA from][the share's place]; each then adds up what it has received.
+  const int outputs = p.tokens * MO_M, most = (outputs + p.cluster - 1) / p.cluster;
+  float* const received = sums + 8 * table;
+  if (p.cluster > 1) cluster_wait();   // (they have all begun)
+  for (int i = threadIdx.x; i < outputs; i += 256) {
+    const float* const from = sums + i / MO_M * LD + i % MO_M;
     float s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) s += sums[k * table + i];
-    sums[i] = s;   // (read by this thread alone before)
+    for (int k = 0; k < 8; ++k) s += from[k * table];
+    const int to = i / most;
+    if (p.cluster > 1) st_cluster(smem_u32(received + rank * most + i - to * most), to, s);
+    else received[i] = s;
   }
-  if (p.cluster > 1) cluster_sync();
-  else __syncthreads();
-  for (int i = rank * 256 + (int)threadIdx.x; i < p.tokens * MO_M; i += p.cluster * 256) {
-    const int token = i / MO_M, ch = i % MO_M, co = strip * MO_M + ch;
+  if (p.cluster > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  for (int i = rank * most + (int)threadIdx.x; i < min(outputs, (rank + 1) * most); i += 256) {   // (in a cluster of one: what this thread has left there)
+    const int token = i / MO_M, co = strip * MO_M + i % MO_M;
     float s = 0.f;
-    for (int k = 0; k < p.cluster; ++k) s += p.cluster > 1 ? ld_cluster(smem_u32(sums + token * LD + ch), k) : sums[token * LD + ch];
+    for (int k = 0; k < p.cluster; ++k) s += received[k * most + i - rank * most];
     if (co < p.K) store_out(p.out, p.out_type, token * p.ld_out + co, s);
   }
-  if (p.cluster > 1) cluster_sync();   // (nobody ends while its table is read)
 }
 
 template <int PARTS>
@@ -499,7 +518,7 @@ cudaError_t down_launch(const DownParams& p, unsigned strips, cudaStream_t s) {
   cfg.numAttrs = 2;
   cfg.gridDim = dim3(strips * (unsigned)p.cluster);
   cfg.blockDim = dim3(256);
-  cfg.dynamicSmemBytes = (size_t)8 * p.tokens * MO_LD * 4 + (size_t)p.choices * 16;
+  cfg.dynamicSmemBytes = (size_t)MO_TABLES * p.tokens * MO_LD * 4 + (size_t)p.choices * 24;
   return cudaLaunchKernelEx(&cfg, moe_down_kernel<PARTS>, p);
 }
 
