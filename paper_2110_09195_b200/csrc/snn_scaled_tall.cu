@@ -149,10 +149,19 @@ __device__ __forceinline__ void tmem_ld_some<64>(uint32_t taddr, uint32_t (&v)[6
       : "r"(taddr)
       : "memory");
 }
-template <int W>
-__device__ __forceinline__ void add_some(uint64_t* acc, const uint32_t (&v)[W], uint64_t f) {
+// Two at a time, or one: of 128 sums a thread the former move registers about (4096 rows of 4096 x 8192 126 us and, one at a time, 112), of 64 and 32 the latter are slower
+// (147 and 137, 192 and 183 us).
+template <int W, bool TWO>
+__device__ __forceinline__ void add_some(float* acc, const uint32_t (&v)[W], float f) {
+  if (TWO) {
+    const uint64_t g = pair_of(f, f);
 #pragma unroll
-  for (int i = 0; i < W / 2; ++i) asm("{\n\t.reg .b64 t;\n\tmov.b64 t, {%1, %2};\n\tfma.rn.f32x2 %0, t, %3, %0;\n\t}" : "+l"(acc[i]) : "r"(v[2 * i]), "r"(v[2 * i + 1]), "l"(f));
+    for (int i = 0; i < W; i += 2)
+      asm("{\n\t.reg .b64 t, a;\n\tmov.b64 t, {%2, %3};\n\tmov.b64 a, {%0, %1};\n\tfma.rn.f32x2 a, t, %4, a;\n\tmov.b64 {%0, %1}, a;\n\t}" : "+f"(acc[i]), "+f"(acc[i + 1]) : "r"(v[i]), "r"(v[i + 1]), "l"(g));
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) acc[i] = fmaf(__uint_as_float(v[i]), f, acc[i]);
+  }
 }
 
 // 16 bytes to the shared memory of a CTA of the cluster.
@@ -394,9 +403,9 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
     uint32_t d_phase = 0, g_phase = 0;
     for (int index = first_tile; ok && scaled_tile<CG>(R, p.E, p.n_ct, index, t); index += step) {
       const int n = t.n - rank * ST_ROWS, co0 = t.ct * N + half * A;   // rows of this CTA's (0 or less: none), first channel
-      uint64_t acc[A / 2];
+      float acc[A];
 #pragma unroll
-      for (int i = 0; i < A / 2; ++i) acc[i] = 0;
+      for (int i = 0; i < A; ++i) acc[i] = 0.f;
       for (int kb = kb_first; ok && kb < kb_last; kb += 4) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars->scales_full[g]), g_phase));
         if (!ok) break;
@@ -420,7 +429,6 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
 #pragma unroll
           for (int u = 0; u < BLOCKS; ++u) {
             const bool last = u + 1 == BLOCKS || kb + i + u + 1 == kb_last;
-            const uint64_t factor = pair_of(f[i + u], f[i + u]);
 #pragma unroll
             for (int c = 0; c < A; c += W) {
               uint32_t v[W];
@@ -433,7 +441,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
                   else mbar_arrive(smem_u32(&bars->d_empty[d]));
                 }
               }
-              add_some<W>(acc + c / 2, v, factor);
+              add_some<W, A < 128>(acc + c, v, f[i + u]);
             }
             if (last) break;
           }
@@ -450,9 +458,8 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
         const int fours = N / 4 / p.split;
 #pragma unroll
         for (int i = 0; i < A / 4; ++i) {
-          const float2 u = floats_of(acc[2 * i]), v = floats_of(acc[2 * i + 1]);
           const int four = half * (A / 4) + i, to = four / fours;
-          st_shared_of(received + (uint32_t)((part * fours + four - to * fours) * ST_ROWS + row) * 16u, to, make_float4(u.x, u.y, v.x, v.y));
+          st_shared_of(received + (uint32_t)((part * fours + four - to * fours) * ST_ROWS + row) * 16u, to, make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]));
         }
         continue;
       }
@@ -496,8 +503,8 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
 #pragma unroll
           for (int c = 0; c < A; c += 32)
             pass([&](int q) {
-              const float2 a = floats_of(acc[c / 2 + 2 * q]), b = floats_of(acc[c / 2 + 2 * q + 1]);
-              return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+              const float* const a = acc + c + 4 * q;
+              return make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
             }, co0 + c, 4, 8);
         } else if (A >= 64) {
 #pragma unroll
@@ -505,7 +512,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
             pass([&](int q) {
               uint32_t w[4];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, floats_of(acc[c / 2 + 4 * q + j]));
+              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, make_float2(acc[c + 8 * q + 2 * j], acc[c + 8 * q + 2 * j + 1]));
               return make_uint4(w[0], w[1], w[2], w[3]);
             }, co0 + c, 8, PIECES);
         } else {   // (32 channels: half of a pass, the other half is not there)
@@ -513,7 +520,7 @@ __device__ __forceinline__ void scaled_tall_body(const TallScaledParams& p, cons
             uint32_t w[4] = {};
             if (q < 4)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, floats_of(acc[(4 * q + j) % (A / 2)]));
+              for (int j = 0; j < 4; ++j) w[j] = pack_pair(p.out_type, make_float2(acc[(8 * q + 2 * j) % A], acc[(8 * q + 2 * j + 1) % A]));
             return make_uint4(w[0], w[1], w[2], w[3]);
           }, co0, 8, PIECES);
         }
