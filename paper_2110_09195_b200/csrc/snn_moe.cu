@@ -561,16 +561,12 @@ cudaError_t moe_forward(const MoeCall& c, int* launched) {
   u.pow = powers();
   // Pieces that the choices make at most: each expert of theirs has one that is not full.
   const long long ctas = 2ll * sm_count(), pieces = ((long long)choices + (long long)min(E, choices) * (MO_N - 1)) / MO_N, items = pieces * ((up.K + MO_M - 1) / MO_M);
-  // Warps of a team, by what its longest run takes: blocks of input channels, and for each item about half of one around them.
-  double best = 0;
-  for (int k = 1; k <= min(8, up.n_kb); k *= 2) {   // (every warp has input channels)
-    const long long teams = min(ctas * (8 / k), (items + 8 / k - 1) / (8 / k) * (8 / k)), runs = (items + teams - 1) / teams;
-    const double time = runs * ((up.n_kb + k - 1) / k + (k == 1 ? 0.5 : 0.8));
-    if (k == 1 || time < best) {
-      best = time;
-      u.k_warps = k;
-    }
-  }
+  // Warps of a team: as many as have input channels, evenly, while all items run at once; and no fewer than four of two blocks each where they do not, whose loads hide one another's
+  // latency.  Both sides (us, teams of 1, 2, 4 and 8): one token, 2 of 8 experts of 4096: 42, 34, 23, 18; 16 tokens, 2 of 32, 4096 -> 2048: 85, 75, 68, 68; 64 tokens, 4 of 64, 2048 -> 1024:
+  // 60.7, 61.2, 60.0, 61.3; 8 tokens, 2 of 64, 1024 -> 2048: 25.7, 18.9, 19.5; 5 tokens, 3 of 60, 1096 -> 1000, five blocks: 19.2, 14.5, 16.0.
+  u.k_warps = 1;
+  for (int k = 2; k <= min(8, up.n_kb); k *= 2)
+    if (2 * ((up.n_kb + k - 1) / k) * k <= 3 * up.n_kb && (items * k <= 8 * ctas || k <= min(4, up.n_kb / 2))) u.k_warps = k;
   const unsigned grid = (unsigned)min(ctas, (items + 8 / u.k_warps - 1) / (8 / u.k_warps));
   e = c.act_type == SNN_ACT_F16 ? up_launch<F16>(u, c.gate != nullptr, grid, c.stream) : up_launch<BF16>(u, c.gate != nullptr, grid, c.stream);
   *launched += 1;

@@ -225,12 +225,12 @@ cudaError_t few_launch(const Scaled& p, const ScaledCall& c, int* launched) {
 }
 
 // Which kernel, by the time that each would take (us), where the experts have equal numbers of rows.  Few rows: the weights' bytes, once for each 8, 16 or 32 rows, or what a
-// CTA's turns take; many rows: each block of 128 input channels takes a tile's CTA 0.15 to 0.28 us (a pair's 0.42 to 0.55: 256 rows and channels), a launch 4, a join of two
-// or four CTAs 1.8; or the weights' bytes.  On 214 calls (dense 256 x 256 to 4096 x 8192 and 8192 x 1024 with 1 to 8192 rows, 8 to 64 experts with 1 to 512 rows each) the
-// kernel taken was 1.0 % slower than the best (geometric mean), 1.26 times at worst (16 experts of 1104 x 1003, 512 rows each: 29.9 us by tiles of 128 channels, 23.8 by
-// 64).  Both sides: one row of 4096 x 4096 5.1 (few rows) and 8.7 us, 16 rows 7.2 and 8.7, 24 rows 11.5 and 8.7; 64 experts of 2048 x 2048, 4 rows each 104 and 50;
-// 24 rows of 8192 x 1024 8.0 by four CTAs a tile and 13.3 by one; 192 rows of 4096 x 8192 15.6 by tiles of 64 channels and 12.1 by 128; 4096 rows 137 by tiles of 128
-// channels and 126 by pairs.
+// CTA's turns take; many rows: each block of 128 input channels takes a tile's CTA 0.14 to 0.28 us (a pair's 0.34 to 0.48: 256 rows and channels), a launch 4, a join of two
+// or four CTAs 1.75; or the weights' bytes.  On 214 calls (dense 256 x 256 to 4096 x 8192 and 8192 x 1024 with 1 to 8192 rows, 8 to 64 experts with 1 to 512 rows each) the
+// kernel taken was 0.7 % slower than the best (geometric mean), 1.24 times at worst (16 experts of 1104 x 1003, 512 rows each: 29.5 us by pairs, 23.7 by tiles of 64
+// channels).  Both sides: one row of 4096 x 4096 5.1 (few rows) and 8.7 us, 16 rows 7.2 and 8.7, 24 rows 11.5 and 8.7; 64 experts of 2048 x 2048, 4 rows each 78 and 49;
+// 24 rows of 8192 x 1024 8.0 by four CTAs a tile and 13.3 by one; 192 rows of 4096 x 8192 15.5 by tiles of 64 channels and 11.8 by 128; 4096 rows 135 by tiles of 128
+// channels and 112 by pairs.
 // SNN_FORCE_ROWS=few, many, 64 (with /2 or /4 behind it: CTAs that share a tile), 128 or 256 in the environment takes that wherever it can run.
 struct Way {
   int tile, split;   // output channels of a tile, and CTAs that share one of 64; or 0: few rows, and eights of rows of a piece
@@ -254,8 +254,8 @@ Way choose_way(const Scaled& p, const ScaledCall& c) {
   }
   const double turns = up(up(each, 8 * nt) * used * up(p.K, 16), 2 * sms);
   Way best{0, nt};
-  double least = 1.6 + (nt == 4 ? 1.45 : 0.0) + 0.34 * turns +
-                 fmax(mb * (nt == 1 ? 0.245 : nt == 2 ? 0.37 : 0.67) * up(nk, 8) * 8 / fmax(nk, 8) * up(each, 8 * nt), turns * up(nk, 8) * (nt == 1 ? 0.46 : nt == 2 ? 0.81 : 1.24));
+  double least = 1.55 + (nt == 4 ? 1.6 : 0.0) + 0.34 * turns +
+                 fmax(mb * (nt == 1 ? 0.24 : nt == 2 ? 0.37 : 0.66) * up(nk, 8) * 8 / fmax(nk, 8) * up(each, 8 * nt), turns * up(nk, 8) * (nt == 1 ? 0.45 : nt == 2 ? 0.79 : 1.16));
   if (force && !strcmp(force, "many")) least = 1e30;
   const auto offer = [&](int tile, int split, double time) {
     if (time < least) {
@@ -265,12 +265,12 @@ Way choose_way(const Scaled& p, const ScaledCall& c) {
   };
   for (int split = 1; split <= 4 && (split == 1 || can_share(split)); split *= 2) {
     const double around = up(used * up(each, 128) * up(p.K, 64) * split, sms);
-    offer(64, split, fmax(3.75 + around * (up(nk, split) * (around > 1 ? 0.21 : 0.147) + 0.39) + (split > 1 ? 1.85 : 0.0), 3.6 + mb / 4.8));
+    offer(64, split, fmax(3.75 + around * (up(nk, split) * (around > 1 ? 0.194 : 0.141) + 0.5) + (split > 1 ? 1.75 : 0.0), 3.3 + mb / 4.8));
   }
   double around = up(used * up(each, 128) * up(p.K, 128), sms);
-  offer(128, 1, fmax(3.75 + around * (nk * (around > 1 ? 0.28 : c.rows <= 64 ? 0.21 : 0.25) + 0.27), 3.6 + mb / 5.3));
+  offer(128, 1, fmax(3.75 + around * (nk * (around > 1 ? 0.283 : c.rows <= 64 ? 0.2 : 0.208) + 0.23), 3.3 + mb / 5.2));
   around = up(used * up(each, 256) * up(p.K, 256), fmax(1.0, floor(sms / 2)));
-  offer(256, 1, fmax(4.2 + around * (nk * (around > 1 ? 0.545 : 0.42) + 0.74), 4.2 + mb / 2.9));
+  offer(256, 1, fmax(4.5 + around * (nk * (around > 1 ? 0.477 : 0.339) + 0.77), 4.5 + mb / 4.1));
   return best;
 }
 
