@@ -404,7 +404,7 @@ SNN_API snn_status_t snn_conv_experts_activate(const void* gate_dev, int64_t ld_
  *   h_j    = fn(gate_e(act[t])) * up_e(act[t])               e = ids[j];  fn(up_e(act[t])) without a gate
  *   out[t] = sum_j w_j * down_e(h_j)                         zeros where no expert can be chosen
  * in two launches (three above SNN_MOE_FUSED_TOKENS tokens: the router's comes first).  Sums are fp32; h is kept as the sum of
- * bf16 parts, three of them (all of its 24 bits) for SNN_OUT_F32, two (16 or more) for 16-bit outputs; one rounding to out_type.
+ * three bf16 parts (all of its 24 bits); one rounding to out_type, so that 16-bit outputs are the rounded fp32 ones.
  * The order of the sums depends on the sizes and on which experts the tokens go to, on nothing else.  An infinity or NaN in a token's activations reaches that token's outputs
  * and no others.  For more tokens call route, experts, activate, experts and combine, with the same handles.
  *

@@ -11,6 +11,7 @@ namespace {
 constexpr int MO_N = 8;    // rows of a piece
 constexpr int MO_M = 32;   // output channels of a warp
 constexpr int MO_FEW = SNN_MOE_FUSED_TOKENS * SNN_ROUTE_TOP_MAX;
+constexpr int MO_PARTS = 3;   // bf16 numbers whose sum is a value between the projections: all of its 24 bits
 
 // What lies in the workspace.
 struct MoeWork {
@@ -20,7 +21,7 @@ struct MoeWork {
   float* shares;             // [slots]: the weight of each row in its token's sum
   int32_t *offsets, *ids, *slots;   // of a router in a launch of its own
   float* weights;
-  uint16_t* h;               // [parts][slots][hidden], bf16
+  uint16_t* h;               // [MO_PARTS][slots][hidden], bf16
 };
 long long carve(void* base, int E, int slots, int hidden, MoeWork* w) {
   long long at = 0;
@@ -38,7 +39,7 @@ long long carve(void* base, int E, int slots, int hidden, MoeWork* w) {
   m.ids = static_cast<int32_t*>(take(slots * 4ll));
   m.slots = static_cast<int32_t*>(take(slots * 4ll));
   m.weights = static_cast<float*>(take(slots * 4ll));
-  m.h = static_cast<uint16_t*>(take(6ll * slots * hidden));
+  m.h = static_cast<uint16_t*>(take(2ll * MO_PARTS * slots * hidden));
   if (w) *w = m;
   return at;
 }
@@ -78,7 +79,7 @@ struct UpParams {
   const float* alpha[2];
   const void* act;
   long long ld_act;
-  int tokens, E, C, H, n_mt, n_kb, k_warps, fn, parts, fused;
+  int tokens, E, C, H, n_mt, n_kb, k_warps, fn, fused;
   RouteParams route;   // ids, weights and slots: of a router in a launch of its own, else unused
   MoeWork work;
   Powers pow;
@@ -103,7 +104,8 @@ __device__ __forceinline__ void team_sync(int team, int warps) {
 // First launch.  Up to SNN_MOE_FUSED_TOKENS tokens, every CTA routes for itself (a token a warp, then each choice finds its place among at most 128): less than a launch in
 // front.  Then 8 rows of an expert times 32 output channels, of both the gate and the other projection, are an item of a team of warps, which share the input channels;
 // a team has a run of items.  A team of one warp holds whole sums and needs nobody; larger ones, where there are few items, meet in shared memory.  What comes out
-// behind the activation goes to memory as the sum of `parts` bf16 numbers.
+// behind the activation goes to memory as the sum of three bf16 numbers, whatever the outputs' type: with two, outputs of 16 bits are as near to the formula, but other ones than the
+// rounded fp32 outputs wherever those lie next to a border.
 template <class T, bool GATE>
 __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
   constexpr int G = GATE ? 2 : 1, WIDE = G * MO_M;
@@ -284,8 +286,9 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
       uint16_t* const to = p.work.h + (size_t)(now.r0 + c) * p.H + co;
       float rest = v;
       const bool finite = fabsf(v) <= 3.402823466e38f;
-      for (int k = 0; k < p.parts; ++k) {
-        const bool whole = k + 1 == p.parts || !finite;
+#pragma unroll
+      for (int k = 0; k < MO_PARTS; ++k) {
+        const bool whole = k + 1 == MO_PARTS || !finite;
         const __nv_bfloat16 part = whole ? __float2bfloat16_rn(rest) : __ushort_as_bfloat16((unsigned short)(__float_as_uint(rest) >> 16));
         to[k * step] = __bfloat16_as_ushort(part);
         rest = finite ? rest - __bfloat162float(part) : 0.f;
@@ -354,14 +357,13 @@ __device__ __forceinline__ int4 ld_piece(const int4* p) {
 // each.  The outputs are linear in what the pieces give, so a warp adds its run's products, times the scale and the row's share, to a table of its own [tokens][channels],
 // and the tables are added up at the end, warp by warp, then CTA by CTA: each CTA sends every other one the outputs that that one writes (one barrier; read from there they took
 // two, and 5 tokens with 3 of 60 experts of 1000 -> 1003 17.4 us instead of 16.3).  No atomics, no partial sums in memory, and
-// no waiting until then.  Sums of three parts (fp32 outputs) begin anew every 256 channels: the matrix instructions cut what they add.
+// no waiting until then.  Sums begin anew every 256 channels: the matrix instructions cut what they add.
 // What bounds it, and the first launch, is the expansion and the warp's matrix instruction behind it, which share their issue port: 17.5 cycles for 256 weights and 8 rows in one
 // part, 26 in two; 64 tokens with 4 of 64 experts (2048 -> 1024 -> 2048) 20 us each.  The same on the 5th-generation tensor cores (weights expanded into tensor memory, 128 channels a
 // CTA, clusters of four to eight) took 0.5 us for 128 x 256 weights and came out even: 60.3 and 59.3 us for those 64 tokens, 18.5 and 18.3 for one (2 of 8, 4096): not kept.
 constexpr int MO_LD = MO_M + 1, MO_TABLES = 9;
-template <int PARTS>
 __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
-  constexpr int LD = MO_LD, RING = PARTS == 3 ? 2 : 4;
+  constexpr int LD = MO_LD, RING = 2;
   extern __shared__ int4 pieces[];
   int* const tokens = reinterpret_cast<int*>(pieces + p.choices);   // of the rows
   float* const shares = reinterpret_cast<float*>(tokens + p.choices);
@@ -388,7 +390,7 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   const long long first = units * w / warps, last = units * (w + 1) / warps;
   const size_t step = (size_t)p.choices * p.C;
   TileBits bits, more;
-  uint4 b[RING][PARTS][2];   // the rows of the next blocks of 64, as in the first launch
+  uint4 b[RING][MO_PARTS][2];   // the rows of the next blocks of 64, as in the first launch
   struct Place {
     int piece, kb, e, r0, n;
     const uint16_t* x;
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   };
   auto load_rows = [&](const Place& at, int j) {
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k)
+    for (int k = 0; k < MO_PARTS; ++k)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int c = at.kb * 256 + j * 64 + 32 * h;
@@ -444,15 +446,14 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
     float part[2][4] = {};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      multiply64<BF16, PARTS>(PARTS == 3 ? part : acc, bits, j, b[j % RING], pow);
+      multiply64<BF16, MO_PARTS>(part, bits, j, b[j % RING], pow);
       if (j + RING < 4) load_rows(now, j + RING);
       else if (another) load_rows(then, j + RING - 4);
     }
-    if (PARTS == 3)
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) acc[m][q] += part[m][q];
+      for (int q = 0; q < 4; ++q) acc[m][q] += part[m][q];
     begins = then.kb == 0 || !another;
     if (begins) {   // (a piece's rows are of different tokens)
 #pragma unroll
@@ -501,10 +502,9 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   }
 }
 
-template <int PARTS>
 cudaError_t down_launch(const DownParams& p, unsigned strips, cudaStream_t s) {
   static unsigned long long done = 0;
-  const cudaError_t e = allow_max_smem(moe_down_kernel<PARTS>, &done);
+  const cudaError_t e = allow_max_smem(moe_down_kernel, &done);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -519,7 +519,7 @@ cudaError_t down_launch(const DownParams& p, unsigned strips, cudaStream_t s) {
   cfg.gridDim = dim3(strips * (unsigned)p.cluster);
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = (size_t)MO_TABLES * p.tokens * MO_LD * 4 + (size_t)p.choices * 24;
-  return cudaLaunchKernelEx(&cfg, moe_down_kernel<PARTS>, p);
+  return cudaLaunchKernelEx(&cfg, moe_down_kernel, p);
 }
 
 template <class T>
@@ -557,7 +557,6 @@ cudaError_t moe_forward(const MoeCall& c, int* launched) {
   u.n_mt = up.n_mt;
   u.n_kb = up.n_kb;
   u.fn = c.fn;
-  u.parts = c.out_type == SNN_OUT_F32 ? 3 : 2;
   u.pow = powers();
   // Pieces that the choices make at most: each expert of theirs has one that is not full.
   const long long ctas = 2ll * sm_count(), pieces = ((long long)choices + (long long)min(E, choices) * (MO_N - 1)) / MO_N, items = pieces * ((up.K + MO_M - 1) / MO_M);
@@ -576,7 +575,7 @@ cudaError_t moe_forward(const MoeCall& c, int* launched) {
   const int strips = (down.K + MO_M - 1) / MO_M;
   while (d.cluster < 8 && strips * d.cluster * 2 <= ctas && d.cluster * 8 < pieces * down.n_kb) d.cluster *= 2;
   *launched += 1;
-  return u.parts == 3 ? down_launch<3>(d, (unsigned)strips, c.stream) : down_launch<2>(d, (unsigned)strips, c.stream);
+  return down_launch(d, (unsigned)strips, c.stream);
 }
 
 }  // namespace snn
