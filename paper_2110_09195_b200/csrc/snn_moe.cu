@@ -56,9 +56,9 @@ struct TileBits {
   // the word of the 64 input channels from 64 j on
   __device__ __forceinline__ uint32_t word(int m, int j) const { return j < 2 ? w[m][j & 1].x : w[m][j & 1].y; }
 };
-// 64 input channels' products with P parts of 8 rows: the weights, expanded once, are the M operand.
+// 64 input channels' products with P parts of 8 rows: the weights, expanded once, are the M operand.  The first part's go to `acc`, the others' to `low`.
 template <class T, int P>
-__device__ __forceinline__ void multiply64(float (&acc)[2][4], const TileBits& bits, int j, const uint4 (&b)[P][2], const Powers& pow) {
+__device__ __forceinline__ void multiply64(float (&acc)[2][4], float (&low)[2][4], const TileBits& bits, int j, const uint4 (&b)[P][2], const Powers& pow) {
 #pragma unroll
   for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -69,7 +69,7 @@ __device__ __forceinline__ void multiply64(float (&acc)[2][4], const TileBits& b
 #pragma unroll
       for (int k = 0; k < P; ++k) {
         const uint4& v = b[k][s >> 1];
-        mma_16x8<T>(acc[m], a0, a1, a2, a3, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
+        mma_16x8<T>(k ? low[m] : acc[m], a0, a1, a2, a3, s & 1 ? v.z : v.x, s & 1 ? v.w : v.y);
       }
     }
 }
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
 #pragma unroll
-        for (int i = 0; i < G; ++i) multiply64<T, 1>(acc[i], bits[i], j, b[j], pow);
+        for (int i = 0; i < G; ++i) multiply64<T, 1>(acc[i], acc[i], bits[i], j, b[j], pow);
         if (another) load_rows(then, next, j);
       }
     }
@@ -357,7 +357,8 @@ __device__ __forceinline__ int4 ld_piece(const int4* p) {
 // each.  The outputs are linear in what the pieces give, so a warp adds its run's products, times the scale and the row's share, to a table of its own [tokens][channels],
 // and the tables are added up at the end, warp by warp, then CTA by CTA: each CTA sends every other one the outputs that that one writes (one barrier; read from there they took
 // two, and 5 tokens with 3 of 60 experts of 1000 -> 1003 17.4 us instead of 16.3).  No atomics, no partial sums in memory, and
-// no waiting until then.  Sums begin anew every 256 channels: the matrix instructions cut what they add.
+// no waiting until then.  The matrix instructions cut what they add: sums begin anew every 256 channels, and the lower two parts, which lie below what a sum of the first would keep of
+// them, have sums of their own (fp32 outputs of 5 tokens, 1096 -> 1000 -> 1003, 1.8e-7 off, and 8.6e-7 where all three went into one; no slower).
 // What bounds it, and the first launch, is the expansion and the warp's matrix instruction behind it, which share their issue port: 17.5 cycles for 256 weights and 8 rows in one
 // part, 26 in two; 64 tokens with 4 of 64 experts (2048 -> 1024 -> 2048) 20 us each.  The same on the 5th-generation tensor cores (weights expanded into tensor memory, 128 channels a
 // CTA, clusters of four to eight) took 0.5 us for 128 x 256 weights and came out even: 60.3 and 59.3 us for those 64 tokens, 18.5 and 18.3 for one (2 of 8, 4096): not kept.
@@ -421,18 +422,12 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
 #pragma unroll
     for (int j = 0; j < RING; ++j) load_rows(now, j);
   }
-  float acc[2][4] = {}, alpha[4], share[2];
-  int token[2];
+  float acc[2][4] = {}, low[2][4] = {}, alpha[4];
   bool begins = true;
   for (long long unit = first; unit < last; ++unit) {
-    if (begins) {   // what its outputs need
+    if (begins) {   // the scales that its outputs need
 #pragma unroll
       for (int q = 0; q < 4; ++q) alpha[q] = ld_number(p.alpha + (size_t)now.e * p.n_mt * 16 + strip * MO_M + g + 8 * q);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        share[q] = 2 * t + q < now.n ? shares[now.r0 + 2 * t + q] : 0.f;
-        token[q] = 2 * t + q < now.n ? tokens[now.r0 + 2 * t + q] : 0;
-      }
     }
     bits = more;
     Place then = now;
@@ -446,7 +441,7 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
     float part[2][4] = {};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      multiply64<BF16, MO_PARTS>(part, bits, j, b[j % RING], pow);
+      multiply64<BF16, MO_PARTS>(part, low, bits, j, b[j % RING], pow);
       if (j + RING < 4) load_rows(now, j + RING);
       else if (another) load_rows(then, j + RING - 4);
     }
@@ -459,18 +454,19 @@ __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
 #pragma unroll
       for (int q = 0; q < 2; ++q)
         if (2 * t + q < now.n) {
-          float* const to = mine + token[q] * LD + g;
+          const float share = shares[now.r0 + 2 * t + q];
+          float* const to = mine + tokens[now.r0 + 2 * t + q] * LD + g;
 #pragma unroll
           for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
               float* const at = to + 16 * m + 8 * u;
-              *at = fmaf(share[q], alpha[2 * m + u] * acc[m][2 * u + q], *at);
-              acc[m][2 * u + q] = 0.f;
+              *at = fmaf(share, alpha[2 * m + u] * (acc[m][2 * u + q] + low[m][2 * u + q]), *at);
+              acc[m][2 * u + q] = low[m][2 * u + q] = 0.f;
             }
         } else {
 #pragma unroll
-          for (int m = 0; m < 2; ++m) acc[m][q] = acc[m][2 + q] = 0.f;
+          for (int m = 0; m < 2; ++m) acc[m][q] = acc[m][2 + q] = low[m][q] = low[m][2 + q] = 0.f;
         }
       __syncwarp();
     }

@@ -73,3 +73,17 @@ def test_the_third_part(snn, T, hidden, gated, act, out):  # noqa: F811
         between = between * (x @ w_gate.T)
     y = h.forward(x.to(act), torch.zeros(T, 1, device="cuda"), 1, out=torch.empty(T, 75, dtype=out, device="cuda"))
     assert torch.equal(y, (between @ w_down.T).float().to(out))
+
+
+@pytest.mark.parametrize("T", [1, 8, 9])
+@pytest.mark.parametrize("hidden", [256, 512])
+def test_sums_of_the_lower_parts(snn, T, hidden):  # noqa: F811
+    """256 times 65536 + 255.9921875.  The upper 8 bits add up to 2^24 and the lower ones to 65534, both exactly; so is their sum, 16842750, and twice that.  (In one sum that the matrix instructions cut,
+    what is below 2 would be lost as soon as 2^24 is near.)"""
+    value = 65536 + 255.9921875
+    down, w_down = _layer(snn, hidden, 8, 510)
+    up, w_up = _layer(snn, 16, hidden, 511, lambda w: value * w_down[0] * w[:, 5])
+    x = torch.zeros(T, 16, dtype=BF16, device="cuda")
+    x[:, 5] = 1.0
+    y = snn.SnnConvMoe(up, down, fn=snn.FN_NONE).forward(x, torch.zeros(T, 1, device="cuda"), 1, out_type=snn.OUT_F32)
+    assert value * hidden == 16842750 * (hidden // 256) and (y[:, 0] == value * hidden).all()
