@@ -106,7 +106,10 @@ __device__ __forceinline__ void team_sync(int team, int warps) {
 // a team has a run of items.  A team of one warp holds whole sums and needs nobody; larger ones, where there are few items, meet in shared memory.  What comes out
 // behind the activation goes to memory as the sum of three bf16 numbers, whatever the outputs' type: with two, outputs of 16 bits are as near to the formula, but other ones than the
 // rounded fp32 outputs wherever those lie next to a border.
-template <class T, bool GATE>
+// ANEW: sums begin anew every 256 channels, as in the second launch; for warps with more than two blocks of these.  The others' sums are cut 32 times at most; to begin anew
+// costs them 2 to 4 % (64 tokens, 4 of 64 experts, 2048 -> 1024 -> 2048: 66.7 and 68.8 us).  3 tokens, 16384 channels, activations of sizes from 1 to 2^-12: fp32 outputs 3.0e-7 off, and
+// 3.0e-6 in sums that go on; 64 tokens, 4096 channels, two blocks a warp: 3.1e-7 and 6.2e-7.
+template <class T, bool GATE, bool ANEW>
 __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
   constexpr int G = GATE ? 2 : 1, WIDE = G * MO_M;
   __shared__ float red_both[2][8][MO_N][WIDE + 1];
@@ -274,12 +277,21 @@ __global__ void __launch_bounds__(256, 2) moe_up_kernel(const UpParams p) {
         }
       }
       if (another) load_bits(then, next);
+      float anew[G][2][4] = {};
+      float (&part)[G][2][4] = ANEW ? anew : acc;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
 #pragma unroll
-        for (int i = 0; i < G; ++i) multiply64<T, 1>(acc[i], acc[i], bits[i], j, b[j], pow);
+        for (int i = 0; i < G; ++i) multiply64<T, 1>(part[i], part[i], bits[i], j, b[j], pow);
         if (another) load_rows(then, next, j);
       }
+      if (ANEW)
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[i][m][q] += anew[i][m][q];
     }
     // 8 bits at a time, cut (the rests are exact), the last part rounded; an infinity or NaN in the first
     auto write = [&](int c, int co, float v) {
@@ -518,9 +530,13 @@ cudaError_t down_launch(const DownParams& p, unsigned strips, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, moe_down_kernel, p);
 }
 
+template <class T, bool ANEW>
+cudaError_t up_launch(const UpParams& p, bool gate, unsigned ctas, cudaStream_t s) {
+  return gate ? launch_dependent(moe_up_kernel<T, true, ANEW>, ctas, 256, 0, s, p) : launch_dependent(moe_up_kernel<T, false, ANEW>, ctas, 256, 0, s, p);
+}
 template <class T>
 cudaError_t up_launch(const UpParams& p, bool gate, unsigned ctas, cudaStream_t s) {
-  return gate ? launch_dependent(moe_up_kernel<T, true>, ctas, 256, 0, s, p) : launch_dependent(moe_up_kernel<T, false>, ctas, 256, 0, s, p);
+  return p.n_kb > 2 * p.k_warps ? up_launch<T, true>(p, gate, ctas, s) : up_launch<T, false>(p, gate, ctas, s);
 }
 
 }  // namespace

@@ -87,3 +87,24 @@ def test_sums_of_the_lower_parts(snn, T, hidden):  # noqa: F811
     x[:, 5] = 1.0
     y = snn.SnnConvMoe(up, down, fn=snn.FN_NONE).forward(x, torch.zeros(T, 1, device="cuda"), 1, out_type=snn.OUT_F32)
     assert value * hidden == 16842750 * (hidden // 256) and (y[:, 0] == value * hidden).all()
+
+
+@pytest.mark.parametrize("T", [1, 7, 12])
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("act,unit", [(BF16, 1.0), (F16, 2.0 ** -9)])
+def test_long_sums_are_rounded_and_not_cut(snn, T, gated, act, unit):  # noqa: F811
+    """32768 channels, in 128 blocks of 256 one of which is not zero; the eight warps that share them have every eighth block.  First 2^24 or, every second warp,
+    -2^24, then 15 times 1.5 where it was 2^24: 90 in all.  Rounded to nearest, 2^24 + 1.5 misses by half of 2 at most, 60 times, and adding up the warps' sums, none
+    above 2^24 + 32, seven times: 67.  Cut, the 1.5 are lost: 90.  With a gate it is the same projection: the square, and its rounding."""
+    up, w = _layer(snn, 32768, 8, 520, lambda w: torch.tensor([1.0] + [0.0] * 7))
+    down, w_down = _layer(snn, 8, 40, 521)
+    v = torch.zeros(32768, dtype=torch.float64, device="cuda")
+    for b in range(128):
+        v[256 * b + 37 * b % 256] = (2.0 ** 24 if b < 8 else 1.5) * (1.0 if b % 2 == 0 else -1.0 if b < 8 else 0.0)
+    assert v.sum() == 90
+    x = (v * w[0] * unit).to(act).expand(T, -1).contiguous()
+    h = snn.SnnConvMoe(up, down, gate=up if gated else None, fn=snn.FN_NONE)
+    y = h.forward(x, torch.zeros(T, 1, device="cuda"), 1, out_type=snn.OUT_F32).double() / w_down[:, 0] / unit
+    if gated:
+        y = torch.sqrt(y / unit)
+    assert ((y - 90).abs() <= 67 + 2.0 ** -22 * 200).all()
