@@ -44,17 +44,21 @@ __global__ void __launch_bounds__(256) activate_kernel(const ActivateParams p) {
   u.load(static_cast<const E*>(p.up) + r * p.ld_up + c);
   if (GATE) g.load(static_cast<const E*>(p.gate) + r * p.ld_gate + c);
   float2 v[4];
+  auto all = [&](auto near) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const float2 a = u.pair(q);
-    const uint64_t w = pair_of(a.x, a.y);
-    if (GATE) {
-      const float2 b = g.pair(q);
-      v[q] = floats_of(mul2(activated2(p.fn, pair_of(b.x, b.y)), w));
-    } else {
-      v[q] = floats_of(activated2(p.fn, w));
+    for (int q = 0; q < 4; ++q) {
+      const float2 a = u.pair(q);
+      const uint64_t w = pair_of(a.x, a.y);
+      if (GATE) {
+        const float2 b = g.pair(q);
+        v[q] = floats_of(mul2(activated2<decltype(near)::value>(p.fn, pair_of(b.x, b.y)), w));
+      } else {
+        v[q] = floats_of(activated2<decltype(near)::value>(p.fn, w));
+      }
     }
-  }
+  };
+  if (p.fn == SNN_FN_SILU && !((GATE ? g.lowest(g) : u.lowest(u)) < SILU_NEAR)) all(std::true_type{});
+  else all(std::false_type{});
   const long long at = r * p.ld_out + c;
   if (p.out_type == SNN_OUT_F32) {
     float4* const out = reinterpret_cast<float4*>(static_cast<float*>(p.out) + at);
@@ -142,20 +146,24 @@ __global__ void __launch_bounds__(256) quantise_kernel(const QuantiseParams p) {
         else g[h].zero();
       }
     }
+    auto all = [&](auto near) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const float2 a = u[q >> 2].pair(q & 3);
-      uint64_t w = pair_of(a.x, a.y);
-      if (GATE) {
-        const float2 h = g[q >> 2].pair(q & 3);
-        w = mul2(activated2(p.fn, pair_of(h.x, h.y)), w);
-      } else {
-        w = activated2(p.fn, w);
+      for (int q = 0; q < 8; ++q) {
+        const float2 a = u[q >> 2].pair(q & 3);
+        uint64_t w = pair_of(a.x, a.y);
+        if (GATE) {
+          const float2 h = g[q >> 2].pair(q & 3);
+          w = mul2(activated2<decltype(near)::value>(p.fn, pair_of(h.x, h.y)), w);
+        } else {
+          w = activated2<decltype(near)::value>(p.fn, w);
+        }
+        const float2 f = floats_of(w);
+        v[2 * q] = f.x;
+        v[2 * q + 1] = f.y;
       }
-      const float2 f = floats_of(w);
-      v[2 * q] = f.x;
-      v[2 * q + 1] = f.y;
-    }
+    };
+    if (p.fn == SNN_FN_SILU && !((GATE ? g[0].lowest(g[1]) : u[0].lowest(u[1])) < SILU_NEAR)) all(std::true_type{});
+    else all(std::false_type{});
   }
   const uint32_t mine = 0xffu << (threadIdx.x & 24);
   float most = 0.f;
