@@ -371,9 +371,11 @@ __device__ __forceinline__ int4 ld_piece(const int4* p) {
 // two, and 5 tokens with 3 of 60 experts of 1000 -> 1003 17.4 us instead of 16.3).  No atomics, no partial sums in memory, and
 // no waiting until then.  The matrix instructions cut what they add: sums begin anew every 256 channels, and the lower two parts, which lie below what a sum of the first would keep of
 // them, have sums of their own (fp32 outputs of 5 tokens, 1096 -> 1000 -> 1003, 1.8e-7 off, and 8.6e-7 where all three went into one; no slower).
-// What bounds it, and the first launch, is the expansion and the warp's matrix instruction behind it, which share their issue port: 17.5 cycles for 256 weights and 8 rows in one
-// part, 26 in two; 64 tokens with 4 of 64 experts (2048 -> 1024 -> 2048) 20 us each.  The same on the 5th-generation tensor cores (weights expanded into tensor memory, 128 channels a
-// CTA, clusters of four to eight) took 0.5 us for 128 x 256 weights and came out even: 60.3 and 59.3 us for those 64 tokens, 18.5 and 18.3 for one (2 of 8, 4096): not kept.
+// What bounds it, and the first launch, is no single unit: 64 tokens with 4 of 64 experts (2048 -> 1024 -> 2048) take 38 and 36 us with cold caches at 44 to 46 % of the issue slots, 34 to
+// 41 % of the integer units, 20 and 33 % of the tensor pipe and 6 to 11 % of the memory rate.  The four or five warps of a scheduler wait for fixed latencies (1.5 to 1.7 of a warp's cycles
+// for each that it issues), the multiplications' pipe (1.1 to 1.5), memory (0.9 to 1.2) and, in the first launch, instructions (1.5).  A lone warp takes 17.5 cycles for 256 weights and
+// 8 rows in one part, 26 in two.  The same on the 5th-generation tensor cores (weights expanded into tensor memory, 128 channels a CTA, clusters of four to eight), then in two parts,
+// took 0.5 us for 128 x 256 weights and came out even: 60.3 and 59.3 us for those 64 tokens, 18.5 and 18.3 for one (2 of 8, 4096): not kept.
 constexpr int MO_LD = MO_M + 1, MO_TABLES = 9;
 __global__ void __launch_bounds__(256, 2) moe_down_kernel(const DownParams p) {
   constexpr int LD = MO_LD, RING = 2;
@@ -573,7 +575,7 @@ cudaError_t moe_forward(const MoeCall& c, int* launched) {
   // Pieces that the choices make at most: each expert of theirs has one that is not full.
   const long long ctas = 2ll * sm_count(), pieces = ((long long)choices + (long long)min(E, choices) * (MO_N - 1)) / MO_N, items = pieces * ((up.K + MO_M - 1) / MO_M);
   // Warps of a team: as many as have input channels, evenly, while all items run at once; and no fewer than four of two blocks each where they do not, whose loads hide one another's
-  // latency.  Both sides (us, teams of 1, 2, 4 and 8): one token, 2 of 8 experts of 4096: 42, 34, 23, 18; 16 tokens, 2 of 32, 4096 -> 2048: 85, 75, 68, 68; 64 tokens, 4 of 64, 2048 -> 1024:
+  // latency.  Both sides (us, teams of 1, 2, 4 and 8; with two parts in place of three): one token, 2 of 8 experts of 4096: 42, 34, 23, 18; 16 tokens, 2 of 32, 4096 -> 2048: 85, 75, 68, 68; 64 tokens, 4 of 64, 2048 -> 1024:
   // 60.7, 61.2, 60.0, 61.3; 8 tokens, 2 of 64, 1024 -> 2048: 25.7, 18.9, 19.5; 5 tokens, 3 of 60, 1096 -> 1000, five blocks: 19.2, 14.5, 16.0.
   u.k_warps = 1;
   for (int k = 2; k <= min(8, up.n_kb); k *= 2)

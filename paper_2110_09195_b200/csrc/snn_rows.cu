@@ -30,7 +30,7 @@ struct ActivateParams {
   Divisor each;   // eights of a row, or 256ths
 };
 
-// A thread has 8 neighbouring columns.  Bound by memory: each value is read and written once, and leaves the caches first (8191 x 8192 gated bf16 values behind SILU 64 us, 6.3 TB/s).
+// A thread has 8 neighbouring columns.  Bound by memory: each value is read and written once, and leaves the caches first (8191 x 8192 gated bf16 values behind SILU 66 us, 6.1 TB/s).
 template <class Y, bool GATE>
 __global__ void __launch_bounds__(256) activate_kernel(const ActivateParams p) {
   const uint32_t i = blockIdx.x * 256 + threadIdx.x;
@@ -108,7 +108,7 @@ __device__ __forceinline__ uint64_t quotients(uint64_t v, uint64_t minus_scale, 
 
 // 8 lanes have a block of 128 channels of a row, 8 neighbouring ones and the 8 that lie 64 behind them each: the largest magnitude by three shuffles, two divisions for the
 // scale, three or five multiplications and additions for each value.  ODD: columns, row lengths or pointers that are not multiples of 8 values.  Bound by
-// memory, nearly by the number of instructions (8191 x 4096 gated bf16 values behind SILU: 16 lanes a block, two corrections always and comparisons against infinity took 46 us, now 33: 5.2 TB/s, 75 % of the issue slots).
+// memory, nearly by the number of instructions (8191 x 4096 gated bf16 values behind SILU: 16 lanes a block, two corrections always and comparisons against infinity took 46 us, now 34: 5.0 TB/s, 74 % of the issue slots).
 template <class Y, bool GATE, bool ODD>
 __global__ void __launch_bounds__(256) quantise_kernel(const QuantiseParams p) {
   const uint32_t i = blockIdx.x * 32 + (threadIdx.x >> 3);

@@ -17,7 +17,8 @@ namespace {
 //   CG = 1, N = 128 or 64: fewer rows, more tiles, for problems that would leave SMs without any; of 64 a tile may be shared by two or four CTAs of a cluster, each a
 //   run of the input channels.  What bounds these is a block's waits, issues and commits: 300 to 400 cycles of one warp, so two warps do that in turns (one row of 4096 x
 //   4096 11.0 and 10.7 us), and of narrow stages two blocks go together (8.7).
-// 4096 rows of 4096 x 8192 take 112 us in a short run (2.45 PFLOP/s), 8192 rows 222 in a long one at the power limit (2.48).
+// 4096 rows of 4096 x 8192 take 112 us in a short run (2.45 PFLOP/s), 136 to 138 among other calls, each with inputs that the caches do not hold (2.0); 8192 rows 222 in a long run at the power
+// limit (2.48).
 constexpr int ST_ROWS = 128;          // of a CTA's tile
 constexpr int ST_MAX_STAGES = 16;
 constexpr int ST_OUT_WARPS = 8;
