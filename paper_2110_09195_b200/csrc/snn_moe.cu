@@ -372,7 +372,7 @@ __device__ __forceinline__ int4 ld_piece(const int4* p) {
 // no waiting until then.  The matrix instructions cut what they add: sums begin anew every 256 channels, and the lower two parts, which lie below what a sum of the first would keep of
 // them, have sums of their own (fp32 outputs of 5 tokens, 1096 -> 1000 -> 1003, 1.8e-7 off, and 8.6e-7 where all three went into one; no slower).
 // What bounds it, and the first launch, is no single unit: 64 tokens with 4 of 64 experts (2048 -> 1024 -> 2048) take 38 and 36 us with cold caches at 44 to 46 % of the issue slots, 34 to
-// 41 % of the integer units, 20 and 33 % of the tensor pipe and 6 to 11 % of the memory rate.  The four or five warps of a scheduler wait for fixed latencies (1.5 to 1.7 of a warp's cycles
+// 41 % of the integer units, 20 and 33 % of the tensor pipe and 6 to 11 % of the memory rate.  The four warps of a scheduler wait for fixed latencies (1.5 to 1.7 of a warp's cycles
 // for each that it issues), the multiplications' pipe (1.1 to 1.5), memory (0.9 to 1.2) and, in the first launch, instructions (1.5).  A lone warp takes 17.5 cycles for 256 weights and
 // 8 rows in one part, 26 in two.  The same on the 5th-generation tensor cores (weights expanded into tensor memory, 128 channels a CTA, clusters of four to eight), then in two parts,
 // took 0.5 us for 128 x 256 weights and came out even: 60.3 and 59.3 us for those 64 tokens, 18.5 and 18.3 for one (2 of 8, 4096): not kept.
